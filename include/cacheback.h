@@ -362,6 +362,164 @@ cb_status cb_select_noalloc(int32_t n, const float *const *scores, const int64_t
  * since the last read.  Blocks the host. */
 cb_status cb_select_noalloc_status(void *stream);
 
+/*
+ * ---- The receiver's side: rotary positions, rows held in 4 bits, attention over them ----
+ *
+ * The paper's receiver re-prefills its message (App. C.3); these calls are what a receiver needs
+ * that takes K/V rows instead, and whose cache or message is to be small.  They follow the same
+ * conventions as the calls above; head_dim, the heads and the limits are the context's.
+ */
+
+/* cb_create without the scratch of cb_score and cb_select, for a context that only packs, unpacks,
+ * turns, attends, compacts or gathers: max_positions and n_layers then cost no memory.  cb_score and
+ * cb_select refuse such a context with CB_EINVAL.  The room for cb_attend's partial results is
+ * allocated here (other contexts allocate it in their first cb_attend).  Errors as cb_create. */
+cb_status cb_create_receiver(const cb_config *cfg, cb_ctx **out);
+
+/*
+ * Rotary embedding.  Pair k (k < dims / 2) of a head turns by position * f_k:
+ *   f_k = base^(-2k / dims)                                       scaling 0 (none)
+ *   f_k = base^(-2k / dims) / factor                              scaling 1 (linear)
+ *   f_k = base^(-2k / dims) * (1 - w_k + w_k / factor)            scaling 2 (by parts: fast pairs keep
+ *         their frequency, slow ones are stretched), with w_k = clamp((k - lo) / (hi - lo), 0, 1),
+ *         D(t) = dims * ln(original / (2 pi t)) / (2 ln base) (the pair that turns t times over
+ *         `original` positions), lo = max(floor(D(beta_fast)), 0), hi = min(ceil(D(beta_slow)),
+ *         dims - 1), hi = lo + 0.001 where hi <= lo
+ * and the turned pair is multiplied by `attention`.  Elements from dims on are left as they are.
+ *   style      0: pairs (k, k + dims / 2); 1: pairs (2k, 2k + 1)
+ *   dims       rotary part of the head, a multiple of 16 up to head_dim; 0: the whole head
+ *   factor     >= 1 (scalings 1 and 2); original >= 1, beta_fast > beta_slow > 0 (scaling 2; 0 for the
+ *              betas takes 32 and 1)
+ *   attention  > 0; 0 takes 1, and 0.1 ln(factor) + 1 with scaling 2
+ *   inverse    1: the transposed turn (by -position * f_k, multiplied by `attention` as well), which
+ *              is the gradient of the forward one
+ */
+typedef struct {
+    double base;
+    int32_t style, dims, scaling;
+    double factor;
+    int64_t original;
+    double beta_fast, beta_slow;
+    double attention;
+    int32_t inverse;
+} cb_rope;
+
+/* Vectors to turn: X[l][r][h][:] at x + l*s_layer + r*s_tok + h*s_head (l < n_layers, r < n_tokens,
+ * h < n_heads; any counts, not the context's), written to y with its own strides.  Strides as the
+ * shared conventions say; those of a dimension of size one are not used.  y is x with the same
+ * strides (in place) or does not touch x's memory, and no vector of the call may be written by
+ * another.  Token r is at position pos[r] (device int32, 4-byte aligned) or, where pos is NULL, at
+ * pos0 + r, which stays within +-2^40; any sign. */
+typedef struct {
+    const void *x;
+    void *y;
+    int32_t n_layers, n_heads;
+    int64_t n_tokens;
+    int64_t s_layer, s_tok, s_head;
+    int64_t o_layer, o_tok, o_head;
+    const int32_t *pos;
+    int64_t pos0;
+} cb_vectors;
+
+/* Turn n sets of vectors (e.g. the queries and the keys of a step) in one launch per 64 sets; sums
+ * and products are fp32, each result is rounded once to bf16.  A set without tokens, heads or layers
+ * is skipped.  Errors: CB_EINVAL (pointers, strides, cb_rope values, x and y overlapping),
+ * CB_ESHAPE (n < 1, negative counts). */
+cb_status cb_rotary(cb_ctx *ctx, int32_t n, const cb_vectors *sets, const cb_rope *rope, void *stream);
+
+/*
+ * A cache or message held in 4 bits.  The value of element e of a row is c * s: c in -7..7 the
+ * element's code, s the scale of the group of 32 neighbouring elements that e is in.  A scale is a
+ * number of 5 significant bits within 2^-20 .. 2^13, held as bf16, so that every value is a bf16
+ * number exactly.
+ *   codes   head_dim / 2 bytes a row: bits 4i..4i+3 of its 32-bit word w (little endian) hold c + 8
+ *           of element 8w + 2i (i < 4) or 8w + 2(i - 4) + 1 (i >= 4)
+ *   scales  head_dim / 32 bf16 a row, group by group
+ * Both arrays have the same index order.  The strides count ELEMENTS of rows of head_dim elements and
+ * are multiples of head_dim: row (l, g, t) is at o = l*s_layer + g*s_head + t*s_pos, its codes at byte
+ * o / 2 of k (v), its scales at byte o / 16 of k_scale (v_scale); K and V share them.  Paged layout
+ * (pages != NULL) as in cb_kv: row t is row t % page_size of page pages[t / page_size], s_page
+ * elements apart; n_pages * s_page may not pass 2^31 * head_dim.
+ *   alignment  codes 16 bytes, scales 8 (head_dim 128) or 4 (head_dim 64)
+ *   T          rows that may be read or written, >= 0
+ *   length     device int32 (4-byte aligned) or NULL.  cb_attend then reads the first
+ *              min(max(*length, 0), T) rows, as *length is when the kernel runs: a captured graph
+ *              follows a cache that grows.  The other calls do not read it.
+ * Rows are written by cb_pack, or by the caller in this format.  A scale that is not within
+ * 0 .. 2^13 (NaN and infinities too) reads as 0, and a block-table entry outside [0, n_pages) as rows
+ * of zeros that cb_pack does not write; the next cb_sync_status reports CB_EDEVICE.  Rows from T (or
+ * *length) on may hold anything. */
+typedef struct {
+    void *k, *v;
+    void *k_scale, *v_scale;
+    int64_t T;
+    int64_t s_layer, s_head, s_pos;
+    const int32_t *pages;
+    int32_t page_size;
+    int64_t s_page, n_pages;
+    const int32_t *length;
+} cb_packed;
+
+/*
+ * Pack K/V rows into 4 bits (cb_compact whose message is held in 4 bits, or the appending of new
+ * rows to a cache): for every sender i, layer l < n_layers, KV head g and j < count[i]
+ *     row (layer + l, g, at) of caches[i] = row (l, g, idx[i][j]) of senders[i],
+ *     at = rows[i][j], or offset[i] + j without rows.
+ * A group's scale is the smallest number of 5 significant bits that is at least max|x| / 7, within
+ * 2^-20 .. 2^13; the code is x / s rounded to the nearest whole number, halves away from zero.
+ * |x| above 7 * 2^13 (infinity too) is held as 7 * 2^13, NaN as 0, and the next cb_sync_status
+ * reports CB_EDEVICE.  Every bit written is a function of the row alone.
+ *   senders   K and V as cb_compact reads them (strided or paged; device or mapped host memory);
+ *             s_layer counts from the first layer of the call
+ *   idx       device int32 [count[i]], 4-byte aligned; idx or idx[i] NULL: rows 0 .. count[i] - 1
+ *   rows      device int32 [count[i]], 4-byte aligned; rows or rows[i] NULL: offset[i] + j, which has
+ *             to lie within caches[i].T.  Of equal entries one row stays, which one is not defined.
+ *   layer, n_layers   layers of the cache that the call writes: a whole message, or one layer of a
+ *             forward pass
+ * An idx or rows entry out of range skips its row and is reported by cb_sync_status as CB_EDEVICE.
+ * Errors: CB_EINVAL, CB_ESHAPE (layers, T above the limit, too many rows), CB_EBUDGET (count < 0,
+ * rows past caches[i].T).
+ */
+cb_status cb_pack(cb_ctx *ctx, int32_t n, const cb_kv *senders, const int32_t *const *idx, const int64_t *count,
+                  const cb_packed *caches, const int64_t *offset, const int32_t *const *rows, int32_t layer,
+                  int32_t n_layers, void *stream);
+
+/* Restore packed rows as bf16, all layers: cb_compact from 4-bit caches (exact: every value is a bf16
+ * number).  Arguments as cb_compact's; idx or idx[i] NULL: rows 0 .. count[i] - 1. */
+cb_status cb_unpack(cb_ctx *ctx, int32_t n, const cb_packed *caches, const int32_t *const *idx, const int64_t *count,
+                    void *k_out, void *v_out, int64_t out_capacity, const int64_t *out_offset, int64_t o_layer,
+                    int64_t o_head, void *stream);
+
+/* Queries of one sequence: Q[r][h][:] at q + r*s_tok + h*s_head, r < m; the outputs at
+ * out + r*o_tok + h*o_head (bf16; not overlapping anything the call reads); lse (fp32 [m][n_q_heads], contiguous,
+ * 4-byte aligned) or NULL. */
+typedef struct {
+    const void *q;
+    void *out;
+    float *lse;
+    int32_t m;
+    int64_t s_tok, s_head;
+    int64_t o_tok, o_head;
+} cb_attend_query;
+
+/*
+ * Attention of m query tokens over a 4-bit cache, one layer: with L rows in the cache, query token r
+ * stands at position L - m + r (its own row is the cache's row there: pack a step's new K/V first) and
+ *     out[r][h] = sum_t a_t v_t,  a = softmax over the rows t that r sees of softmax_scale * <q_{r,h}, k_t>
+ *     lse[r][h] = ln sum_t exp(softmax_scale * <q_{r,h}, k_t>)
+ * over KV head h / G.  causal: r sees rows up to its own position; window > 0 (only with causal): and
+ * no rows at or below position - window.  Otherwise r sees all L rows.  A token that sees no row gets
+ * out = 0 and lse = -infinity.  Logits, weights' sums and outputs are summed in fp32, weights enter
+ * their product with the values as fp16 scaled to the row's largest, and out is rounded once to bf16.  With lse a caller joins
+ * attention over several caches.  m may differ between sequences; m = 0 skips a sequence.
+ *   caches    T <= max_positions; sequences may share one cache
+ * Errors: CB_EINVAL, CB_ESHAPE (n above max_senders, m above max_query_tokens, T above max_positions,
+ * layer), CB_ENOMEM (no room for the partial results: see cb_create_receiver; a first call inside a
+ * stream capture on a context of cb_create).
+ */
+cb_status cb_attend(cb_ctx *ctx, int32_t layer, int32_t n, const cb_packed *caches, const cb_attend_query *queries,
+                    int32_t causal, int64_t window, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,10 +14,11 @@ from __future__ import annotations
 from typing import List, Optional, Sequence
 
 from .binding import (CB_EBUDGET, CB_ECUDA, CB_EDEVICE, CB_EINVAL, CB_ENOMEM, CB_ESHAPE, CB_ETIMEOUT, CB_OK, EXPORTED,
-                      LIB_PATH, CacheBack, CBError, PagedKV, budget, chain_budget, load_library)
+                      LIB_PATH, CacheBack, CBError, PackedKV, PagedKV, Receiver, Rotary, budget, chain_budget,
+                      load_library)
 
 __all__ = ["CacheBack", "CBError", "PagedKV", "budget", "chain_budget", "load_library", "LIB_PATH", "EXPORTED",
-           "Filter", "Chain",
+           "Filter", "Chain", "Receiver", "PackedKV", "Rotary",
            "CB_OK", "CB_EINVAL", "CB_ESHAPE", "CB_EBUDGET", "CB_ENOMEM", "CB_ECUDA", "CB_ETIMEOUT", "CB_EDEVICE"]
 
 
@@ -114,6 +115,16 @@ class Filter:
 
     def indices(self) -> List:
         return [x[:b] for x, b in zip(self.idx, self.budgets)]
+
+    def pack(self, held: Optional[PackedKV] = None, stream=None) -> PackedKV:
+        """compact into 4 bits: the selected K/V rows of every layer as a PackedKV of `capacity` rows (0.28
+        of compact's bytes), senders back to back; `held` (room for them) is written where given."""
+        if held is None:
+            nL, Hkv, _, d = self.Ks[0].shape
+            held = PackedKV.empty(nL, Hkv, max(self.capacity, 1), d, self.k_out.device)
+        self.cb.pack(self.Ks, self.Vs, [held] * len(self.Ks), self.offsets, idx=self.idx, counts=self.budgets, stream=stream)
+        held.T = self.capacity
+        return held
 
     # -- message encodings (Sec. 3.1 "State Representation", App. C.3) ------------------
     def message_rows(self, tables: Sequence, stream=None):

@@ -22,7 +22,8 @@ STATUS_NAMES = ["CB_OK", "CB_EINVAL", "CB_ESHAPE", "CB_EBUDGET", "CB_ENOMEM", "C
 EXPORTED = ["cb_config_init", "cb_create", "cb_score", "cb_budget", "cb_select", "cb_compact",
             "cb_sync_status", "cb_destroy", "cb_last_error", "cb_scratch_bytes", "cb_score_path", "cb_select_noalloc",
             "cb_select_noalloc_status", "cb_gather", "cb_chain_budget", "cb_compact_rope",
-            "cb_enable_stage_timing", "cb_stage_times", "cb_set_wait_limit", "cb_set_score_sms"]
+            "cb_enable_stage_timing", "cb_stage_times", "cb_set_wait_limit", "cb_set_score_sms",
+            "cb_create_receiver", "cb_rotary", "cb_pack", "cb_unpack", "cb_attend"]
 
 
 class CBError(RuntimeError):
@@ -52,6 +53,35 @@ class cb_query(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("m", ctypes.c_int32), ("s_layer", ctypes.c_int64),
                 ("s_tok", ctypes.c_int64), ("s_head", ctypes.c_int64), ("k_self", ctypes.c_void_p),
                 ("ks_layer", ctypes.c_int64), ("ks_tok", ctypes.c_int64), ("ks_head", ctypes.c_int64)]
+
+
+class cb_rope(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("style", ctypes.c_int32), ("dims", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("factor", ctypes.c_double), ("original", ctypes.c_int64),
+                ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double), ("attention", ctypes.c_double),
+                ("inverse", ctypes.c_int32)]
+
+
+class cb_vectors(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("n_layers", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("n_tokens", ctypes.c_int64), ("s_layer", ctypes.c_int64),
+                ("s_tok", ctypes.c_int64), ("s_head", ctypes.c_int64), ("o_layer", ctypes.c_int64),
+                ("o_tok", ctypes.c_int64), ("o_head", ctypes.c_int64), ("pos", ctypes.c_void_p),
+                ("pos0", ctypes.c_int64)]
+
+
+class cb_packed(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("T", ctypes.c_int64), ("s_layer", ctypes.c_int64),
+                ("s_head", ctypes.c_int64), ("s_pos", ctypes.c_int64), ("pages", ctypes.c_void_p),
+                ("page_size", ctypes.c_int32), ("s_page", ctypes.c_int64), ("n_pages", ctypes.c_int64),
+                ("length", ctypes.c_void_p)]
+
+
+class cb_attend_query(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("m", ctypes.c_int32),
+                ("s_tok", ctypes.c_int64), ("s_head", ctypes.c_int64), ("o_tok", ctypes.c_int64),
+                ("o_head", ctypes.c_int64)]
 
 
 _LIB = None
@@ -112,6 +142,19 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.cb_enable_stage_timing.restype = ctypes.c_int
     lib.cb_stage_times.argtypes = [P, ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)]
     lib.cb_stage_times.restype = ctypes.c_int
+    lib.cb_create_receiver.argtypes = lib.cb_create.argtypes
+    lib.cb_create_receiver.restype = ctypes.c_int
+    lib.cb_rotary.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_vectors), ctypes.POINTER(cb_rope), P]
+    lib.cb_rotary.restype = ctypes.c_int
+    lib.cb_pack.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_kv), P, P, ctypes.POINTER(cb_packed), P, P,
+                            ctypes.c_int32, ctypes.c_int32, P]
+    lib.cb_pack.restype = ctypes.c_int
+    lib.cb_unpack.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_packed), P, P, P, P, ctypes.c_int64, P,
+                              ctypes.c_int64, ctypes.c_int64, P]
+    lib.cb_unpack.restype = ctypes.c_int
+    lib.cb_attend.argtypes = [P, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(cb_packed),
+                              ctypes.POINTER(cb_attend_query), ctypes.c_int32, ctypes.c_int64, P]
+    lib.cb_attend.restype = ctypes.c_int
     if path is None:
         _LIB = lib
     return lib
@@ -229,8 +272,109 @@ def query_desc(Q, Kself=None) -> cb_query:
     return cb_query(Q.data_ptr(), Q.size(1), st[0], st[1], st[2], Kself.data_ptr(), ks[0], ks[1], ks[2])
 
 
+class PackedKV:
+    """A cache or message held in 4 bits (cb_packed): codes c in -7..7 and one scale s for every 32
+    neighbouring elements of a row; an element's value is c * s.
+
+    k, v:                uint8 codes, [nL][Hkv][T][d / 2]; paged: [nL][n_pages][page_size][Hkv][d / 2]
+    k_scale, v_scale:    bf16 scales, the same index order with d / 32 in the last place; any strides
+                         that step over rows alike in codes and scales
+    T:                   rows cached (default: all there is room for); may be assigned as the cache grows
+    pages:               int32 device tensor of a paged cache (the sequence's block table)
+    length:              optional int32 device tensor of one element: CacheBack.attend reads the first
+                         min(T, length) rows, as it is when the kernel runs
+    `capacity` is the number of rows there is room for (pack writes below it).
+    """
+
+    GROUP = 32
+
+    def __init__(self, k, v, k_scale, v_scale, T: Optional[int] = None, pages=None, length=None):
+        paged = pages is not None
+        dims = 5 if paged else 4
+        _require(all(x.dim() == dims for x in (k, v, k_scale, v_scale)), "codes and scales need %d dimensions" % dims)
+        _require(k.element_size() == v.element_size() == 1 and k_scale.element_size() == v_scale.element_size() == 2,
+                 "codes are bytes and scales 16-bit numbers")
+        _require(k.shape == v.shape and k_scale.shape == v_scale.shape and k.shape[:-1] == k_scale.shape[:-1] and
+                 k.shape[-1] == 16 * k_scale.shape[-1], "codes hold d / 2 and scales d / 32 elements of the same rows")
+        kd, sd = k.shape[-1], k_scale.shape[-1]
+        for x, n in ((k, kd), (v, kd), (k_scale, sd), (v_scale, sd)):
+            _require(x.stride(-1) == 1, "rows are contiguous")
+            # (the stride of a dimension of one entry says nothing)
+            _require(all(a == 1 or (s % n == 0 and s // n == t // kd) for a, s, t in
+                         zip(x.shape[:-1], x.stride()[:-1], k.stride()[:-1])),
+                     "codes and scales of K and V need the same strides in rows")
+        self.k, self.v, self.k_scale, self.v_scale, self.pages, self.length = k, v, k_scale, v_scale, pages, length
+        self.head_dim = 2 * kd
+        self.device = k.device
+        if paged:
+            self.page_size, self.n_pages = k.shape[2], k.shape[1]
+            _require(self.page_size & (self.page_size - 1) == 0, "page_size must be a power of two")
+            _require(pages.element_size() == 4 and pages.dim() == 1 and pages.is_contiguous(), "pages are a row of int32")
+            self.n_layers, self.n_kv_heads = k.shape[0], k.shape[3]
+            self.capacity = pages.numel() * self.page_size
+            order = (0, 3, 2)
+        else:
+            self.n_layers, self.n_kv_heads, self.capacity = k.shape[:3]
+            order = (0, 1, 2)
+        _require(length is None or (length.element_size() == 4 and length.numel() == 1), "length is one int32")
+        row = [k.stride(i) // kd * self.head_dim if k.shape[i] > 1 else self.head_dim for i in order]
+        self._rows = row
+        self._page = (k.stride(1) // kd * self.head_dim if k.shape[1] > 1 else self.head_dim) if paged else 0
+        self.T = self.capacity if T is None else int(T)
+        _require(0 <= self.T <= self.capacity, "T = %d not in [0, %d]" % (self.T, self.capacity))
+
+    @classmethod
+    def empty(cls, n_layers: int, n_kv_heads: int, T: int, head_dim: int, device=None) -> "PackedKV":
+        """Room for T rows (whose contents are undefined until they are packed)."""
+        import torch
+        row = (n_layers, n_kv_heads, T)
+        return cls(*[torch.empty(row + (head_dim // 2,), dtype=torch.uint8, device=device) for _ in range(2)],
+                   *[torch.empty(row + (head_dim // 32,), dtype=torch.bfloat16, device=device) for _ in range(2)])
+
+    @property
+    def bytes(self) -> int:
+        """Bytes that T rows take (codes and scales of K and V, every layer and head)."""
+        return 2 * self.n_layers * self.n_kv_heads * self.T * (self.head_dim // 2 + self.head_dim // 16)
+
+    def desc(self, T: Optional[int] = None) -> cb_packed:
+        r = self._rows
+        p = cb_packed(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                      self.T if T is None else T, r[0], r[1], r[2])
+        if self.pages is not None:
+            p.pages, p.page_size, p.s_page, p.n_pages = self.pages.data_ptr(), self.page_size, self._page, self.n_pages
+        if self.length is not None:
+            p.length = self.length.data_ptr()
+        return p
+
+
+class Rotary:
+    """A rotary embedding (cb_rope): base, pairs as "halves" (k, k + dims / 2) or "pairs" (2k, 2k + 1),
+    `dims` rotary elements of a head (0: all), scaling "none", "linear" or "yarn" (by parts) by `factor`
+    over `original` positions; attention 0 takes the scaling's own factor of cosine and sine."""
+
+    STYLES = {"halves": 0, "pairs": 1, 0: 0, 1: 1}
+    SCALINGS = {"none": 0, "linear": 1, "yarn": 2}
+
+    def __init__(self, base: float, style="halves", dims: int = 0, scaling: str = "none", factor: float = 1.0,
+                 original: int = 0, beta_fast: float = 0.0, beta_slow: float = 0.0, attention: float = 0.0):
+        if style not in self.STYLES or scaling not in self.SCALINGS:
+            raise ValueError("style is one of halves, pairs; scaling one of none, linear, yarn")
+        self._c = [cb_rope(base, self.STYLES[style], dims, self.SCALINGS[scaling], factor, original, beta_fast, beta_slow,
+                           attention, inverse) for inverse in (0, 1)]
+
+    def desc(self, inverse: bool = False) -> cb_rope:
+        return self._c[1 if inverse else 0]
+
+
+def _require(ok: bool, message: str):
+    if not ok:
+        raise ValueError(message)
+
+
 class CacheBack:
     """One cb_ctx.  Methods enqueue work on a CUDA stream (default: torch's current stream)."""
+
+    _create = "cb_create"
 
     def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_query_tokens: int,
                  max_positions: int, max_senders: int = 1, p: float = 2.0, alpha: float = 2.0,
@@ -246,7 +390,7 @@ class CacheBack:
         cfg.score_kernel = score_kernel
         self.cfg = cfg
         h = ctypes.c_void_p()
-        st = self.lib.cb_create(ctypes.byref(cfg), ctypes.byref(h))
+        st = getattr(self.lib, self._create)(ctypes.byref(cfg), ctypes.byref(h))
         if st != CB_OK:
             raise CBError(st, self.lib.cb_last_error(None).decode())
         self.h = h
@@ -343,6 +487,101 @@ class CacheBack:
                                        out.shape[0], Oa, out.stride(0) * out.element_size(),
                                        _stream_handle(stream)))
 
+    # -- the receiver's side: rotary positions, rows in 4 bits, attention over them -----------------
+    def rotary(self, xs: Sequence, rope: Rotary, ys: Optional[Sequence] = None, pos=None, pos0: int = 0,
+               inverse: bool = False, stream=None):
+        """Turn bf16 vectors [nL][tokens][heads][d] (or [tokens][heads][d]) to their positions: ys[i] from
+        xs[i], in place where ys or ys[i] is None.  pos: int32 device tensor of every token's position,
+        or a list of one (or None) per set; else token r is at pos0 + r.  inverse: the transposed turn
+        (the gradient of the forward one).  Returns ys."""
+        n = len(xs)
+        ys = [x if y is None else y for x, y in zip(xs, ys or [None] * n)]
+        pos = list(pos) if isinstance(pos, (list, tuple)) else [pos] * n
+        sets = (cb_vectors * n)()
+        for i, (x, y, p) in enumerate(zip(xs, ys, pos)):
+            _require(x.shape == y.shape and x.dim() in (3, 4) and x.shape[-1] == self.cfg.head_dim, "vectors are [nL][tokens][heads][d]")
+            _require(x.element_size() == y.element_size() == 2, "vectors are bf16")
+            xt, yt = x.stride(), y.stride()
+            _require(xt[-1] == yt[-1] == 1, "vectors are contiguous")
+            nl, xl, yl = (x.shape[0], xt[0], yt[0]) if x.dim() == 4 else (1, 0, 0)
+            _require(p is None or (p.element_size() == 4 and p.is_contiguous() and p.numel() == x.shape[-3]), "pos holds one int32 a token")
+            sets[i] = cb_vectors(x.data_ptr(), y.data_ptr(), nl, x.shape[-2], x.shape[-3], xl, xt[-3], xt[-2], yl, yt[-3],
+                                 yt[-2], None if p is None else p.data_ptr(), int(pos0))
+        self._check(self.lib.cb_rotary(self.h, n, sets, ctypes.byref(rope.desc(inverse)), _stream_handle(stream)))
+        return ys
+
+    def pack(self, Ks: Sequence, Vs: Sequence, caches: Sequence, offsets: Optional[Sequence[int]] = None,
+             idx: Optional[Sequence] = None, counts: Optional[Sequence[int]] = None, rows: Optional[Sequence] = None,
+             layer: int = 0, stream=None):
+        """Rows of bf16 K and V [layers][Hkv][T][d] (or PagedKV) into 4-bit caches: row idx[i][j] (row j
+        without idx) of sender i becomes row rows[i][j] (offsets[i] + j without rows) of caches[i], in the
+        layers from `layer` on.  counts: rows of each sender (default: all of idx, or of K)."""
+        n = len(Ks)
+        idx, rows = idx or [None] * n, rows or [None] * n
+        counts = counts or [int(K.shape[2]) if x is None else int(x.numel()) for K, x in zip(Ks, idx)]
+        for K, x, r, c, p in zip(Ks, idx, rows, counts, caches):
+            _require(all(t is None or (t.element_size() == 4 and t.is_contiguous() and t.numel() >= c) for t in (x, r)), "idx and rows hold an int32 a row")
+            self._fits(p)
+            _require(K.shape[1] == p.n_kv_heads and K.shape[3] == p.head_dim and K.shape[0] == Ks[0].shape[0], "K and V do not match the cache")
+        kv = (cb_kv * n)(*[kv_desc(K, V) for K, V in zip(Ks, Vs)])
+        held = (cb_packed * n)(*[p.desc(min(p.capacity, self.cfg.max_positions)) for p in caches])
+        ip = _ptr_array([None if x is None else x.data_ptr() for x in idx])
+        rp = _ptr_array([None if r is None else r.data_ptr() for r in rows])
+        off = None if offsets is None else _ptr_array(list(map(int, offsets)), ctypes.c_int64)
+        self._check(self.lib.cb_pack(self.h, n, kv, ip, _ptr_array(list(map(int, counts)), ctypes.c_int64), held, off, rp,
+                                     int(layer), int(Ks[0].shape[0]), _stream_handle(stream)))
+
+    def unpack(self, caches: Sequence, k_out, v_out, offsets: Optional[Sequence[int]] = None, idx: Optional[Sequence] = None,
+               counts: Optional[Sequence[int]] = None, stream=None):
+        """Rows of 4-bit caches as bf16, all layers: row idx[i][j] (row j without idx) of caches[i] becomes row
+        offsets[i] + j of k_out, v_out [nL][Hkv][capacity][d]; by default every cached row, caches back to
+        back."""
+        n = len(caches)
+        idx = idx or [None] * n
+        counts = counts or [p.T if x is None else int(x.numel()) for p, x in zip(caches, idx)]
+        offsets = offsets or [sum(counts[:i]) for i in range(n)]
+        for p, x, c in zip(caches, idx, counts):
+            self._fits(p)
+            _require(x is None or (x.element_size() == 4 and x.is_contiguous() and x.numel() >= c), "idx holds an int32 a row")
+        ost = k_out.stride()
+        _require(ost[3] == 1 and ost[2] == k_out.size(3) == self.cfg.head_dim and v_out.stride() == ost and
+                 v_out.shape == k_out.shape and k_out.element_size() == 2 and
+                 tuple(k_out.shape[:2]) == (self.cfg.n_layers, self.cfg.n_kv_heads), "k_out, v_out are bf16 [nL][Hkv][capacity][d]")
+        held = (cb_packed * n)(*[p.desc() for p in caches])
+        self._check(self.lib.cb_unpack(self.h, n, held, _ptr_array([None if x is None else x.data_ptr() for x in idx]),
+                                       _ptr_array(list(map(int, counts)), ctypes.c_int64), k_out.data_ptr(), v_out.data_ptr(),
+                                       k_out.size(2), _ptr_array(list(map(int, offsets)), ctypes.c_int64), ost[0], ost[1],
+                                       _stream_handle(stream)))
+
+    def attend(self, caches: Sequence, Qs: Sequence, outs: Sequence, layer: int = 0, causal: bool = True, window: int = 0,
+               lses: Optional[Sequence] = None, stream=None):
+        """One layer's attention over 4-bit caches: outs[i] (bf16 [m][Hq][d]) of query tokens Qs[i] (bf16
+        [m][Hq][d]), the last m positions of caches[i] (causal: each sees the rows up to its own, the last
+        `window` of them where window > 0; otherwise all); lses[i] (fp32 [m][Hq], contiguous) receives the
+        log-sum-exp.  Qs, outs and lses may be tensors with the sequences in their first dimension."""
+        n = len(caches)
+        _require(len(Qs) == len(outs) == n and (lses is None or len(lses) == n), "one query and output per cache")
+        q = (cb_attend_query * n)()
+        for i in range(n):
+            self._fits(caches[i])
+            Q, out = Qs[i], outs[i]
+            qt, ot = Q.stride(), out.stride()
+            m, heads, d = Q.shape
+            _require(out.shape == Q.shape and heads == self.cfg.n_q_heads and d == self.cfg.head_dim and qt[2] == ot[2] == 1 and
+                     Q.element_size() == out.element_size() == 2, "queries and outputs are bf16 [m][Hq][d]")
+            lse = None
+            if lses is not None and lses[i] is not None:
+                _require(lses[i].shape == (m, heads) and lses[i].is_contiguous() and lses[i].element_size() == 4, "lse is fp32 [m][Hq]")
+                lse = lses[i].data_ptr()
+            q[i] = cb_attend_query(Q.data_ptr(), out.data_ptr(), lse, m, qt[0], qt[1], ot[0], ot[1])
+        held = (cb_packed * n)(*[p.desc() for p in caches])
+        self._check(self.lib.cb_attend(self.h, int(layer), n, held, q, 1 if causal else 0, int(window), _stream_handle(stream)))
+
+    def _fits(self, p: PackedKV):
+        c = self.cfg
+        _require(p.n_layers == c.n_layers and p.n_kv_heads == c.n_kv_heads and p.head_dim == c.head_dim,
+                 "the cache's layers, heads or head dimension are not the context's")
+
     def set_wait_limit(self, limit_ns: int = 0, stall_next_score: bool = False):
         """cb_set_wait_limit: limit of one bounded device wait (0: the 1 s default); with
         stall_next_score the next tcgen05 cb_score makes one wait run out (failure-detection test)."""
@@ -368,3 +607,15 @@ class CacheBack:
 
     def sync_status(self, stream=None):
         self._check(self.lib.cb_sync_status(self.h, _stream_handle(stream)))
+
+
+class Receiver(CacheBack):
+    """A context without the scratch of score and select (cb_create_receiver): rotary, pack, unpack,
+    attend, compact and gather, with max_positions and n_layers free."""
+
+    _create = "cb_create_receiver"
+
+    def __init__(self, n_layers: int, n_q_heads: int, n_kv_heads: int, head_dim: int, max_query_tokens: int,
+                 max_positions: int, max_senders: int = 1, softmax_scale: float = 0.0, lib_path: Optional[str] = None):
+        super().__init__(n_layers, n_q_heads, n_kv_heads, head_dim, max_query_tokens, max_positions, max_senders,
+                         softmax_scale=softmax_scale, lib_path=lib_path)

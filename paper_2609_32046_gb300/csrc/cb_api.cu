@@ -12,9 +12,9 @@
 #include <vector>
 
 #include <cuda_runtime.h>
-#include <nvtx3/nvToolsExt.h>
 
 #include "cacheback.h"
+#include "cb_ctx.cuh"
 #include "cb_internal.cuh"
 
 namespace cbk {
@@ -51,39 +51,11 @@ void stage_mark(StageTimer* t, int stage, cudaStream_t st) {
 }
 }  // namespace cbk
 
-constexpr int64_t kDefaultWaitNs = 1000000000;   // 1 s
-
-struct cb_ctx {
-    cb_config cfg;
-    int device = 0;
-    int num_sms = 0;
-    int G = 1;
-    bool use_tc = false;
-    bool tc_stage_must = false;     // paged senders must be staged (the shapes score_kernel = 2 takes)
-    float scale = 0.f;
-    float* scratch = nullptr;       // per sender: pass-1 partials, then pass-2 partials in their place
-    float* offs = nullptr;
-    uint16_t* ext = nullptr;        // tcgen05 passes: per-row offset terms [S][nS][R_pad][16] bf16
-    uint16_t* ones = nullptr;       // tcgen05 passes: [128][16] bf16 block of ones columns
-    float* span_keys = nullptr;
-    uint16_t* stage = nullptr;      // tcgen05 passes: contiguous copies of paged senders' K (on demand)
-    int64_t stage_elems = 0;
-    bool stage_captured = false;    // a captured cb_score uses `stage`: a graph holds its address
-    std::vector<uint16_t*> old_stages;   // outgrown buffers that graphs may still use, until cb_destroy
-    uint32_t* err = nullptr;
-    int64_t keys_per_sender = 0;
-    int64_t scratch_bytes = 0;
-    int32_t score_path = 0;         // kernels of the last cb_score: 2 tcgen05, 1 mma.sync, 0 none yet
-    int64_t wait_ns = kDefaultWaitNs;   // limit of one bounded device wait (tcgen05 passes)
-    int32_t stall_next = 0;         // failure-detection test: stall the next cb_score once
-    int32_t score_sms = 0;          // SMs of the persistent score kernels (0: all)
-    cbk::StageTimer* timer = nullptr;
-    std::string last_error;
-};
-
 namespace {
-
 thread_local std::string g_create_error;
+}  // namespace
+
+namespace cbk {
 
 cb_status fail(cb_ctx* ctx, cb_status st, const char* fmt, ...) {
     char buf[512];
@@ -98,23 +70,8 @@ cb_status fail(cb_ctx* ctx, cb_status st, const char* fmt, ...) {
     return st;
 }
 
-// Makes ctx's device current for the duration of a call, restoring the caller's device after.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
-
-
 // The pointer must be device (or managed) memory on ctx's device.
-cb_status check_device_ptr(cb_ctx* ctx, const void* p, const char* what, int i, int align = 16) {
+cb_status check_device_ptr(cb_ctx* ctx, const void* p, const char* what, int i, int align) {
     if (!p) return fail(ctx, CB_EINVAL, "%s[%d] is NULL", what, i);
     if (reinterpret_cast<uintptr_t>(p) % (uintptr_t)align != 0)
         return fail(ctx, CB_EINVAL, "%s[%d] is not %d-byte aligned", what, i, align);
@@ -161,7 +118,17 @@ cb_status check_source_ptr(cb_ctx* ctx, const void* p, const char* what, int i, 
     return st;
 }
 
-bool stride_ok(int64_t s) { return s > 0 && (s % 8) == 0; }
+}  // namespace cbk
+
+using cbk::check_device_ptr;
+using cbk::check_source_ptr;
+using cbk::DeviceGuard;
+using cbk::fail;
+using cbk::kDefaultWaitNs;
+using cbk::NvtxRange;
+using cbk::stride_ok;
+
+namespace {
 
 // Small senders of head dimension 64 keep to the mma.sync passes: up to about this much work (in
 // pieces of 128 positions x 16 tokens of one group, four an SM) those take less time than the
@@ -231,9 +198,40 @@ cudaError_t alloc(T** p, size_t count, int64_t* total) {
     return cudaMalloc(reinterpret_cast<void**>(p), count * sizeof(T));
 }
 
+cudaError_t alloc_attend(cb_ctx* ctx, int64_t* total) {
+    const int64_t rows = cbk::attend_part_rows(ctx->num_sms);
+    cudaError_t e = alloc(&ctx->attend_part, (size_t)(rows * ctx->cfg.head_dim), total);
+    if (e == cudaSuccess) e = alloc(&ctx->attend_ml, (size_t)rows, total);
+    return e;
+}
+
 }  // namespace
 
 namespace cbk {
+// A capture of the call's own stream takes no allocation; another stream's is left alone (the mode is
+// the thread's own, and put back).
+cb_status attend_scratch(cb_ctx* ctx, cudaStream_t st) {
+    if (ctx->attend_ml) return CB_OK;
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) cudaGetLastError();
+    if (cap != cudaStreamCaptureStatusNone)
+        return fail(ctx, CB_ENOMEM, "the first cb_attend of a context allocates: make it before the stream is captured");
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    int64_t total = 0;
+    const cudaError_t e = alloc_attend(ctx, &total);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        cudaFree(ctx->attend_part);
+        ctx->attend_part = nullptr;
+        ctx->attend_ml = nullptr;
+        return fail(ctx, CB_ENOMEM, "cannot allocate %lld bytes for partial results", (long long)total);
+    }
+    ctx->scratch_bytes += total;
+    return CB_OK;
+}
+
 // Error text of entry points that take no context (read back by cb_last_error(NULL)).
 void set_context_free_error(const char* msg) { g_create_error = msg; }
 }  // namespace cbk
@@ -277,7 +275,9 @@ int64_t cb_scratch_bytes(const cb_ctx* ctx) { return ctx ? ctx->scratch_bytes : 
 
 int32_t cb_score_path(const cb_ctx* ctx) { return ctx ? ctx->score_path : 0; }
 
-cb_status cb_create(const cb_config* cfg, cb_ctx** out) {
+}  // extern "C"
+
+static cb_status create(const cb_config* cfg, cb_ctx** out, bool receiver) {
     if (!out) return fail(nullptr, CB_EINVAL, "out is NULL");
     *out = nullptr;
     if (!cfg) return fail(nullptr, CB_EINVAL, "cfg is NULL");
@@ -324,7 +324,8 @@ cb_status cb_create(const cb_config* cfg, cb_ctx** out) {
     ctx->cfg = c;
     ctx->device = dev;
     ctx->G = G;
-    ctx->use_tc = c.score_kernel == 2 || (c.score_kernel == 0 && tc_ok);
+    ctx->receiver = receiver;
+    ctx->use_tc = !receiver && (c.score_kernel == 2 || (c.score_kernel == 0 && tc_ok));
     ctx->tc_stage_must = tc_asked_ok;
     ctx->scale = c.softmax_scale > 0.f ? c.softmax_scale : 1.f / std::sqrt((float)c.head_dim);
     cudaDeviceGetAttribute(&ctx->num_sms, cudaDevAttrMultiProcessorCount, dev);
@@ -334,9 +335,13 @@ cb_status cb_create(const cb_config* cfg, cb_ctx** out) {
     const int64_t rows = (int64_t)c.max_query_tokens * G;
     ctx->keys_per_sender = (c.max_positions + c.span_width - 1) / c.span_width;
     int64_t total = 0;
-    e = alloc(&ctx->scratch, (size_t)(S * cbk::score_scratch_floats(nS, rows, c.max_positions)), &total);
-    if (e == cudaSuccess) e = alloc(&ctx->offs, (size_t)(S * nS * rows), &total);
-    if (e == cudaSuccess) e = alloc(&ctx->span_keys, (size_t)(S * ctx->keys_per_sender), &total);
+    if (!receiver) {
+        e = alloc(&ctx->scratch, (size_t)(S * cbk::score_scratch_floats(nS, rows, c.max_positions)), &total);
+        if (e == cudaSuccess) e = alloc(&ctx->offs, (size_t)(S * nS * rows), &total);
+        if (e == cudaSuccess) e = alloc(&ctx->span_keys, (size_t)(S * ctx->keys_per_sender), &total);
+    } else {
+        e = alloc_attend(ctx, &total);
+    }
     if (e == cudaSuccess && ctx->use_tc) {
         e = alloc(&ctx->ext, (size_t)(S * nS * cbk::rows_pad128(rows) * cbk::kExtCols), &total);
         if (e == cudaSuccess) e = alloc(&ctx->ones, (size_t)(128 * cbk::kExtCols), &total);
@@ -360,6 +365,12 @@ cb_status cb_create(const cb_config* cfg, cb_ctx** out) {
     return CB_OK;
 }
 
+extern "C" {
+
+cb_status cb_create(const cb_config* cfg, cb_ctx** out) { return create(cfg, out, false); }
+
+cb_status cb_create_receiver(const cb_config* cfg, cb_ctx** out) { return create(cfg, out, true); }
+
 void cb_destroy(cb_ctx* ctx) {
     if (!ctx) return;
     {
@@ -372,25 +383,20 @@ void cb_destroy(cb_ctx* ctx) {
         cudaFree(ctx->span_keys);
         cudaFree(ctx->stage);
         for (uint16_t* p : ctx->old_stages) cudaFree(p);
+        cudaFree(ctx->attend_part);
+        cudaFree(ctx->attend_ml);
         cudaFree(ctx->err);
         delete ctx->timer;
     }
     delete ctx;
 }
 
-namespace {
-// An NVTX range over one call of the C-ABI (header-only NVTX: free unless a profiler listens).
-struct NvtxRange {
-    explicit NvtxRange(const char* name) { nvtxRangePushA(name); }
-    ~NvtxRange() { nvtxRangePop(); }
-};
-}  // namespace
-
 cb_status cb_score(cb_ctx* ctx, int32_t n, const cb_kv* senders, const cb_query* queries, float* const* scores,
                    void* stream) {
     NvtxRange nr("cb_score");
     if (!ctx) return fail(nullptr, CB_EINVAL, "ctx is NULL");
     ctx->last_error.clear();
+    if (ctx->receiver) return fail(ctx, CB_EINVAL, "the context was made by cb_create_receiver");
     const cb_config& c = ctx->cfg;
     if (n < 1 || n > c.max_senders) return fail(ctx, CB_ESHAPE, "n = %d not in [1, %d]", n, c.max_senders);
     if (!senders || !queries || !scores) return fail(ctx, CB_EINVAL, "senders, queries or scores is NULL");
@@ -543,6 +549,7 @@ cb_status cb_select(cb_ctx* ctx, int32_t n, const float* const* scores, const in
     NvtxRange nr("cb_select");
     if (!ctx) return fail(nullptr, CB_EINVAL, "ctx is NULL");
     ctx->last_error.clear();
+    if (ctx->receiver) return fail(ctx, CB_EINVAL, "the context was made by cb_create_receiver");
     const cb_config& c = ctx->cfg;
     if (n < 1 || n > c.max_senders) return fail(ctx, CB_ESHAPE, "n = %d not in [1, %d]", n, c.max_senders);
     if (!scores || !T || !budget || !idx) return fail(ctx, CB_EINVAL, "scores, T, budget or idx is NULL");
@@ -804,11 +811,14 @@ cb_status cb_sync_status(cb_ctx* ctx, void* stream) {
             return fail(ctx, CB_ETIMEOUT,
                         "a bounded device wait gave up (code 0x%x: bits 8+ name the wait); the results are invalid",
                         word);
-        return fail(ctx, CB_EDEVICE, "kernel bounds check failed (code 0x%x:%s%s%s%s)", word,
+        return fail(ctx, CB_EDEVICE, "kernel bounds check failed (code 0x%x:%s%s%s%s%s%s%s)", word,
                     (word & cbk::kErrCompactIndex) ? " compact index outside [0, T)" : "",
                     (word & cbk::kErrSelectBudget) ? " select count mismatch" : "",
                     (word & cbk::kErrGatherIndex) ? " gather index outside [0, T)" : "",
-                    (word & cbk::kErrPageIndex) ? " block-table entry outside [0, n_pages)" : "");
+                    (word & cbk::kErrPageIndex) ? " block-table entry outside [0, n_pages)" : "",
+                    (word & cbk::kErrPackValue) ? " packed value not finite or above 7 * 2^13" : "",
+                    (word & cbk::kErrPackScale) ? " scale of a packed row outside [0, 2^13]" : "",
+                    (word & cbk::kErrPackRow) ? " packed row's destination outside [0, T)" : "");
     }
     return CB_OK;
 }
