@@ -20,6 +20,9 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kStep = 32;                // positions a warp takes at a time
+// Weights are exp2(z - top + 14): up to 2^14, so that fp16 holds those down to 2^-28 of the largest as
+// normal numbers and to 2^-38 at all, and 32-bit sums stay in range.
+constexpr float kWeightBits = 14.f;
 
 // D (16 x 8) += A (16 x 16) B (16 x 8), fp32 sums.
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -269,7 +272,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_attend_few(const __grid_constan
 #pragma unroll
             for (int k = 4; k <= 16; k *= 2) l += __shfl_xor_sync(0xFFFFFFFFu, l, k);
             if (gid == 0) {
-                sh_m[warp][nt * 8 + 2 * tig + h] = top[nt][h];
+                sh_m[warp][nt * 8 + 2 * tig + h] = top[nt][h] - kWeightBits;
                 sh_l[warp][nt * 8 + 2 * tig + h] = l;
             }
         }
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(kWarps * 32) k_attend_few(const __grid_constan
             float M = sh_m[0][r];
 #pragma unroll
             for (int w = 1; w < kWarps; ++w) M = fmaxf(M, sh_m[w][r]);
-            const float f = top[nt][h] == -INFINITY ? 0.f : exp2f(top[nt][h] - M);
+            const float f = top[nt][h] == -INFINITY ? 0.f : exp2f(top[nt][h] - kWeightBits - M);
             // elements (D / 8) gid + 2 i (register h) and + 2 i + 1 (register 2 + h)
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
@@ -391,6 +394,7 @@ cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num
     for (int i = 0; i < b.n; ++i) rows = b.s[i].m > rows ? b.s[i].m : rows;
     rows *= b.G;
     if (rows == 0) return cudaSuccess;
+    if (rows > 16) return launch_attend_tc(b, head_dim, st, num_sms);
     const int tile_rows = rows <= 8 ? 8 : 16;
     for (int64_t blocks = (int64_t)num_sms * 4; !attend_plan(b, tile_rows, blocks, kWarps * kStep, num_sms); blocks /= 2) {}
     int splits = 1, tiles = 1;

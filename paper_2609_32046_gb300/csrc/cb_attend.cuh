@@ -14,10 +14,6 @@ namespace cbk {
 
 using sm100::ex2;
 
-// Weights are exp2(z - M + 14): up to 2^14, so that fp16 holds those down to 2^-28 of a row's largest as
-// normal numbers and to 2^-38 at all, where 32-bit sums of up to 2^24 of them stay in range.
-constexpr float kWeightBits = 14.f;
-
 constexpr uint32_t kTopScaleBits = 0x4600u;   // 2^13 as bf16, the largest scale
 
 // Query rows of partial results a context holds for each SM: 16 parts of 16 rows, or two of 128.
@@ -101,8 +97,7 @@ __device__ __forceinline__ void values_f16(uint32_t word, uint32_t s2, uint32_t 
     }
 }
 
-// Four elements of an output row, from sums relative to M with weights of kWeightBits, and the row's
-// log-sum-exp.
+// Four elements of an output row and the row's log-sum-exp, from sums of weights exp2(z - M).
 template <int D>
 __device__ __forceinline__ void attend_write(const AttendBatch& b, const AttendSeq& s, int g, int row, int d, float4 y,
                                              float M, float l) {
@@ -112,7 +107,12 @@ __device__ __forceinline__ void attend_write(const AttendBatch& b, const AttendS
     *reinterpret_cast<uint2*>(s.out + (int64_t)r * s.o_tok + (int64_t)h * s.o_head + d) =
         make_uint2(reinterpret_cast<const uint32_t&>(lo), reinterpret_cast<const uint32_t&>(hi));
     if (d == 0 && s.lse)
-        s.lse[(int64_t)r * b.n_q_heads + h] = l == 0.f ? -INFINITY : (M - kWeightBits + log2f(l)) * 0.6931471805599453f;
+        s.lse[(int64_t)r * b.n_q_heads + h] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
 }
+
+// Host side, shared by the launchers.
+bool attend_plan(AttendBatch& b, int tile_rows, int64_t blocks, int64_t least, int num_sms);
+cudaError_t attend_join(const AttendBatch& b, int head_dim, int tile_rows, cudaStream_t st);
+cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms);
 
 }  // namespace cbk

@@ -3,8 +3,8 @@
 Tolerance of an output element, A = sum_t a_t |v_t|:
   2^-8 |out|        its rounding to bf16 (half a step)
   2^-11 A           weights rounded to fp16 (half a step), the values exact
-  2^-37 T max|v|    weights below fp16's smallest step (2^-24 of 2^14, half of it: 2^-39 of the row's largest;
-                    a row's largest weight is at most the sum, so 2^-37 covers the sums' halves)
+  2^-32 T max|v|    weights below fp16's smallest step: they are held times 2^7 or more over the row's largest,
+                    which the sum is no smaller than, and are off by half of 2^-24
   2 E A             every weight is off by the factor exp(e), |e| <= E, in the sum above and in the sum below:
                     E = 2 (d + 8) 2^-23 max sum |q k| scale (products summed in fp32 that may be cut off
                     instead of rounded, and the scaling) + 2^-20 (exp2's approximation) + T 2^-23 (sums of T terms)
@@ -87,7 +87,7 @@ class Case:
             o, lse, A, size = ref.attention(q.double(), k, v, scale, causal, window)
             E = 2 * (self.d + 8) * 2.0 ** -23 * size + 2.0 ** -20 + L * 2.0 ** -23
             big = float(v.abs().max()) if L else 0.0
-            tol = o.abs() * 2.0 ** -8 + A * (2.0 ** -11 + 2 * E) + 2.0 ** -37 * L * big
+            tol = o.abs() * 2.0 ** -8 + A * (2.0 ** -11 + 2 * E) + 2.0 ** -32 * L * big
             err = (self.out[i].double() - o).abs()
             assert (err <= tol).all(), "sequence %d: off by %.3g more than %.3g" % (i, float((err - tol).max()), float(tol.mean()))
             empty = torch.isinf(lse)
