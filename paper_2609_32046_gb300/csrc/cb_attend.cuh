@@ -76,23 +76,35 @@ __device__ __forceinline__ uint32_t f16_scales(uint32_t lo, uint32_t hi) {
     return reinterpret_cast<const uint32_t&>(h);
 }
 
-// Pairs of nibbles (j, j + 4), j = 0..3, of a word as numbers c * s: 128 + u (bf16) or 1024 + u (fp16)
-// by setting bits, less the bias is c, exactly; so is the product.
+// Pairs of nibbles (j, j + 4), j = 0..3, of a word as numbers c * s, exactly, by one fma each: setting bits
+// makes u = c + 8 the number 128 + 4 u (bf16, the nibble at bit 2) or 1024 + 16 u (fp16, at bit 4), and
+//   (128 + 4 u) (s / 4) - 40 s = (1024 + 16 u) (s / 16) - 72 s = c s.
+// 40 s and 72 s have 8 and 9 significant bits: bf16 and fp16 numbers.  With the nibble at bit 0 they would
+// have 10 (136 s) and 13 (1032 s), and the bias a subtraction of its own.
+__device__ __forceinline__ uint32_t nibbles_at(uint32_t word, int shift, uint32_t mask, uint32_t bits) {
+    return ((shift >= 0 ? word << (shift >= 0 ? shift : 0) : word >> (shift < 0 ? -shift : 0)) & mask) | bits;
+}
 __device__ __forceinline__ void values_bf16(uint32_t word, uint32_t s2, uint32_t (&out)[4]) {
+    const __nv_bfloat162 s = reinterpret_cast<const __nv_bfloat162&>(s2);
+    const __nv_bfloat162 a = __hmul2(s, __floats2bfloat162_rn(0.25f, 0.25f)), b = __hmul2(s, __floats2bfloat162_rn(-40.f, -40.f));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t x = ((word >> (4 * j)) & 0x000F000Fu) | 0x43004300u;
-        const __nv_bfloat162 c = __hsub2(reinterpret_cast<const __nv_bfloat162&>(x), __floats2bfloat162_rn(136.f, 136.f));
-        const __nv_bfloat162 p = __hmul2(c, reinterpret_cast<const __nv_bfloat162&>(s2));
+        const uint32_t x = nibbles_at(word, 2 - 4 * j, 0x003C003Cu, 0x43004300u);
+        const __nv_bfloat162 p = __hfma2(reinterpret_cast<const __nv_bfloat162&>(x), a, b);
         out[j] = reinterpret_cast<const uint32_t&>(p);
     }
 }
+// NEAR: every s is 0 or within 2^-16 .. 2^9, where s / 16 and 72 s are fp16 numbers.  Otherwise c by one fma
+// and its product with s by another instruction.
+template <bool NEAR>
 __device__ __forceinline__ void values_f16(uint32_t word, uint32_t s2, uint32_t (&out)[4]) {
+    const __half2 s = reinterpret_cast<const __half2&>(s2);
+    const __half2 u = __floats2half2_rn(0.0625f, 0.0625f), w = __floats2half2_rn(-72.f, -72.f);
+    const __half2 a = NEAR ? __hmul2(s, u) : u, b = NEAR ? __hmul2(s, w) : w;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t x = ((word >> (4 * j)) & 0x000F000Fu) | 0x64006400u;
-        const __half2 c = __hsub2(reinterpret_cast<const __half2&>(x), __floats2half2_rn(1032.f, 1032.f));
-        const __half2 p = __hmul2(c, reinterpret_cast<const __half2&>(s2));
+        const uint32_t x = nibbles_at(word, 4 - 4 * j, 0x00F000F0u, 0x64006400u);
+        const __half2 c = __hfma2(reinterpret_cast<const __half2&>(x), a, b), p = NEAR ? c : __hmul2(c, s);
         out[j] = reinterpret_cast<const uint32_t&>(p);
     }
 }

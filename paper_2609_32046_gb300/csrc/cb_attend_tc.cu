@@ -302,8 +302,8 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     uint32_t u[4], v[4];
-                    values_f16(__byte_perm(x.w[2 * i][k], x.w[2 * i + 1][k], 0x5410), s2[i], u);
-                    values_f16(__byte_perm(x.w[2 * i][k], x.w[2 * i + 1][k], 0x7632), s2[i], v);
+                    values_f16<false>(__byte_perm(x.w[2 * i][k], x.w[2 * i + 1][k], 0x5410), s2[i], u);
+                    values_f16<false>(__byte_perm(x.w[2 * i][k], x.w[2 * i + 1][k], 0x7632), s2[i], v);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         even[e][i] = u[e];
