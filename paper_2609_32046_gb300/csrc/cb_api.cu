@@ -202,6 +202,14 @@ cudaError_t alloc_attend(cb_ctx* ctx, int64_t* total) {
     const int64_t rows = cbk::attend_part_rows(ctx->num_sms);
     cudaError_t e = alloc(&ctx->attend_part, (size_t)(rows * ctx->cfg.head_dim), total);
     if (e == cudaSuccess) e = alloc(&ctx->attend_ml, (size_t)rows, total);
+    const size_t n = (size_t)ctx->num_sms * cbk::kFewBlocksPerSm;
+    if (e == cudaSuccess) e = alloc(&ctx->attend_tickets, n, total);
+    // (on a stream of its own: the legacy stream would wait for, and spoil, another stream's capture)
+    cudaStream_t st = nullptr;
+    if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&st, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaMemsetAsync(ctx->attend_tickets, 0, n * sizeof(int32_t), st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (st) cudaStreamDestroy(st);
     return e;
 }
 
@@ -211,7 +219,7 @@ namespace cbk {
 // A capture of the call's own stream takes no allocation; another stream's is left alone (the mode is
 // the thread's own, and put back).
 cb_status attend_scratch(cb_ctx* ctx, cudaStream_t st) {
-    if (ctx->attend_ml) return CB_OK;
+    if (ctx->attend_tickets) return CB_OK;
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     if (cudaStreamIsCapturing(st, &cap) != cudaSuccess) cudaGetLastError();
     if (cap != cudaStreamCaptureStatusNone)
@@ -224,8 +232,11 @@ cb_status attend_scratch(cb_ctx* ctx, cudaStream_t st) {
     if (e != cudaSuccess) {
         cudaGetLastError();
         cudaFree(ctx->attend_part);
+        cudaFree(ctx->attend_ml);
+        cudaFree(ctx->attend_tickets);
         ctx->attend_part = nullptr;
         ctx->attend_ml = nullptr;
+        ctx->attend_tickets = nullptr;
         return fail(ctx, CB_ENOMEM, "cannot allocate %lld bytes for partial results", (long long)total);
     }
     ctx->scratch_bytes += total;
@@ -385,6 +396,7 @@ void cb_destroy(cb_ctx* ctx) {
         for (uint16_t* p : ctx->old_stages) cudaFree(p);
         cudaFree(ctx->attend_part);
         cudaFree(ctx->attend_ml);
+        cudaFree(ctx->attend_tickets);
         cudaFree(ctx->err);
         delete ctx->timer;
     }

@@ -52,6 +52,7 @@ struct cb_ctx {
     bool receiver = false;          // no scratch for cb_score and cb_select
     float* attend_part = nullptr;   // cb_attend: partial results (outputs; maxima and sums)
     float2* attend_ml = nullptr;
+    int32_t* attend_tickets = nullptr;   // zero between calls
     cbk::RopeTable rope;
     cbk::StageTimer* timer = nullptr;
     std::string last_error;

@@ -279,9 +279,7 @@ struct AttendSeq {
     float* lse;
     int64_t s_tok, s_head, o_tok, o_head;
     int32_t m;
-    int32_t tiles;            // row tiles a KV head
-    int32_t splits;           // parts of the positions, each of which leaves a partial result (1: none)
-    int32_t slot0;            // first partial slot
+    int32_t pair0;            // row tiles of the sequences before
 };
 
 struct AttendBatch {
@@ -291,8 +289,10 @@ struct AttendBatch {
     int32_t causal;
     int64_t window;           // 0: none
     uint32_t* err;
-    float* part;              // partial outputs [slot][rows of a tile][d], then (max, sum) [slot][rows]
-    float2* part_ml;
+    float* part;              // partial outputs [slot][rows of a tile][d]
+    float2* part_ml;          // their (maximum, sum) [slot][rows of a tile]
+    int32_t* tickets;         // one a block of k_attend_few, zero between calls
+    int32_t pairs;            // row tiles of all sequences
     uint64_t wait_ns;
     AttendSeq s[kMaxBatch];
 };
@@ -300,10 +300,11 @@ struct AttendBatch {
 cudaError_t launch_rotary(const RotaryBatch& b, int head_dim, int style, cudaStream_t st, int num_sms);
 cudaError_t launch_pack(const PackBatch& b, int head_dim, cudaStream_t st, int num_sms);
 cudaError_t launch_unpack(const PackBatch& b, int head_dim, cudaStream_t st, int num_sms);
-// Fills in tiles, splits and slot0 of every sequence and launches.
+// Fills in pair0 and pairs and launches.
 cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms);
 // Query rows of partial results that launch_attend may use on num_sms SMs.
 int64_t attend_part_rows(int num_sms);
+constexpr int kFewBlocksPerSm = 4;   // blocks of k_attend_few an SM holds, and tickets a context has for each
 
 // Records the message cb_last_error(NULL) returns (entry points without a context).
 void set_context_free_error(const char* msg);

@@ -68,9 +68,9 @@ cb_status check_page_fields(cb_ctx* ctx, const int32_t* pages, int32_t page_size
 
 cb_status check_packed(cb_ctx* ctx, const cb_packed& p, int i) {
     const int d = ctx->cfg.head_dim;
-    if (p.T < 0 || p.T > ctx->cfg.max_positions)
-        return fail(ctx, CB_ESHAPE, "caches[%d].T = %lld not in [0, %lld]", i, (long long)p.T,
-                    (long long)ctx->cfg.max_positions);
+    const int64_t most = ctx->cfg.max_positions < kMaxRows - 4096 ? ctx->cfg.max_positions : kMaxRows - 4096;
+    if (p.T < 0 || p.T > most)
+        return fail(ctx, CB_ESHAPE, "caches[%d].T = %lld not in [0, %lld]", i, (long long)p.T, (long long)most);
     cb_status st;
     if (p.length && (st = check_device_ptr(ctx, p.length, "caches.length", i, 4))) return st;
     if (p.T == 0) return CB_OK;
@@ -366,6 +366,9 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         if ((st = check_device_ptr(ctx, q.q, "queries.q", i)) || (st = check_device_ptr(ctx, q.out, "queries.out", i)))
             return st;
         if (q.lse && (st = check_device_ptr(ctx, q.lse, "queries.lse", i, 4))) return st;
+        // (units of work are counted in 32 bits)
+        if ((caches[i].T / 128 + 2) * c.n_kv_heads * ((int64_t)q.m * ctx->G / 128 + 1) > ((int64_t)1 << 31) / kMaxBatch)
+            return fail(ctx, CB_ESHAPE, "sequence %d: too many positions, heads and query tokens for one launch", i);
         some.push_back(i);
     }
     if (some.empty()) return CB_OK;
@@ -383,6 +386,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         b.err = ctx->err;
         b.part = ctx->attend_part;
         b.part_ml = ctx->attend_ml;
+        b.tickets = ctx->attend_tickets;
         b.wait_ns = (uint64_t)ctx->wait_ns;
         for (int k = 0; k < b.n; ++k) {
             const cb_packed& p = caches[some[b0 + k]];
