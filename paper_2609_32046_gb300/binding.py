@@ -203,6 +203,7 @@ def _ptr_array(values, ctype=ctypes.c_void_p):
 
 
 _torch_cuda = None
+_raw_stream = None
 
 
 def _stream_handle(stream) -> int:
@@ -215,6 +216,19 @@ def _stream_handle(stream) -> int:
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
+
+
+def _stream_on(stream, tensor) -> int:
+    """The stream's handle; None: torch's current stream of the tensor's device."""
+    if stream is not None:
+        return stream if isinstance(stream, int) else stream.cuda_stream
+    if not tensor.is_cuda:
+        return _stream_handle(None)       # (the call refuses the tensor)
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        _raw_stream = torch._C._cuda_getCurrentRawStream
+    return _raw_stream(tensor.device.index)
 
 
 class PagedKV:
@@ -279,7 +293,7 @@ class PackedKV:
     k, v:                uint8 codes, [nL][Hkv][T][d / 2]; paged: [nL][n_pages][page_size][Hkv][d / 2]
     k_scale, v_scale:    bf16 scales, the same index order with d / 32 in the last place; any strides
                          that step over rows alike in codes and scales
-    T:                   rows cached (default: all there is room for); may be assigned as the cache grows
+    T:                   rows cached (default: all there is room for); may be assigned as the cache grows, as `length` may
     pages:               int32 device tensor of a paged cache (the sequence's block table)
     length:              optional int32 device tensor of one element: CacheBack.attend reads the first
                          min(T, length) rows, as it is when the kernel runs
@@ -303,7 +317,7 @@ class PackedKV:
             _require(all(a == 1 or (s % n == 0 and s // n == t // kd) for a, s, t in
                          zip(x.shape[:-1], x.stride()[:-1], k.stride()[:-1])),
                      "codes and scales of K and V need the same strides in rows")
-        self.k, self.v, self.k_scale, self.v_scale, self.pages, self.length = k, v, k_scale, v_scale, pages, length
+        self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
         self.head_dim = 2 * kd
         self.device = k.device
         if paged:
@@ -316,10 +330,15 @@ class PackedKV:
         else:
             self.n_layers, self.n_kv_heads, self.capacity = k.shape[:3]
             order = (0, 1, 2)
-        _require(length is None or (length.element_size() == 4 and length.numel() == 1), "length is one int32")
         row = [k.stride(i) // kd * self.head_dim if k.shape[i] > 1 else self.head_dim for i in order]
-        self._rows = row
         self._page = (k.stride(1) // kd * self.head_dim if k.shape[1] > 1 else self.head_dim) if paged else 0
+        # the description with its T left open (bytes of a cb_packed are copied faster than fields are set)
+        d = cb_packed(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), 0, row[0], row[1], row[2])
+        if paged:
+            d.pages, d.page_size, d.s_page, d.n_pages = pages.data_ptr(), self.page_size, self._page, self.n_pages
+        self._desc = d
+        self.length = length
+        self._shape = (self.n_layers, self.n_kv_heads, self.head_dim)
         self.T = self.capacity if T is None else int(T)
         _require(0 <= self.T <= self.capacity, "T = %d not in [0, %d]" % (self.T, self.capacity))
 
@@ -336,15 +355,19 @@ class PackedKV:
         """Bytes that T rows take (codes and scales of K and V, every layer and head)."""
         return 2 * self.n_layers * self.n_kv_heads * self.T * (self.head_dim // 2 + self.head_dim // 16)
 
+    @property
+    def length(self):
+        return self._length
+
+    @length.setter
+    def length(self, x):
+        _require(x is None or (x.element_size() == 4 and x.numel() == 1), "length is one int32")
+        self._length = x
+        self._desc.length = None if x is None else x.data_ptr()
+
     def desc(self, T: Optional[int] = None) -> cb_packed:
-        r = self._rows
-        p = cb_packed(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
-                      self.T if T is None else T, r[0], r[1], r[2])
-        if self.pages is not None:
-            p.pages, p.page_size, p.s_page, p.n_pages = self.pages.data_ptr(), self.page_size, self._page, self.n_pages
-        if self.length is not None:
-            p.length = self.length.data_ptr()
-        return p
+        self._desc.T = self.T if T is None else T
+        return self._desc
 
 
 class Rotary:
@@ -389,6 +412,7 @@ class CacheBack:
         cfg.pool_width, cfg.span_width, cfg.n_sink, cfg.n_latent = pool_width, span_width, n_sink, n_latent
         cfg.score_kernel = score_kernel
         self.cfg = cfg
+        self._shape = (n_layers, n_kv_heads, head_dim)
         h = ctypes.c_void_p()
         st = getattr(self.lib, self._create)(ctypes.byref(cfg), ctypes.byref(h))
         if st != CB_OK:
@@ -507,7 +531,8 @@ class CacheBack:
             _require(p is None or (p.element_size() == 4 and p.is_contiguous() and p.numel() == x.shape[-3]), "pos holds one int32 a token")
             sets[i] = cb_vectors(x.data_ptr(), y.data_ptr(), nl, x.shape[-2], x.shape[-3], xl, xt[-3], xt[-2], yl, yt[-3],
                                  yt[-2], None if p is None else p.data_ptr(), int(pos0))
-        self._check(self.lib.cb_rotary(self.h, n, sets, ctypes.byref(rope.desc(inverse)), _stream_handle(stream)))
+        self._check(self.lib.cb_rotary(self.h, n, sets, ctypes.byref(rope.desc(inverse)),
+                                      _stream_on(stream, xs[0]) if n else 0))
         return ys
 
     def pack(self, Ks: Sequence, Vs: Sequence, caches: Sequence, offsets: Optional[Sequence[int]] = None,
@@ -529,7 +554,7 @@ class CacheBack:
         rp = _ptr_array([None if r is None else r.data_ptr() for r in rows])
         off = None if offsets is None else _ptr_array(list(map(int, offsets)), ctypes.c_int64)
         self._check(self.lib.cb_pack(self.h, n, kv, ip, _ptr_array(list(map(int, counts)), ctypes.c_int64), held, off, rp,
-                                     int(layer), int(Ks[0].shape[0]), _stream_handle(stream)))
+                                     int(layer), int(Ks[0].shape[0]), _stream_on(stream, caches[0].k)))
 
     def unpack(self, caches: Sequence, k_out, v_out, offsets: Optional[Sequence[int]] = None, idx: Optional[Sequence] = None,
                counts: Optional[Sequence[int]] = None, stream=None):
@@ -551,7 +576,7 @@ class CacheBack:
         self._check(self.lib.cb_unpack(self.h, n, held, _ptr_array([None if x is None else x.data_ptr() for x in idx]),
                                        _ptr_array(list(map(int, counts)), ctypes.c_int64), k_out.data_ptr(), v_out.data_ptr(),
                                        k_out.size(2), _ptr_array(list(map(int, offsets)), ctypes.c_int64), ost[0], ost[1],
-                                       _stream_handle(stream)))
+                                       _stream_on(stream, k_out)))
 
     def attend(self, caches: Sequence, Qs: Sequence, outs: Sequence, layer: int = 0, causal: bool = True, window: int = 0,
                lses: Optional[Sequence] = None, stream=None):
@@ -561,26 +586,39 @@ class CacheBack:
         log-sum-exp.  Qs, outs and lses may be tensors with the sequences in their first dimension."""
         n = len(caches)
         _require(len(Qs) == len(outs) == n and (lses is None or len(lses) == n), "one query and output per cache")
-        q = (cb_attend_query * n)()
-        for i in range(n):
-            self._fits(caches[i])
-            Q, out = Qs[i], outs[i]
-            qt, ot = Q.stride(), out.stride()
-            m, heads, d = Q.shape
-            _require(out.shape == Q.shape and heads == self.cfg.n_q_heads and d == self.cfg.head_dim and qt[2] == ot[2] == 1 and
-                     Q.element_size() == out.element_size() == 2, "queries and outputs are bf16 [m][Hq][d]")
-            lse = None
-            if lses is not None and lses[i] is not None:
-                _require(lses[i].shape == (m, heads) and lses[i].is_contiguous() and lses[i].element_size() == 4, "lse is fp32 [m][Hq]")
-                lse = lses[i].data_ptr()
-            q[i] = cb_attend_query(Q.data_ptr(), out.data_ptr(), lse, m, qt[0], qt[1], ot[0], ot[1])
-        held = (cb_packed * n)(*[p.desc() for p in caches])
-        self._check(self.lib.cb_attend(self.h, int(layer), n, held, q, 1 if causal else 0, int(window), _stream_handle(stream)))
+        c, shape = self.cfg, self._shape
+        q, held = (cb_attend_query * n)(), (cb_packed * n)()
+        whole = all(hasattr(x, "data_ptr") for x in (Qs, outs)) and (lses is None or hasattr(lses, "data_ptr"))
+        if whole and n:          # one tensor each: the sequences' addresses by arithmetic
+            self._queries(Qs[0], outs[0], None if lses is None else lses[0])
+            m = Qs.shape[1]
+            a, (sa, ta, ha) = Qs.data_ptr(), Qs.stride()[:3]
+            o, (so, to, ho) = outs.data_ptr(), outs.stride()[:3]
+            e, se = (None, 0) if lses is None else (lses.data_ptr(), 4 * lses.stride(0))
+        for i, p in enumerate(caches):
+            if p._shape != shape:
+                self._fits(p)
+            p._desc.T = p.T
+            held[i] = p._desc
+            if whole:
+                q[i] = (a + 2 * i * sa, o + 2 * i * so, None if e is None else e + i * se, m, ta, ha, to, ho)
+            else:
+                q[i] = self._queries(Qs[i], outs[i], None if lses is None else lses[i])
+        self._check(self.lib.cb_attend(self.h, int(layer), n, held, q, 1 if causal else 0, int(window),
+                                       _stream_on(stream, caches[0].k) if n else 0))
+
+    def _queries(self, Q, out, lse):
+        """One sequence's fields of a cb_attend_query, looked over."""
+        qt, ot = Q.stride(), out.stride()
+        m, heads, d = Q.shape
+        _require(out.shape == Q.shape and heads == self.cfg.n_q_heads and d == self.cfg.head_dim and qt[2] == ot[2] == 1 and
+                 Q.element_size() == out.element_size() == 2, "queries and outputs are bf16 [m][Hq][d]")
+        _require(lse is None or (lse.shape == (m, heads) and lse.is_contiguous() and lse.element_size() == 4),
+                 "lse is fp32 [m][Hq]")
+        return (Q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), m, qt[0], qt[1], ot[0], ot[1])
 
     def _fits(self, p: PackedKV):
-        c = self.cfg
-        _require(p.n_layers == c.n_layers and p.n_kv_heads == c.n_kv_heads and p.head_dim == c.head_dim,
-                 "the cache's layers, heads or head dimension are not the context's")
+        _require(p._shape == self._shape, "the cache's layers, heads or head dimension are not the context's")
 
     def set_wait_limit(self, limit_ns: int = 0, stall_next_score: bool = False):
         """cb_set_wait_limit: limit of one bounded device wait (0: the 1 s default); with

@@ -11,6 +11,7 @@
 #include <string>
 #include <vector>
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "cacheback.h"
@@ -87,6 +88,38 @@ cb_status check_device_ptr(cb_ctx* ctx, const void* p, const char* what, int i, 
     if (a.device != ctx->device)
         return fail(ctx, CB_EINVAL, "%s[%d] lives on device %d, context on device %d", what, i, a.device,
                     ctx->device);
+    return CB_OK;
+}
+
+// cuMemGetAddressRange, by the runtime (the library links no driver); null where there is none.
+using AddressRange = CUresult (*)(CUdeviceptr*, size_t*, CUdeviceptr);
+static AddressRange address_range() {
+    static const AddressRange f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuMemGetAddressRange", &p, 3020, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return AddressRange(nullptr);
+        }
+        return reinterpret_cast<AddressRange>(p);
+    }();
+    return f;
+}
+
+cb_status DevicePtrs::check(const void* p, const char* what, int i, int align) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    if (a && a % (uintptr_t)align == 0)
+        for (int k = 0; k < n_; ++k)
+            if (a >= lo_[k] && a < hi_[k]) return CB_OK;
+    const cb_status st = check_device_ptr(ctx_, p, what, i, align);
+    if (st != CB_OK || n_ == 8 || !address_range()) return st;
+    CUdeviceptr base = 0;
+    size_t size = 0;
+    if (address_range()(&base, &size, (CUdeviceptr)a) == CUDA_SUCCESS && size) {
+        lo_[n_] = (uintptr_t)base;
+        hi_[n_++] = (uintptr_t)base + size;
+    }
     return CB_OK;
 }
 

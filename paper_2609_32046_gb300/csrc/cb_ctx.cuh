@@ -68,6 +68,19 @@ cb_status fail(cb_ctx* ctx, cb_status st, const char* fmt, ...);
 cb_status check_device_ptr(cb_ctx* ctx, const void* p, const char* what, int i, int align = 16);
 cb_status check_source_ptr(cb_ctx* ctx, const void* p, const char* what, int i, int align, const void** dev);
 
+// check_device_ptr for the many pointers of one call: allocations that one of them was found in are known for the
+// others (a query of the driver takes longer than all the rest of a pointer's check).
+class DevicePtrs {
+public:
+    explicit DevicePtrs(cb_ctx* ctx) : ctx_(ctx) {}
+    cb_status check(const void* p, const char* what, int i, int align = 16);
+
+private:
+    cb_ctx* ctx_;
+    uintptr_t lo_[8] = {}, hi_[8] = {};
+    int n_ = 0;
+};
+
 // cb_attend's room for partial results, allocated by the first call that needs it.
 cb_status attend_scratch(cb_ctx* ctx, cudaStream_t st);
 

@@ -59,32 +59,32 @@ int log2_of(int32_t page_size) {
     return sh;
 }
 
-cb_status check_page_fields(cb_ctx* ctx, const int32_t* pages, int32_t page_size, int64_t n_pages, const char* what, int i) {
+cb_status check_page_fields(cb_ctx* ctx, DevicePtrs& ptrs, const int32_t* pages, int32_t page_size, int64_t n_pages, const char* what, int i) {
     if (page_size < 1 || page_size > 65536 || (page_size & (page_size - 1)) != 0)
         return fail(ctx, CB_EINVAL, "%s[%d].page_size = %d is not a power of two in [1, 65536]", what, i, page_size);
     if (n_pages < 1) return fail(ctx, CB_EINVAL, "%s[%d].n_pages must be at least 1", what, i);
-    return check_device_ptr(ctx, pages, "pages", i, 4);
+    return ptrs.check(pages, "pages", i, 4);
 }
 
-cb_status check_packed(cb_ctx* ctx, const cb_packed& p, int i) {
+cb_status check_packed(cb_ctx* ctx, DevicePtrs& ptrs, const cb_packed& p, int i) {
     const int d = ctx->cfg.head_dim;
     const int64_t most = ctx->cfg.max_positions < kMaxRows - 4096 ? ctx->cfg.max_positions : kMaxRows - 4096;
     if (p.T < 0 || p.T > most)
         return fail(ctx, CB_ESHAPE, "caches[%d].T = %lld not in [0, %lld]", i, (long long)p.T, (long long)most);
     cb_status st;
-    if (p.length && (st = check_device_ptr(ctx, p.length, "caches.length", i, 4))) return st;
+    if (p.length && (st = ptrs.check(p.length, "caches.length", i, 4))) return st;
     if (p.T == 0) return CB_OK;
     const int scale_align = d == 128 ? 8 : 4;
-    if ((st = check_device_ptr(ctx, p.k, "caches.k", i))) return st;
-    if ((st = check_device_ptr(ctx, p.v, "caches.v", i))) return st;
-    if ((st = check_device_ptr(ctx, p.k_scale, "caches.k_scale", i, scale_align))) return st;
-    if ((st = check_device_ptr(ctx, p.v_scale, "caches.v_scale", i, scale_align))) return st;
+    if ((st = ptrs.check(p.k, "caches.k", i))) return st;
+    if ((st = ptrs.check(p.v, "caches.v", i))) return st;
+    if ((st = ptrs.check(p.k_scale, "caches.k_scale", i, scale_align))) return st;
+    if ((st = ptrs.check(p.v_scale, "caches.v_scale", i, scale_align))) return st;
     auto ok = [d](int64_t s) { return s > 0 && s % d == 0 && s / d < kMaxRows * 16; };
     if (!ok(p.s_layer) || !ok(p.s_head) || !ok(p.s_pos))
         return fail(ctx, CB_EINVAL, "caches[%d]: strides must be positive multiples of head_dim", i);
     if (p.pages) {
         if (!ok(p.s_page)) return fail(ctx, CB_EINVAL, "caches[%d].s_page must be a positive multiple of head_dim", i);
-        if ((st = check_page_fields(ctx, p.pages, p.page_size, p.n_pages, "caches", i))) return st;
+        if ((st = check_page_fields(ctx, ptrs, p.pages, p.page_size, p.n_pages, "caches", i))) return st;
         if (p.n_pages > kMaxRows || p.s_page / d > kMaxRows / p.n_pages ||
             p.s_pos / d > kMaxRows / p.page_size ||
             (p.n_pages - 1) * (p.s_page / d) + (p.page_size - 1) * (p.s_pos / d) >= kMaxRows)
@@ -163,6 +163,7 @@ cb_status rotary_impl(cb_ctx* ctx, int32_t n, const cb_vectors* sets, const cb_r
     if (rope->dims < 0 || rope->dims > d || rope->dims % 16)
         return fail(ctx, CB_EINVAL, "rope dims %d not a multiple of 16 up to %d", rope->dims, d);
     DeviceGuard dg(ctx->device);
+    DevicePtrs ptrs(ctx);
     if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
     const int dims = rope->dims ? rope->dims : d;
     cb_status st;
@@ -186,8 +187,8 @@ cb_status rotary_impl(cb_ctx* ctx, int32_t n, const cb_vectors* sets, const cb_r
         if (!same && x < y + 2 * so && y < x + 2 * si)
             return fail(ctx, CB_EINVAL, "sets[%d]: y overlaps x and is not x itself", i);
         if (!rows_apart(out, 3, d)) return fail(ctx, CB_EINVAL, "sets[%d]: vectors of y overlap", i);
-        if ((st = check_device_ptr(ctx, v.x, "sets.x", i)) || (st = check_device_ptr(ctx, v.y, "sets.y", i))) return st;
-        if (v.pos && (st = check_device_ptr(ctx, v.pos, "sets.pos", i, 4))) return st;
+        if ((st = ptrs.check(v.x, "sets.x", i)) || (st = ptrs.check(v.y, "sets.y", i))) return st;
+        if (v.pos && (st = ptrs.check(v.pos, "sets.pos", i, 4))) return st;
         if (!v.pos && (v.pos0 < -kMaxPos || v.pos0 > kMaxPos - v.n_tokens))
             return fail(ctx, CB_EINVAL, "sets[%d].pos0 is not within +-2^40", i);
         some.push_back(i);
@@ -228,13 +229,14 @@ cb_status pack_impl(cb_ctx* ctx, int32_t n, const cb_kv* senders, const int32_t*
     if (layer < 0 || n_layers < 1 || n_layers > c.n_layers - layer)
         return fail(ctx, CB_ESHAPE, "layers [%d, %d) not in [0, %d)", layer, layer + n_layers, c.n_layers);
     DeviceGuard dg(ctx->device);
+    DevicePtrs ptrs(ctx);
     if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
     std::vector<const void*> kdev(n), vdev(n);
     cb_status st;
     for (int i = 0; i < n; ++i) {
         const cb_kv& s = senders[i];
         const bool by_row = rows && rows[i];
-        if ((st = check_packed(ctx, caches[i], i))) return st;
+        if ((st = check_packed(ctx, ptrs, caches[i], i))) return st;
         if (count[i] < 0 || count[i] >= kMaxRows) return fail(ctx, CB_EBUDGET, "count[%d] = %lld", i, (long long)count[i]);
         if (count[i] == 0) continue;
         if (s.T < 1 || s.T > c.max_positions)
@@ -252,10 +254,10 @@ cb_status pack_impl(cb_ctx* ctx, int32_t n, const cb_kv* senders, const int32_t*
         if ((st = check_source_ptr(ctx, s.v, "senders.v", i, 16, &vdev[i]))) return st;
         if (s.pages) {
             if (!stride_ok(s.s_page)) return fail(ctx, CB_EINVAL, "senders[%d].s_page must be a positive multiple of 8", i);
-            if ((st = check_page_fields(ctx, s.pages, s.page_size, s.n_pages, "senders", i))) return st;
+            if ((st = check_page_fields(ctx, ptrs, s.pages, s.page_size, s.n_pages, "senders", i))) return st;
         }
-        if (idx && idx[i] && (st = check_device_ptr(ctx, idx[i], "idx", i, 4))) return st;
-        if (by_row && (st = check_device_ptr(ctx, rows[i], "rows", i, 4))) return st;
+        if (idx && idx[i] && (st = ptrs.check(idx[i], "idx", i, 4))) return st;
+        if (by_row && (st = ptrs.check(rows[i], "rows", i, 4))) return st;
     }
     for (int b0 = 0; b0 < n; b0 += kMaxPackBatch) {
         PackBatch b;
@@ -299,19 +301,20 @@ cb_status unpack_impl(cb_ctx* ctx, int32_t n, const cb_packed* caches, const int
         o_layer / c.n_kv_heads < o_head)
         return fail(ctx, CB_EINVAL, "output strides must be multiples of 8 and not overlap rows");
     DeviceGuard dg(ctx->device);
+    DevicePtrs ptrs(ctx);
     if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
     cb_status st;
-    if ((st = check_device_ptr(ctx, k_out, "k_out", 0))) return st;
-    if ((st = check_device_ptr(ctx, v_out, "v_out", 0))) return st;
+    if ((st = ptrs.check(k_out, "k_out", 0))) return st;
+    if ((st = ptrs.check(v_out, "v_out", 0))) return st;
     for (int i = 0; i < n; ++i) {
-        if ((st = check_packed(ctx, caches[i], i))) return st;
+        if ((st = check_packed(ctx, ptrs, caches[i], i))) return st;
         if (count[i] < 0 || count[i] >= kMaxRows) return fail(ctx, CB_EBUDGET, "count[%d] = %lld", i, (long long)count[i]);
         const bool by_idx = idx && idx[i];
         if (count[i] > 0 && (caches[i].T == 0 || (!by_idx && count[i] > caches[i].T)))
             return fail(ctx, CB_EBUDGET, "count[%d] = %lld above caches[%d].T", i, (long long)count[i], i);
         if (out_offset[i] < 0 || out_offset[i] > out_capacity - count[i])
             return fail(ctx, CB_EBUDGET, "cache %d: rows exceed out_capacity %lld", i, (long long)out_capacity);
-        if (count[i] > 0 && by_idx && (st = check_device_ptr(ctx, idx[i], "idx", i, 4))) return st;
+        if (count[i] > 0 && by_idx && (st = ptrs.check(idx[i], "idx", i, 4))) return st;
     }
     for (int b0 = 0; b0 < n; b0 += kMaxPackBatch) {
         PackBatch b;
@@ -349,12 +352,13 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
     if (causal != 0 && causal != 1) return fail(ctx, CB_EINVAL, "causal must be 0 or 1");
     if (window < 0 || (window && !causal)) return fail(ctx, CB_EINVAL, "window must be >= 0, and 0 unless causal");
     DeviceGuard dg(ctx->device);
+    DevicePtrs ptrs(ctx);
     if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
     cb_status st;
     std::vector<int32_t> some;
     for (int i = 0; i < n; ++i) {
         const cb_attend_query& q = queries[i];
-        if ((st = check_packed(ctx, caches[i], i))) return st;
+        if ((st = check_packed(ctx, ptrs, caches[i], i))) return st;
         if (q.m < 0 || q.m > c.max_query_tokens)
             return fail(ctx, CB_ESHAPE, "queries[%d].m = %d not in [0, %d]", i, q.m, c.max_query_tokens);
         if (q.m == 0) continue;
@@ -363,9 +367,9 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
             return fail(ctx, CB_EINVAL, "queries[%d]: strides must be positive multiples of 8", i);
         if (span_of(in, 2, d) < 0 || span_of(out, 2, d) < 0 || !rows_apart(out, 2, d))
             return fail(ctx, CB_EINVAL, "queries[%d]: strides are too large, or rows of out overlap", i);
-        if ((st = check_device_ptr(ctx, q.q, "queries.q", i)) || (st = check_device_ptr(ctx, q.out, "queries.out", i)))
+        if ((st = ptrs.check(q.q, "queries.q", i)) || (st = ptrs.check(q.out, "queries.out", i)))
             return st;
-        if (q.lse && (st = check_device_ptr(ctx, q.lse, "queries.lse", i, 4))) return st;
+        if (q.lse && (st = ptrs.check(q.lse, "queries.lse", i, 4))) return st;
         // (units of work are counted in 32 bits)
         if ((caches[i].T / 128 + 2) * c.n_kv_heads * ((int64_t)q.m * ctx->G / 128 + 1) > ((int64_t)1 << 31) / kMaxBatch)
             return fail(ctx, CB_ESHAPE, "sequence %d: too many positions, heads and query tokens for one launch", i);

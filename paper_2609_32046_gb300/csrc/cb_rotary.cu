@@ -18,6 +18,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;
+constexpr int kMaxTokens = 8;       // tokens a block takes at a time
 
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_f(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -27,71 +28,95 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
-// A unit is 16 elements of a row, two 16-byte pieces: 8 pairs (8u .. 8u + 7) of the rotary part, whose
+// Tokens a block takes at a time: enough vectors (layer, head) for four a thread.
+__host__ __device__ __forceinline__ int tokens_at_once(int rows, int lanes) {
+    const int n = (kUnroll * lanes + rows - 1) / rows;
+    return n < 1 ? 1 : n < kMaxTokens ? n : kMaxTokens;
+}
+
+// A unit is 16 elements of a vector, two 16-byte pieces: 8 pairs (8u .. 8u + 7) of the rotary part, whose
 // halves are dims / 2 apart (STYLE 0) or which lie side by side (STYLE 1), or 16 elements behind it.
-// Block: one token of one set, D / 16 units of 256 / (D / 16) rows (layer, head) at a time; a thread
-// keeps its unit's eight sines and cosines for all rows it walks, so that the special-function unit
-// works once a token and not once a head.
-// Grid: x = token (and slice of the rows, innermost), y = set.
+// A block takes up to eight tokens of a set at a time: their sines and cosines go to shared memory, one a
+// thread, and D / 16 units of 256 / (D / 16) vectors in turn read them there.  (With every thread working out
+// the eight of its unit, 24 vectors a token left the special-function unit more to do than memory: 6001
+// tokens x 8 layers x 24 heads, d = 64, 91 us.)
+// Grid: x = token group (and slice of its vectors, innermost), y = set.
 template <int D, int STYLE>
 __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ RotaryBatch b, int slices) {
     constexpr int U = D / 16, LANES = kThreads / U;
+    __shared__ __align__(16) float2 turn_of[2][kMaxTokens][D / 2];       // cosine, sine
     const RotarySet& s = b.s[blockIdx.y];
-    const int64_t r = blockIdx.x / (unsigned)slices;
-    if (r >= s.n_tokens) return;
     const int u = threadIdx.x % U;
     const bool turn = u * 16 < b.dims;
-    if (!turn && s.x == s.y) return;                       // in place: nothing to do behind the rotary part
     const int e0 = turn && STYLE == 0 ? u * 8 : u * 16;    // the unit's two pieces
     const int e1 = turn && STYLE == 0 ? u * 8 + b.dims / 2 : u * 16 + 8;
-    float c[8], n[8];
-    if (turn) {
-        const int64_t pos = s.pos ? (int64_t)__ldg(s.pos + r) : s.pos0 + r;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint64_t turns = (uint64_t)pos * b.turns[u * 8 + k];
+    const bool idle = !turn && s.x == s.y;                 // in place: nothing to do behind the rotary part
+    const int H = s.n_heads, NL = s.n_layers, rows = NL * H, many = tokens_at_once(rows, LANES);
+    const int pairs = b.dims / 2, step = LANES * slices;
+    const int dt = step / rows, dl = step % rows / H, dh = step % rows % H;      // a step's tokens, layers, heads
+    int buffer = 0;
+    for (int64_t t0 = (int64_t)(blockIdx.x / (unsigned)slices) * many; t0 < s.n_tokens;
+         t0 += (int64_t)(gridDim.x / (unsigned)slices) * many, buffer ^= 1) {
+        const int n = (int)min((int64_t)many, s.n_tokens - t0);
+        for (int i = threadIdx.x; i < n * pairs; i += kThreads) {
+            const int t = i / pairs, k = i - t * pairs;
+            const int64_t pos = s.pos ? (int64_t)__ldg(s.pos + t0 + t) : s.pos0 + t0 + t;
+            const uint64_t turns = (uint64_t)pos * b.turns[k];
             const float a = (float)(int32_t)(uint32_t)(turns >> 32) * 1.4629180792671596e-09f;   // 2 pi / 2^32
-            c[k] = __cosf(a) * b.gain;
-            n[k] = __sinf(a) * b.sine_gain;
+            turn_of[buffer][t][k] = make_float2(__cosf(a) * b.gain, __sinf(a) * b.sine_gain);
         }
-    }
-    const int rows = s.n_layers * s.n_heads;
-    const int step = LANES * slices;
-    for (int q0 = (int)(blockIdx.x % (unsigned)slices) * LANES + threadIdx.x / U; q0 < rows; q0 += step * kUnroll) {
-        uint4 va[kUnroll], vb[kUnroll];
-        uint16_t* out[kUnroll];
+        __syncthreads();      // (a buffer is written again two turns later, behind the next turn's barrier)
+        if (idle) continue;
+        const int first = (int)(blockIdx.x % (unsigned)slices) * LANES + threadIdx.x / U;
+        int t = first / rows, l = first % rows / H, h = first % rows % H;
+        while (t < n) {
+            uint4 va[kUnroll], vb[kUnroll];
+            uint16_t* out[kUnroll];
+            int at[kUnroll];
 #pragma unroll
-        for (int i = 0; i < kUnroll; ++i) {
-            const int q = q0 + i * step;
-            if (q >= rows) break;
-            const int l = q / s.n_heads, h = q - l * s.n_heads;
-            const uint16_t* x = s.x + l * s.s_layer + r * s.s_tok + h * s.s_head;
-            out[i] = s.y + l * s.o_layer + r * s.o_tok + h * s.o_head;
-            va[i] = *reinterpret_cast<const uint4*>(x + e0);
-            vb[i] = *reinterpret_cast<const uint4*>(x + e1);
-        }
-#pragma unroll
-        for (int i = 0; i < kUnroll; ++i) {
-            if (q0 + i * step >= rows) break;
-            if (turn) {
-                uint32_t a[4] = {va[i].x, va[i].y, va[i].z, va[i].w}, w[4] = {vb[i].x, vb[i].y, vb[i].z, vb[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (STYLE == 0) {        // a: first elements of pairs 2j, 2j + 1; w: their second ones
-                        const float a0 = lo_f(a[j]), a1 = hi_f(a[j]), w0 = lo_f(w[j]), w1 = hi_f(w[j]);
-                        a[j] = pack_bf16(a0 * c[2 * j] - w0 * n[2 * j], a1 * c[2 * j + 1] - w1 * n[2 * j + 1]);
-                        w[j] = pack_bf16(w0 * c[2 * j] + a0 * n[2 * j], w1 * c[2 * j + 1] + a1 * n[2 * j + 1]);
-                    } else {                 // a: pair j; w: pair 4 + j
-                        const float a0 = lo_f(a[j]), a1 = hi_f(a[j]), w0 = lo_f(w[j]), w1 = hi_f(w[j]);
-                        a[j] = pack_bf16(a0 * c[j] - a1 * n[j], a1 * c[j] + a0 * n[j]);
-                        w[j] = pack_bf16(w0 * c[4 + j] - w1 * n[4 + j], w1 * c[4 + j] + w0 * n[4 + j]);
-                    }
+            for (int i = 0; i < kUnroll; ++i) {
+                at[i] = -1;
+                if (t < n) {
+                    const int64_t r = t0 + t;
+                    const uint16_t* x = s.x + l * s.s_layer + r * s.s_tok + h * s.s_head;
+                    out[i] = s.y + l * s.o_layer + r * s.o_tok + h * s.o_head;
+                    va[i] = *reinterpret_cast<const uint4*>(x + e0);
+                    vb[i] = *reinterpret_cast<const uint4*>(x + e1);
+                    at[i] = t;
                 }
-                va[i] = make_uint4(a[0], a[1], a[2], a[3]);
-                vb[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                h += dh;
+                l += dl;
+                t += dt;
+                if (h >= H) { h -= H; ++l; }
+                if (l >= NL) { l -= NL; ++t; }
             }
-            *reinterpret_cast<uint4*>(out[i] + e0) = va[i];
-            *reinterpret_cast<uint4*>(out[i] + e1) = vb[i];
+#pragma unroll
+            for (int i = 0; i < kUnroll; ++i) {
+                if (at[i] < 0) continue;
+                if (turn) {
+                    const float4* f = reinterpret_cast<const float4*>(&turn_of[buffer][at[i]][u * 8]);
+                    uint32_t a[4] = {va[i].x, va[i].y, va[i].z, va[i].w}, w[4] = {vb[i].x, vb[i].y, vb[i].z, vb[i].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (STYLE == 0) {        // a: first elements of pairs 2j, 2j + 1; w: their second ones
+                            const float4 c = f[j];
+                            const float a0 = lo_f(a[j]), a1 = hi_f(a[j]), w0 = lo_f(w[j]), w1 = hi_f(w[j]);
+                            a[j] = pack_bf16(a0 * c.x - w0 * c.y, a1 * c.z - w1 * c.w);
+                            w[j] = pack_bf16(w0 * c.x + a0 * c.y, w1 * c.z + a1 * c.w);
+                        } else {                 // a: pairs 0..3 of the unit, w: 4..7; word j is one pair
+                            const float4 c = f[j / 2], g = f[2 + j / 2];
+                            const float ca = j & 1 ? c.z : c.x, na = j & 1 ? c.w : c.y, cw = j & 1 ? g.z : g.x, nw = j & 1 ? g.w : g.y;
+                            const float a0 = lo_f(a[j]), a1 = hi_f(a[j]), w0 = lo_f(w[j]), w1 = hi_f(w[j]);
+                            a[j] = pack_bf16(a0 * ca - a1 * na, a1 * ca + a0 * na);
+                            w[j] = pack_bf16(w0 * cw - w1 * nw, w1 * cw + w0 * nw);
+                        }
+                    }
+                    va[i] = make_uint4(a[0], a[1], a[2], a[3]);
+                    vb[i] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+                __stcs(reinterpret_cast<uint4*>(out[i] + e0), va[i]);
+                __stcs(reinterpret_cast<uint4*>(out[i] + e1), vb[i]);
+            }
         }
     }
 }
@@ -99,18 +124,20 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
 }  // namespace
 
 cudaError_t launch_rotary(const RotaryBatch& b, int head_dim, int style, cudaStream_t st, int num_sms) {
-    int64_t tokens = 0, rows = 0;
+    const int lanes = kThreads / (head_dim / 16);
+    int64_t groups = 0, most = 1;
     for (int i = 0; i < b.n; ++i) {
-        const int64_t q = (int64_t)b.s[i].n_layers * b.s[i].n_heads;
-        tokens = b.s[i].n_tokens > tokens ? b.s[i].n_tokens : tokens;
-        rows = q > rows ? q : rows;
+        const int rows = b.s[i].n_layers * b.s[i].n_heads, many = tokens_at_once(rows, lanes);
+        const int64_t g = (b.s[i].n_tokens + many - 1) / many, k = ((int64_t)rows * many + lanes - 1) / lanes;
+        groups = g > groups ? g : groups;
+        most = k > most ? k : most;
     }
-    if (tokens == 0 || rows == 0) return cudaSuccess;
-    // enough blocks for eight an SM where there are few tokens, at least one pass of rows a block
-    const int64_t lanes = kThreads / (head_dim / 16), most = (rows + lanes - 1) / lanes;
-    int64_t slices = ((int64_t)num_sms * 8 + tokens * b.n - 1) / (tokens * b.n);
+    // slices where there are few groups, so that eight blocks an SM have work, each a pass of vectors at least
+    const int64_t full = (int64_t)num_sms * 8;
+    int64_t slices = (full + groups * b.n - 1) / (groups * b.n);
     slices = slices < most ? slices : most;
-    const dim3 grid((unsigned)(tokens * slices), (unsigned)b.n);
+    const int64_t cap = full * 4 / slices > 1 ? full * 4 / slices : 1;
+    const dim3 grid((unsigned)((groups < cap ? groups : cap) * slices), (unsigned)b.n);
     if (head_dim == 128) {
         if (style == 0) k_rotary<128, 0><<<grid, kThreads, 0, st>>>(b, (int)slices);
         else k_rotary<128, 1><<<grid, kThreads, 0, st>>>(b, (int)slices);
