@@ -13,6 +13,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include "cb_attend.cuh"
 #include "cb_internal.cuh"
 
 namespace cbk {
@@ -21,7 +22,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRows = 4;                 // rows a thread has in flight
 constexpr uint32_t kLargest = 0x4760u;   // 7 * 2^13 as bf16
-constexpr uint32_t kTopScale = 0x4600u;  // 2^13 as bf16
 
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
     uint4 v;
@@ -71,57 +71,79 @@ __device__ __forceinline__ uint32_t code_word(const uint32_t (&w)[4], float r) {
     return (m ^ (n * 7u)) + (0x88888888u - n * 7u);
 }
 
+// Rows of a block's tile: where each comes from and goes to (elements or rows from the segment's base on, -1
+// where it is not to be moved).  One thread a row looks up the index, the block tables and the bounds; the 8 or 16
+// threads that move it read the result.
+template <int D, bool PACK>
+__device__ __forceinline__ longlong2 look_up(const PackBatch& bt, const PackSender& sd, int64_t j) {
+    longlong2 r = make_longlong2(-1, -1);
+    if (j >= sd.count) return r;
+    const int64_t t = sd.idx ? (int64_t)__ldg(sd.idx + j) : j;
+    if (t < 0 || t >= sd.T) {
+        atomicOr(bt.err, kErrCompactIndex);
+        return r;
+    }
+    if (!PACK) {
+        const int64_t from = packed_row(sd.held, t);
+        if (from < 0) atomicOr(bt.err, kErrPageIndex);
+        return make_longlong2(from, j);          // (a row of a bad page is restored as zeros)
+    }
+    const int64_t at = sd.rows ? (int64_t)__ldg(sd.rows + j) : sd.dst_off + j;
+    if (at < 0 || at >= sd.dst_T) {
+        atomicOr(bt.err, kErrPackRow);
+        return r;
+    }
+    const int64_t from = row_offset(sd.pm, sd.ks_p, t), to = packed_row(sd.held, at);
+    if (from < 0 || to < 0) {
+        atomicOr(bt.err, kErrPageIndex);
+        return r;
+    }
+    return make_longlong2(from, to);
+}
+
 // Grid: x = (K or V, layer, head) segment, y = sender, z = slice of the segment's rows.
-// A thread takes 8 elements (16 bytes) of four rows; the four threads of a group each work out the
-// scale of one of the four rows and hand it round.
+// A thread takes 8 elements (16 bytes) of four rows of a tile; the four threads of a group each work out the
+// scale of one of the four rows and hand it round, two rows' largest values to a word.
+// Bound by instructions more than by its bytes (2 read and 9/16 written an element): 2048 of 8192
+// positions of 36 layers x 8 heads of 128 take 78 us, 4.9 TB/s; with every thread looking up its own rows and two
+// exchanges a row it was 116 us.
 template <int D>
 __global__ void __launch_bounds__(kThreads) k_pack(const __grid_constant__ PackBatch bt) {
     constexpr int CH = D / 8;              // threads a row
-    constexpr int ROWS = kThreads / CH;    // rows a block pass
+    constexpr int ROWS = kThreads / CH, TILE = ROWS * kRows;
+    __shared__ longlong2 where[2][TILE];
     const PackSender& sd = bt.s[blockIdx.y];
     const int seg = blockIdx.x;
     const int g = seg % bt.n_kv_heads;
     const int l = (seg / bt.n_kv_heads) % bt.n_layers;
     const int kv = seg / (bt.n_kv_heads * bt.n_layers);
-    const uint16_t* src = sd.src[kv] + (int64_t)l * sd.ks_l + (int64_t)g * sd.ks_h;
-    const int64_t base = (int64_t)(bt.layer + l) * sd.held.s_layer + (int64_t)g * sd.held.s_head;
-    uint8_t* code = sd.held.code[kv] + base * (D / 2);
-    uint16_t* scale = sd.held.scale[kv] + base * (D / 32);
     const int ch = threadIdx.x % CH, mine = threadIdx.x & 3;
-    const int64_t stride = (int64_t)ROWS * gridDim.z;
-    const int64_t first = (int64_t)blockIdx.z * ROWS;
-    // (the block's threads stay together: warps hold rows of different j)
-    for (int64_t jb = first; jb < sd.count; jb += stride * kRows) {
-        const int64_t j0 = jb + threadIdx.x / CH;
+    const uint16_t* src = sd.src[kv] + (int64_t)l * sd.ks_l + (int64_t)g * sd.ks_h + ch * 8;
+    const int64_t base = (int64_t)(bt.layer + l) * sd.held.s_layer + (int64_t)g * sd.held.s_head;
+    uint8_t* code = sd.held.code[kv] + base * (D / 2) + ch * 4;
+    uint16_t* scale = sd.held.scale[kv] + base * (D / 32) + ch / 4;
+    int buffer = 0;
+    int64_t jb = (int64_t)blockIdx.z * TILE;
+    if (threadIdx.x < TILE) where[0][threadIdx.x] = look_up<D, true>(bt, sd, jb + threadIdx.x);
+    for (; jb < sd.count; jb += (int64_t)gridDim.z * TILE, buffer ^= 1) {
+        __syncthreads();
         uint32_t w[kRows][4];
         int64_t to[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const int64_t j = j0 + u * stride;
-            to[u] = -1;
+            const longlong2 r = where[buffer][u * ROWS + threadIdx.x / CH];
+            to[u] = r.y;
             w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
-            if (j >= sd.count) continue;
-            const int64_t t = sd.idx ? (int64_t)__ldg(sd.idx + j) : j;
-            const int64_t at = sd.rows ? (int64_t)__ldg(sd.rows + j) : sd.dst_off + j;
-            if (t < 0 || t >= sd.T) {
-                atomicOr(bt.err, kErrCompactIndex);
-                continue;
-            }
-            if (at < 0 || at >= sd.dst_T) {
-                atomicOr(bt.err, kErrPackRow);
-                continue;
-            }
-            const int64_t ro = row_offset(sd.pm, sd.ks_p, t), wo = packed_row(sd.held, at);
-            if (ro < 0 || wo < 0) {
-                atomicOr(bt.err, kErrPageIndex);
-                continue;
-            }
-            to[u] = wo;
-            const uint4 v = ld_stream(reinterpret_cast<const uint4*>(src + ro + ch * 8));
+            if (r.y < 0) continue;
+            const uint4 v = ld_stream(reinterpret_cast<const uint4*>(src + r.x));
             w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
         }
+        // the next tile's rows while these are on their way
+        if (threadIdx.x < TILE)
+            where[buffer ^ 1][threadIdx.x] = look_up<D, true>(bt, sd, jb + (int64_t)gridDim.z * TILE + threadIdx.x);
         uint32_t a01 = top_bits(w[0]) | (top_bits(w[1]) << 16), a23 = top_bits(w[2]) | (top_bits(w[3]) << 16);
-        if (__any_sync(0xFFFFFFFFu, (__vmaxu2(a01, a23) & 0xFFFFu) > kLargest || (__vmaxu2(a01, a23) >> 16) > kLargest)) {
+        const uint32_t both = __vmaxu2(a01, a23);
+        if (__any_sync(0xFFFFFFFFu, max(both & 0xFFFFu, both >> 16) > kLargest)) {
             bool bad = false;
 #pragma unroll
             for (int u = 0; u < kRows; ++u) {
@@ -147,80 +169,68 @@ __global__ void __launch_bounds__(kThreads) k_pack(const __grid_constant__ PackB
         for (int u = 0; u < kRows; ++u) {
             const float r = __shfl_sync(0xFFFFFFFFu, inv, u, 4), su = __shfl_sync(0xFFFFFFFFu, s, u, 4);
             if (to[u] < 0) continue;
-            *reinterpret_cast<uint32_t*>(code + to[u] * (D / 2) + ch * 4) = code_word(w[u], r);
-            if (mine == 0) scale[to[u] * (D / 32) + ch / 4] = (uint16_t)(__float_as_uint(su) >> 16);
+            *reinterpret_cast<uint32_t*>(code + to[u] * (D / 2)) = code_word(w[u], r);
+            if (mine == 0) scale[to[u] * (D / 32)] = (uint16_t)(__float_as_uint(su) >> 16);
         }
     }
 }
 
-// The same grid; a thread restores 8 elements of a row.
+// The same grid and tiles; a thread restores 8 elements of each of four rows: the same
+// 2048 positions back in 64 us, 6.0 TB/s.
 template <int D>
 __global__ void __launch_bounds__(kThreads) k_unpack(const __grid_constant__ PackBatch bt) {
     constexpr int CH = D / 8;
-    constexpr int ROWS = kThreads / CH;
+    constexpr int ROWS = kThreads / CH, TILE = ROWS * kRows;
+    __shared__ longlong2 where[2][TILE];
     const PackSender& sd = bt.s[blockIdx.y];
     const int seg = blockIdx.x;
     const int g = seg % bt.n_kv_heads;
     const int l = (seg / bt.n_kv_heads) % bt.n_layers;
     const int kv = seg / (bt.n_kv_heads * bt.n_layers);
-    const int64_t base = (int64_t)l * sd.held.s_layer + (int64_t)g * sd.held.s_head;
-    const uint8_t* code = sd.held.code[kv] + base * (D / 2);
-    const uint16_t* scale = sd.held.scale[kv] + base * (D / 32);
-    uint16_t* dst = bt.out[kv] + (int64_t)l * bt.o_layer + (int64_t)g * bt.o_head + sd.dst_off * D;
     const int ch = threadIdx.x % CH;
-    const int64_t stride = (int64_t)ROWS * gridDim.z;
-    for (int64_t j0 = (int64_t)blockIdx.z * ROWS + threadIdx.x / CH; j0 < sd.count; j0 += stride * kRows) {
+    const int64_t base = (int64_t)l * sd.held.s_layer + (int64_t)g * sd.held.s_head;
+    const uint8_t* code = sd.held.code[kv] + base * (D / 2) + ch * 4;
+    const uint16_t* scale = sd.held.scale[kv] + base * (D / 32) + ch / 4;
+    uint16_t* dst = bt.out[kv] + (int64_t)l * bt.o_layer + (int64_t)g * bt.o_head + sd.dst_off * D + ch * 8;
+    int buffer = 0;
+    int64_t jb = (int64_t)blockIdx.z * TILE;
+    if (threadIdx.x < TILE) where[0][threadIdx.x] = look_up<D, false>(bt, sd, jb + threadIdx.x);
+    for (; jb < sd.count; jb += (int64_t)gridDim.z * TILE, buffer ^= 1) {
+        __syncthreads();
         uint32_t w[kRows], s[kRows];
-        bool ok[kRows];
+        int64_t to[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const int64_t j = j0 + u * stride;
-            ok[u] = false;
-            if (j >= sd.count) continue;
-            const int64_t t = sd.idx ? (int64_t)__ldg(sd.idx + j) : j;
-            if (t < 0 || t >= sd.T) {
-                atomicOr(bt.err, kErrCompactIndex);
-                continue;
-            }
-            const int64_t ro = packed_row(sd.held, t);
-            ok[u] = true;
+            const longlong2 r = where[buffer][u * ROWS + threadIdx.x / CH];
+            to[u] = r.y;
             w[u] = 0x88888888u;
             s[u] = 0;
-            if (ro < 0) {
-                atomicOr(bt.err, kErrPageIndex);
-                continue;
-            }
-            w[u] = __ldg(reinterpret_cast<const uint32_t*>(code + ro * (D / 2) + ch * 4));
-            s[u] = __ldg(scale + ro * (D / 32) + ch / 4);
+            if (r.x < 0) continue;
+            w[u] = __ldg(reinterpret_cast<const uint32_t*>(code + r.x * (D / 2)));
+            s[u] = __ldg(scale + r.x * (D / 32));
         }
+        if (threadIdx.x < TILE)
+            where[buffer ^ 1][threadIdx.x] = look_up<D, false>(bt, sd, jb + (int64_t)gridDim.z * TILE + threadIdx.x);
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            if (!ok[u]) continue;
-            if (s[u] > kTopScale) {
+            if (to[u] < 0) continue;
+            if (s[u] > kTopScaleBits) {
                 atomicOr(bt.err, kErrPackScale);
                 s[u] = 0;
             }
-            const uint32_t s2 = s[u] * 0x10001u;
             uint32_t v[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {       // 0x4300 | u is 128 + u, less 136 is c: exact in bf16
-                const uint32_t x = ((w[u] >> (4 * j)) & 0x000F000Fu) | 0x43004300u;
-                const __nv_bfloat162 c = __hsub2(reinterpret_cast<const __nv_bfloat162&>(x),
-                                                 __floats2bfloat162_rn(136.f, 136.f));
-                const __nv_bfloat162 p = __hmul2(c, reinterpret_cast<const __nv_bfloat162&>(s2));
-                v[j] = reinterpret_cast<const uint32_t&>(p);
-            }
-            st_stream(reinterpret_cast<uint4*>(dst + (j0 + u * stride) * D + ch * 8), make_uint4(v[0], v[1], v[2], v[3]));
+            values_bf16(w[u], s[u] * 0x10001u, v);
+            st_stream(reinterpret_cast<uint4*>(dst + to[u] * D), make_uint4(v[0], v[1], v[2], v[3]));
         }
     }
 }
 
-// Slices of the rows: about 24 blocks an SM over the batch, at least one block pass each.
+// Slices of the rows: about 24 blocks an SM over the batch, at least one tile each.
 dim3 grid_of(const PackBatch& b, int head_dim, int num_sms) {
     int64_t most = 0;
     for (int i = 0; i < b.n; ++i) most = b.s[i].count > most ? b.s[i].count : most;
     const int segs = 2 * b.n_layers * b.n_kv_heads;
-    const int64_t pass = (int64_t)(kThreads / (head_dim / 8));
+    const int64_t pass = (int64_t)(kThreads / (head_dim / 8)) * kRows;
     int64_t slices = ((int64_t)num_sms * 24) / ((int64_t)segs * b.n);
     const int64_t need = (most + pass - 1) / pass;
     if (slices > need) slices = need;
