@@ -235,7 +235,7 @@ cudaError_t alloc_attend(cb_ctx* ctx, int64_t* total) {
     const int64_t rows = cbk::attend_part_rows(ctx->num_sms);
     cudaError_t e = alloc(&ctx->attend_part, (size_t)(rows * ctx->cfg.head_dim), total);
     if (e == cudaSuccess) e = alloc(&ctx->attend_ml, (size_t)rows, total);
-    const size_t n = (size_t)ctx->num_sms * cbk::kFewBlocksPerSm;
+    const size_t n = (size_t)ctx->num_sms * cbk::kFewBlocksPerSm * cbk::kFewTickets;
     if (e == cudaSuccess) e = alloc(&ctx->attend_tickets, n, total);
     // (on a stream of its own: the legacy stream would wait for, and spoil, another stream's capture)
     cudaStream_t st = nullptr;

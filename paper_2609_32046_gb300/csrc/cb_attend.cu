@@ -177,12 +177,6 @@ __device__ __forceinline__ void score_keys(const uint8_t* stage, int row0, const
     }
 }
 
-// Sums of a row: weights are exp2(z - M).
-__device__ __forceinline__ void add_part(float4& y, float& l, const float4& v, float f, float m_sum) {
-    y.x = fmaf(v.x, f, y.x); y.y = fmaf(v.y, f, y.y); y.z = fmaf(v.z, f, y.z); y.w = fmaf(v.w, f, y.w);
-    l = fmaf(m_sum, f, l);
-}
-
 template <int D, int NT>
 constexpr int few_smem() {
     constexpr int stages = kWarps * kStages * Stage<D>::kBytes, join = kWarps * 8 * NT * (D * 4 + 8);
@@ -192,6 +186,19 @@ constexpr int few_smem() {
 // Blocks an SM holds: 120 registers a thread, or 168.
 template <int D, int NT>
 constexpr int few_blocks() { return D == 128 && NT == 2 ? 3 : kFewBlocksPerSm; }
+
+// True in the last of n blocks to come here, which then sees what the others wrote.  Whole block.
+__device__ __forceinline__ bool last_of(int32_t* ticket, int n, int* last) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        *last = atomicAdd(ticket, 1) == n - 1;
+        if (*last) *ticket = 0;
+    }
+    __syncthreads();
+    if (*last) __threadfence();
+    return *last;
+}
 
 // A block takes its run of units (cb_attend.cuh), 8 NT query rows (token, head of the group) of one KV head
 // at a time; its four warps take 32 positions in turn, each with its own copies, running maximum and
@@ -409,19 +416,37 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
             }
         }
         if (!whole) {
-            const int b0 = attend_block(runs, x.first), b1 = attend_block(runs, x.first + x.units - 1);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                int32_t* ticket = b.tickets + b0 * b.n_kv_heads + g;
-                last = atomicAdd(ticket, 1) == b1 - b0;
-                if (last) *ticket = 0;
-            }
-            __syncthreads();
-            if (last) {
-                __threadfence();
-                for (int e = threadIdx.x; e < x.rows * (D / 4); e += kWarps * 32)
-                    attend_join_row<D>(b, s, g, e / (D / 4), e / (D / 4), (e % (D / 4)) * 4, ROWS, x.first, runs, b0, b1, b.n_kv_heads, g);
+            // n parts, from run b0 on, in groups of `size`, about the root of their number.  (Loads that the last
+            // block waits for: 76 parts a head joined at once took 11 us of one token's 38 over 65536 positions, in
+            // two steps 6; 16 parts took 0.8 us longer in two.)
+            const int b0 = attend_block(runs, x.first), n = attend_block(runs, x.first + x.units - 1) - b0 + 1;
+            int size = 16;
+            while (size * size < n) size += 8;
+            const int groups = (n + size - 1) / size, group = (run - b0) / size, head = b0 + group * size;
+            const int skip = attend_run(runs, b0) == x.first ? 0 : 1;          // of the first run's two slots
+            const int of_group = group == 0 ? skip : 0;
+            const int members = min(size, n - group * size);
+            const int64_t group0 = 2 * ((int64_t)head * b.n_kv_heads + g);     // its first block's slots
+            if (last_of(b.tickets + group0 + of_group, members, &last)) {
+                for (int e = threadIdx.x; e < x.rows * (D / 4); e += kWarps * 32) {
+                    const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+                    const Joined j = attend_join_row<D>(b, group0, of_group, 2 * b.n_kv_heads, members, ROWS, r, d);
+                    if (groups == 1) {
+                        attend_write<D>(b, s, g, r, d, j.y, j.M, j.l);
+                    } else {
+                        const int64_t at = (2 * (int64_t)gridDim.x + group0 + of_group) * ROWS + r;
+                        *reinterpret_cast<float4*>(b.part + at * D + d) = j.y;
+                        if (d == 0) b.part_ml[at] = make_float2(j.M, j.l);
+                    }
+                }
+                const int64_t item0 = (int64_t)b0 * b.n_kv_heads + g;
+                if (groups > 1 && last_of(b.tickets + 2 * gridDim.x + item0, groups, &last))
+                    for (int e = threadIdx.x; e < x.rows * (D / 4); e += kWarps * 32) {
+                        const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+                        const Joined j = attend_join_row<D>(b, 2 * ((int64_t)gridDim.x + item0), skip, 2 * size * b.n_kv_heads,
+                                                            groups, ROWS, r, d);
+                        attend_write<D>(b, s, g, r, d, j.y, j.M, j.l);
+                    }
             }
         }
         unit += x.n;
@@ -448,7 +473,7 @@ int64_t attend_pairs(AttendBatch& b, int tile_rows) {
     int64_t units = 0;
     b.pairs = 0;
     for (int i = 0; i < b.n; ++i) {
-        AttendSeq& s = b.s[i];
+        AttendSpan& s = b.span[i];
         const int tiles = (s.m * b.G + tile_rows - 1) / tile_rows;
         const int64_t w = b.causal && b.window ? b.window + s.m : s.T, reach = s.T < w ? s.T : w;
         s.pair0 = b.pairs;
@@ -460,7 +485,7 @@ int64_t attend_pairs(AttendBatch& b, int tile_rows) {
 
 cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
     int rows = 0;
-    for (int i = 0; i < b.n; ++i) rows = b.s[i].m > rows ? b.s[i].m : rows;
+    for (int i = 0; i < b.n; ++i) rows = b.span[i].m > rows ? b.span[i].m : rows;
     rows *= b.G;
     if (rows == 0) return cudaSuccess;
     if (rows > 16) return launch_attend_tc(b, head_dim, st, num_sms);

@@ -23,7 +23,7 @@ constexpr int kMaxPairs = kMaxBatch * 16;     // most (sequence, row tile) pairs
 constexpr int kPartRowsPerSm = 512;
 
 // Rows in the cache.
-__device__ __forceinline__ int64_t attend_length(const AttendSeq& s) {
+__device__ __forceinline__ int64_t attend_length(const AttendSpan& s) {
     if (!s.length) return s.T;
     const int64_t l = *s.length;
     return l < 0 ? 0 : l < s.T ? l : s.T;
@@ -34,7 +34,7 @@ __device__ __forceinline__ int64_t attend_length(const AttendSeq& s) {
 struct Reach {
     int64_t lo, hi, all_to_here, all_from_here;
 };
-__device__ __forceinline__ Reach attend_reach(const AttendBatch& b, const AttendSeq& s, int64_t L, int tile, int tile_rows) {
+__device__ __forceinline__ Reach attend_reach(const AttendBatch& b, const AttendSpan& s, int64_t L, int tile, int tile_rows) {
     const int first = tile * tile_rows, last = min(first + tile_rows, s.m * b.G) - 1;
     Reach x{0, L, 0, L};
     if (b.causal) {
@@ -64,13 +64,20 @@ __device__ __forceinline__ Reach attend_reach(const AttendBatch& b, const Attend
 
 // (What runs once a block or segment is rolled up: fetching the code cost more than running it.)
 
-// Units of pair p.
-__device__ __forceinline__ int attend_units_of(const AttendBatch& b, int tile_rows, int p) {
+// Sequence of pair p.
+__device__ __forceinline__ int attend_seq_of(const AttendBatch& b, int p) {
+    if (b.pairs == b.n) return p;         // (a tile each)
     int i = 0;
 #pragma unroll 1
     for (int step = kMaxBatch / 2; step; step /= 2)
-        if (i + step < b.n && b.s[i + step].pair0 <= p) i += step;
-    const Reach x = attend_reach(b, b.s[i], attend_length(b.s[i]), p - b.s[i].pair0, tile_rows);
+        if (i + step < b.n && b.span[i + step].pair0 <= p) i += step;
+    return i;
+}
+
+// Units of pair p.
+__device__ __forceinline__ int attend_units_of(const AttendBatch& b, int tile_rows, int p) {
+    const AttendSpan& s = b.span[attend_seq_of(b, p)];
+    const Reach x = attend_reach(b, s, attend_length(s), p - s.pair0, tile_rows);
     const int u = (int)((x.hi - x.lo + kUnit - 1) / kUnit);
     return u > 0 ? u : 1;
 }
@@ -149,12 +156,8 @@ __device__ __forceinline__ Item attend_item(const AttendBatch& b, const int* pre
     x.units = pre[p + 1] - pre[p];
     x.g = heads == 1 ? 0 : (u - pre[p] * heads) / x.units;
     x.first = pre[p] * heads + x.g * x.units;
-    int i = 0;
-#pragma unroll 1
-    for (int step = kMaxBatch / 2; step; step /= 2)
-        if (i + step < b.n && b.s[i + step].pair0 <= p) i += step;
-    x.seq = i;
-    x.tile = p - b.s[i].pair0;
+    x.seq = attend_seq_of(b, p);
+    x.tile = p - b.span[x.seq].pair0;
     return x;
 }
 
@@ -164,13 +167,14 @@ __device__ __forceinline__ void attend_segment(const AttendBatch& b, const int* 
     Item item = attend_item(b, pre, heads, u);
     item.g += g0;
     const AttendSeq& s = b.s[item.seq];
-    const int64_t L = attend_length(s);
-    const Reach r = attend_reach(b, s, L, item.tile, tile_rows);
+    const AttendSpan& a = b.span[item.seq];
+    const int64_t L = attend_length(a);
+    const Reach r = attend_reach(b, a, L, item.tile, tile_rows);
     x->first = item.first;
     x->units = item.units;
     x->n = min(end - u, item.units - (u - item.first));
     x->begin = r.lo + (int64_t)(u - item.first) * kUnit;
-    x->at = L - s.m - x->begin;
+    x->at = L - a.m - x->begin;
     const int64_t len = min(r.hi - x->begin, (int64_t)x->n * kUnit);
     x->len = (int)len;
     x->all_to = (int)max((int64_t)0, min(r.all_to_here - x->begin, len));
@@ -178,7 +182,7 @@ __device__ __forceinline__ void attend_segment(const AttendBatch& b, const int* 
     x->seq = item.seq;
     x->g = item.g;
     x->row0 = item.tile * tile_rows;
-    x->rows = min(tile_rows, s.m * b.G - x->row0);
+    x->rows = min(tile_rows, a.m * b.G - x->row0);
     const int64_t head = (int64_t)item.g * s.kv.s_head;
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {
@@ -294,43 +298,49 @@ __device__ __forceinline__ void attend_write(const AttendBatch& b, const AttendS
         s.lse[(int64_t)r * b.n_q_heads + h] = l == 0.f ? -INFINITY : (M + log2f(l)) * 0.6931471805599453f;
 }
 
-// Four elements of a query row from the parts that runs b0 .. b1 left of its item, in that order, eight at a
-// time.  Run k is that of block k * wide + of.
+// Adds a part's four elements and its sum, times f.
+__device__ __forceinline__ void add_part(float4& y, float& l, const float4& v, float f, float sum) {
+    y.x = fmaf(v.x, f, y.x); y.y = fmaf(v.y, f, y.y); y.z = fmaf(v.z, f, y.z); y.w = fmaf(v.w, f, y.w);
+    l = fmaf(sum, f, l);
+}
+
+// Four elements of a row from n parts, in order, eight at a time: parts are slots slot0 + skip, slot0 + step,
+// slot0 + 2 step ...
+struct Joined {
+    float4 y;
+    float M, l;
+};
 template <int D>
-__device__ __forceinline__ void attend_join_row(const AttendBatch& b, const AttendSeq& s, int g, int row, int r, int d,
-                                                int tile_rows, int first, const Runs& runs, int b0, int b1, int wide, int of) {
-    const int second = attend_run(runs, b0) == first ? 0 : 1;       // of the first run's two slots
-    float M = -INFINITY, l = 0.f;
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k0 = b0; k0 <= b1; k0 += 8) {
+__device__ __forceinline__ Joined attend_join_row(const AttendBatch& b, int64_t slot0, int skip, int step, int n, int tile_rows,
+                                                  int r, int d) {
+    Joined j{make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
+#pragma unroll 1
+    for (int k0 = 0; k0 < n; k0 += 8) {
         float2 x[8];
         float4 v[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int k = k0 + i;
-            const int64_t at = (int64_t)(2 * (k * wide + of) + (k == b0 ? second : 0)) * tile_rows + r;
+            const int64_t at = (slot0 + (k ? k * step : skip)) * tile_rows + r;
             x[i] = make_float2(-INFINITY, 0.f);
             v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (k <= b1) {
+            if (k < n) {
                 x[i] = __ldcg(b.part_ml + at);
                 v[i] = __ldcg(reinterpret_cast<const float4*>(b.part + at * D + d));
             }
         }
-        float top = M;
+        float top = j.M;
 #pragma unroll
         for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i].x);
-        const float f = M == -INFINITY ? 0.f : exp2f(M - top);
-        y.x *= f; y.y *= f; y.z *= f; y.w *= f;
-        l *= f;
-        M = top;
+        const float f = j.M == -INFINITY ? 0.f : exp2f(j.M - top);
+        j.y.x *= f; j.y.y *= f; j.y.z *= f; j.y.w *= f;
+        j.l *= f;
+        j.M = top;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float f = x[i].x == -INFINITY ? 0.f : exp2f(x[i].x - M);
-            l = fmaf(x[i].y, f, l);
-            y.x = fmaf(v[i].x, f, y.x); y.y = fmaf(v[i].y, f, y.y); y.z = fmaf(v[i].z, f, y.z); y.w = fmaf(v[i].w, f, y.w);
-        }
+        for (int i = 0; i < 8; ++i)
+            add_part(j.y, j.l, v[i], x[i].x == -INFINITY ? 0.f : exp2f(x[i].x - j.M), x[i].y);
     }
-    attend_write<D>(b, s, g, row, d, y, M, l);
+    return j;
 }
 
 // Host side, shared by the launchers: row tiles of every sequence, and the most units there can be.

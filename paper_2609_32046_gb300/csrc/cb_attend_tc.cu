@@ -657,12 +657,13 @@ __global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ Att
     const Item item = attend_item(b, pre, b.n_kv_heads, u);
     const int b0 = attend_block(runs, item.first), b1 = attend_block(runs, item.first + item.units - 1);
     if (b0 == b1 || (!by_item && (item.first == u || b0 != (int)blockIdx.x))) return;
-    const AttendSeq& s = b.s[item.seq];
-    const int row0 = item.tile * tile_rows, rows = min(tile_rows, s.m * b.G - row0);
+    const int row0 = item.tile * tile_rows, rows = min(tile_rows, b.span[item.seq].m * b.G - row0);
     const int e = blockIdx.y * 256 + threadIdx.x;
-    if (e < rows * (D / 4))
-        attend_join_row<D>(b, s, item.g, row0 + e / (D / 4), e / (D / 4), (e % (D / 4)) * 4, tile_rows, item.first, runs,
-                           b0, b1, 1, 0);
+    if (e >= rows * (D / 4)) return;
+    const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+    const int skip = attend_run(runs, b0) == item.first ? 0 : 1;     // of the first run's two slots
+    const Joined j = attend_join_row<D>(b, 2 * b0, skip, 2, b1 - b0 + 1, tile_rows, r, d);
+    attend_write<D>(b, b.s[item.seq], item.g, row0 + r, d, j.y, j.M, j.l);
 }
 
 template <int D>
@@ -693,7 +694,7 @@ cudaError_t launch(const AttendBatch& b, int blocks, int tile_rows, cudaStream_t
 
 cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
     int m = 0;
-    for (int i = 0; i < b.n; ++i) m = b.s[i].m > m ? b.s[i].m : m;
+    for (int i = 0; i < b.n; ++i) m = b.span[i].m > m ? b.span[i].m : m;
     const int tile_rows = m * b.G <= kTile ? kTile : 2 * kTile;
     const int64_t units = attend_pairs(b, tile_rows);
     const int blocks = (int)(units < num_sms ? units : num_sms);

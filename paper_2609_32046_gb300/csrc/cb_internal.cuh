@@ -272,12 +272,16 @@ struct PackBatch {
 // One sequence of cb_attend.
 struct AttendSeq {
     PackedRows kv;            // bases at the call's layer
-    int64_t T;
-    const int32_t* length;    // or null
     const uint16_t* q;
     uint16_t* out;
     float* lse;
     int64_t s_tok, s_head, o_tok, o_head;
+};
+
+// What decides a sequence's share of the work, apart from the rest: every block reads it of all sequences.
+struct AttendSpan {
+    int64_t T;
+    const int32_t* length;    // or null
     int32_t m;
     int32_t pair0;            // row tiles of the sequences before
 };
@@ -291,9 +295,10 @@ struct AttendBatch {
     uint32_t* err;
     float* part;              // partial outputs [slot][rows of a tile][d]
     float2* part_ml;          // their (maximum, sum) [slot][rows of a tile]
-    int32_t* tickets;         // one a block of k_attend_few, zero between calls
+    int32_t* tickets;         // kFewTickets a block of k_attend_few, zero between calls
     int32_t pairs;            // row tiles of all sequences
     uint64_t wait_ns;
+    AttendSpan span[kMaxBatch];
     AttendSeq s[kMaxBatch];
 };
 
@@ -304,7 +309,8 @@ cudaError_t launch_unpack(const PackBatch& b, int head_dim, cudaStream_t st, int
 cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms);
 // Query rows of partial results that launch_attend may use on num_sms SMs.
 int64_t attend_part_rows(int num_sms);
-constexpr int kFewBlocksPerSm = 4;   // blocks of k_attend_few an SM holds, and tickets a context has for each
+constexpr int kFewBlocksPerSm = 4;   // blocks of k_attend_few an SM holds at most
+constexpr int kFewTickets = 3;       // tickets for each: groups of parts that begin in it (two), items that do
 
 // Records the message cb_last_error(NULL) returns (entry points without a context).
 void set_context_free_error(const char* msg);

@@ -401,14 +401,14 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
                 s.kv.code[x] += layer * s.kv.s_layer * (d / 2);
                 s.kv.scale[x] += layer * s.kv.s_layer * (d / 32);
             }
-            s.T = p.T;
-            s.length = p.length;
+            b.span[k].T = p.T;
+            b.span[k].length = p.length;
+            b.span[k].m = q.m;
             s.q = static_cast<const uint16_t*>(q.q);
             s.out = static_cast<uint16_t*>(q.out);
             s.lse = q.lse;
             s.s_tok = q.s_tok; s.s_head = q.s_head;
             s.o_tok = q.o_tok; s.o_head = q.o_head;
-            s.m = q.m;
         }
         const cudaError_t e = launch_attend(b, d, strm, ctx->num_sms);
         if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "attend launch failed: %s", cudaGetErrorString(e));
