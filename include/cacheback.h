@@ -473,7 +473,8 @@ typedef struct {
  *             s_layer counts from the first layer of the call
  *   idx       device int32 [count[i]], 4-byte aligned; idx or idx[i] NULL: rows 0 .. count[i] - 1
  *   rows      device int32 [count[i]], 4-byte aligned; rows or rows[i] NULL: offset[i] + j, which has
- *             to lie within caches[i].T.  Of equal entries one row stays, which one is not defined.
+ *             to lie within caches[i].T.  No row of a cache may be written twice by one call: what
+ *             stays in it is then a mixture of codes and scales of the two (other rows are not touched)
  *   layer, n_layers   layers of the cache that the call writes: a whole message, or one layer of a
  *             forward pass
  * An idx or rows entry out of range skips its row and is reported by cb_sync_status as CB_EDEVICE.

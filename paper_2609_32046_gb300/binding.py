@@ -306,8 +306,8 @@ class PackedKV:
         paged = pages is not None
         dims = 5 if paged else 4
         _require(all(x.dim() == dims for x in (k, v, k_scale, v_scale)), "codes and scales need %d dimensions" % dims)
-        _require(k.element_size() == v.element_size() == 1 and k_scale.element_size() == v_scale.element_size() == 2,
-                 "codes are bytes and scales 16-bit numbers")
+        _require(k.element_size() == v.element_size() == 1 and _is_bf16(k_scale) and _is_bf16(v_scale),
+                 "codes are bytes and scales bf16")
         _require(k.shape == v.shape and k_scale.shape == v_scale.shape and k.shape[:-1] == k_scale.shape[:-1] and
                  k.shape[-1] == 16 * k_scale.shape[-1], "codes hold d / 2 and scales d / 32 elements of the same rows")
         kd, sd = k.shape[-1], k_scale.shape[-1]
@@ -323,7 +323,7 @@ class PackedKV:
         if paged:
             self.page_size, self.n_pages = k.shape[2], k.shape[1]
             _require(self.page_size & (self.page_size - 1) == 0, "page_size must be a power of two")
-            _require(pages.element_size() == 4 and pages.dim() == 1 and pages.is_contiguous(), "pages are a row of int32")
+            _require(_is_int32(pages) and pages.dim() == 1 and pages.is_contiguous(), "pages are a row of int32")
             self.n_layers, self.n_kv_heads = k.shape[0], k.shape[3]
             self.capacity = pages.numel() * self.page_size
             order = (0, 3, 2)
@@ -339,8 +339,7 @@ class PackedKV:
         self._desc = d
         self.length = length
         self._shape = (self.n_layers, self.n_kv_heads, self.head_dim)
-        self.T = self.capacity if T is None else int(T)
-        _require(0 <= self.T <= self.capacity, "T = %d not in [0, %d]" % (self.T, self.capacity))
+        self.T = self.capacity if T is None else T
 
     @classmethod
     def empty(cls, n_layers: int, n_kv_heads: int, T: int, head_dim: int, device=None) -> "PackedKV":
@@ -356,17 +355,26 @@ class PackedKV:
         return 2 * self.n_layers * self.n_kv_heads * self.T * (self.head_dim // 2 + self.head_dim // 16)
 
     @property
+    def T(self) -> int:
+        return self._T
+
+    @T.setter
+    def T(self, T: int):
+        _require(0 <= T <= self.capacity, "T = %d not in [0, %d]" % (T, self.capacity))
+        self._T = int(T)
+
+    @property
     def length(self):
         return self._length
 
     @length.setter
     def length(self, x):
-        _require(x is None or (x.element_size() == 4 and x.numel() == 1), "length is one int32")
+        _require(x is None or (_is_int32(x) and x.numel() == 1), "length is one int32")
         self._length = x
         self._desc.length = None if x is None else x.data_ptr()
 
     def desc(self, T: Optional[int] = None) -> cb_packed:
-        self._desc.T = self.T if T is None else T
+        self._desc.T = self._T if T is None else T
         return self._desc
 
 
@@ -392,6 +400,22 @@ class Rotary:
 def _require(ok: bool, message: str):
     if not ok:
         raise ValueError(message)
+
+
+_half = None
+
+
+def _is_bf16(x) -> bool:
+    """A tensor of 16-bit storage that does not say it holds fp16."""
+    global _half
+    if _half is None:
+        import torch
+        _half = torch.float16
+    return x.element_size() == 2 and x.dtype is not _half
+
+
+def _is_int32(x) -> bool:
+    return x.element_size() == 4 and not x.dtype.is_floating_point
 
 
 class CacheBack:
@@ -519,16 +543,18 @@ class CacheBack:
         or a list of one (or None) per set; else token r is at pos0 + r.  inverse: the transposed turn
         (the gradient of the forward one).  Returns ys."""
         n = len(xs)
+        _require(ys is None or len(ys) == n, "one y (or None) per x")
         ys = [x if y is None else y for x, y in zip(xs, ys or [None] * n)]
         pos = list(pos) if isinstance(pos, (list, tuple)) else [pos] * n
+        _require(len(pos) == n, "one pos (or None) per x")
         sets = (cb_vectors * n)()
         for i, (x, y, p) in enumerate(zip(xs, ys, pos)):
             _require(x.shape == y.shape and x.dim() in (3, 4) and x.shape[-1] == self.cfg.head_dim, "vectors are [nL][tokens][heads][d]")
-            _require(x.element_size() == y.element_size() == 2, "vectors are bf16")
+            _require(_is_bf16(x) and _is_bf16(y), "vectors are bf16")
             xt, yt = x.stride(), y.stride()
             _require(xt[-1] == yt[-1] == 1, "vectors are contiguous")
             nl, xl, yl = (x.shape[0], xt[0], yt[0]) if x.dim() == 4 else (1, 0, 0)
-            _require(p is None or (p.element_size() == 4 and p.is_contiguous() and p.numel() == x.shape[-3]), "pos holds one int32 a token")
+            _require(p is None or (_is_int32(p) and p.is_contiguous() and p.numel() == x.shape[-3]), "pos holds one int32 a token")
             sets[i] = cb_vectors(x.data_ptr(), y.data_ptr(), nl, x.shape[-2], x.shape[-3], xl, xt[-3], xt[-2], yl, yt[-3],
                                  yt[-2], None if p is None else p.data_ptr(), int(pos0))
         self._check(self.lib.cb_rotary(self.h, n, sets, ctypes.byref(rope.desc(inverse)),
@@ -544,8 +570,12 @@ class CacheBack:
         n = len(Ks)
         idx, rows = idx or [None] * n, rows or [None] * n
         counts = counts or [int(K.shape[2]) if x is None else int(x.numel()) for K, x in zip(Ks, idx)]
-        for K, x, r, c, p in zip(Ks, idx, rows, counts, caches):
-            _require(all(t is None or (t.element_size() == 4 and t.is_contiguous() and t.numel() >= c) for t in (x, r)), "idx and rows hold an int32 a row")
+        _require(n > 0 and all(len(x) == n for x in (Vs, caches, idx, rows, counts, Ks if offsets is None else offsets)),
+                 "one entry per sender in every list")
+        for K, V, x, r, c, p in zip(Ks, Vs, idx, rows, counts, caches):
+            _require(all(t is None or (_is_int32(t) and t.is_contiguous() and t.numel() >= c) for t in (x, r)),
+                     "idx and rows hold an int32 a row")
+            _require(K.dtype == V.dtype and (isinstance(K, PagedKV) or (_is_bf16(K) and K.shape == V.shape)), "K and V are bf16")
             self._fits(p)
             _require(K.shape[1] == p.n_kv_heads and K.shape[3] == p.head_dim and K.shape[0] == Ks[0].shape[0], "K and V do not match the cache")
         kv = (cb_kv * n)(*[kv_desc(K, V) for K, V in zip(Ks, Vs)])
@@ -565,12 +595,13 @@ class CacheBack:
         idx = idx or [None] * n
         counts = counts or [p.T if x is None else int(x.numel()) for p, x in zip(caches, idx)]
         offsets = offsets or [sum(counts[:i]) for i in range(n)]
+        _require(len(idx) == len(counts) == len(offsets) == n, "one entry per cache in every list")
         for p, x, c in zip(caches, idx, counts):
             self._fits(p)
-            _require(x is None or (x.element_size() == 4 and x.is_contiguous() and x.numel() >= c), "idx holds an int32 a row")
+            _require(x is None or (_is_int32(x) and x.is_contiguous() and x.numel() >= c), "idx holds an int32 a row")
         ost = k_out.stride()
         _require(ost[3] == 1 and ost[2] == k_out.size(3) == self.cfg.head_dim and v_out.stride() == ost and
-                 v_out.shape == k_out.shape and k_out.element_size() == 2 and
+                 v_out.shape == k_out.shape and _is_bf16(k_out) and _is_bf16(v_out) and
                  tuple(k_out.shape[:2]) == (self.cfg.n_layers, self.cfg.n_kv_heads), "k_out, v_out are bf16 [nL][Hkv][capacity][d]")
         held = (cb_packed * n)(*[p.desc() for p in caches])
         self._check(self.lib.cb_unpack(self.h, n, held, _ptr_array([None if x is None else x.data_ptr() for x in idx]),
@@ -598,7 +629,7 @@ class CacheBack:
         for i, p in enumerate(caches):
             if p._shape != shape:
                 self._fits(p)
-            p._desc.T = p.T
+            p._desc.T = p._T
             held[i] = p._desc
             if whole:
                 q[i] = (a + 2 * i * sa, o + 2 * i * so, None if e is None else e + i * se, m, ta, ha, to, ho)
@@ -612,8 +643,8 @@ class CacheBack:
         qt, ot = Q.stride(), out.stride()
         m, heads, d = Q.shape
         _require(out.shape == Q.shape and heads == self.cfg.n_q_heads and d == self.cfg.head_dim and qt[2] == ot[2] == 1 and
-                 Q.element_size() == out.element_size() == 2, "queries and outputs are bf16 [m][Hq][d]")
-        _require(lse is None or (lse.shape == (m, heads) and lse.is_contiguous() and lse.element_size() == 4),
+                 _is_bf16(Q) and _is_bf16(out), "queries and outputs are bf16 [m][Hq][d]")
+        _require(lse is None or (lse.shape == (m, heads) and lse.is_contiguous() and lse.element_size() == 4 and lse.dtype.is_floating_point),
                  "lse is fp32 [m][Hq]")
         return (Q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), m, qt[0], qt[1], ot[0], ot[1])
 

@@ -251,3 +251,37 @@ def test_rows_past_32_bits_of_elements():
     rx.unpack([p], ko, vo, idx=[idx])
     rx.sync_status()
     assert torch.equal(vo.double().cpu(), c * s.repeat_interleave(32, -1))
+
+
+def test_a_row_written_twice_leaves_the_others_alone():
+    Hkv, T, d = 2, 40, 128
+    K, V = (_rows((1, Hkv, T, d), s).cuda() for s in (1, 2))
+    rx = _receiver(1, Hkv, d, T)
+    p = cb.PackedKV(*[torch.full((1, Hkv, T, w), 9, dtype=t, device="cuda")
+                      for w, t in ((d // 2, torch.uint8),) * 2 + ((d // 32, torch.bfloat16),) * 2])
+    rows = torch.tensor([5, 6, 5, 5, 7], dtype=torch.int32, device="cuda")
+    rx.pack([K[:, :, :5]], [V[:, :, :5]], [p], rows=[rows])
+    rx.sync_status()                             # codes and scales are well formed
+    c, s = ref.held_rows(K[:, :, [1, 4]].cpu())
+    assert torch.equal(p.k[:, :, 6:8].cpu(), ref.packed_bytes(c)) and torch.equal(p.k_scale[:, :, 6:8].cpu().double(), s)
+    assert (p.k[:, :, :5] == 9).all() and (p.k[:, :, 8:] == 9).all() and (p.v_scale[:, :, 8:] == 9).all()
+
+
+def test_lists_and_types_that_do_not_fit_are_refused():
+    K = _rows((1, 2, 32, 64), 1).cuda()
+    rx = _receiver(1, 2, 64, 32, 2)
+    p = cb.PackedKV.empty(1, 2, 32, 64, "cuda")
+    i32 = torch.zeros(4, dtype=torch.int32, device="cuda")
+    for call in (lambda: rx.pack([K, K], [K], [p, p], [0, 0]),
+                 lambda: rx.pack([K, K], [K, K], [p], [0, 0]),
+                 lambda: rx.pack([K, K], [K, K], [p, p], [0]),
+                 lambda: rx.pack([K, K], [K, K], [p, p], [0, 0], counts=[1]),
+                 lambda: rx.pack([K, K], [K, K], [p, p], [0, 0], idx=[i32]),
+                 lambda: rx.pack([K], [K[:, :, :8]], [p], [0]),
+                 lambda: rx.pack([K.half()], [K.half()], [p], [0]),
+                 lambda: rx.pack([K], [K], [p], [0], idx=[i32.float()]),
+                 lambda: rx.unpack([p, p], K, K, counts=[1, 1], offsets=[0]),
+                 lambda: rx.unpack([p], K.half(), K.half())):
+        with pytest.raises(ValueError):
+            call()
+    rx.sync_status()

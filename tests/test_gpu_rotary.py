@@ -149,3 +149,13 @@ def test_refusals():
     before = x.clone()
     rx.sync_status()
     assert torch.equal(x, before)
+
+
+def test_lists_and_types_that_do_not_fit_are_refused():
+    x = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device="cuda")
+    rx, rope = cb.Receiver(1, 2, 2, 64, 8, 64), cb.Rotary(1e4)
+    pos = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for call in (lambda: rx.rotary([x, x], rope, [x]), lambda: rx.rotary([x, x], rope, pos=[pos]),
+                 lambda: rx.rotary([x.half()], rope), lambda: rx.rotary([x], rope, pos=pos.float())):
+        with pytest.raises(ValueError):
+            call()

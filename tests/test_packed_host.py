@@ -80,3 +80,21 @@ def test_packing_in_bf16_is_exact():
     s = torch.tensor([k * 2.0 ** e for e in range(-24, 9) for k in range(16, 32)] + [2.0 ** 13])
     v = torch.arange(-7.0, 8.0)[None] * s[:, None]
     assert torch.equal(v.to(torch.bfloat16).float(), v) and torch.equal(v.to(torch.float16).float(), v)
+
+
+def test_a_cache_grows_within_its_room():
+    p = cb.PackedKV(*_arrays((1, 2, 50), 128), T=3)
+    p.T = 50
+    for bad in (51, -1):
+        with pytest.raises(ValueError):
+            p.T = bad
+    assert p.T == 50 and p.desc().T == 50
+
+
+def test_other_types_are_refused():
+    k, v, ks, vs = _arrays((1, 2, 50), 128)
+    table = torch.arange(4, dtype=torch.int32)
+    for bad in (lambda: cb.PackedKV(k, v, ks.half(), vs.half()), lambda: cb.PackedKV(k, v, ks, vs, length=torch.zeros(1)),
+                lambda: cb.PackedKV(*_arrays((1, 9, 16, 2), 128), pages=table.float())):
+        with pytest.raises(ValueError):
+            bad()
