@@ -16,6 +16,15 @@
 // half of S for D = 128, where the next S waits for the product that reads P to end.
 // O is scaled in place when a row's maximum has grown by more than 8 (log2 domain) since M was set: seldom
 // after the first tiles; until then weights are up to 2^15, in fp16's range.
+//
+// Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 286 us, 931 TFLOP/s; 64 tokens
+// over 12352 positions 40 us.  256 rows a block, because each unpacking of a tile serves all of them: with 128
+// the same 1024 tokens take 367 us.  Bound by the chain of waits of a stream (weights, their product, the next
+// scores, its maximum), by fetching the roles' code and by the shared memory that the products read: without
+// softmax and unpacking the products alone take 249 us.  Slower: two warps that issue (335 us), 16 softmax warps
+// of 72 registers (408), registers not moved between the roles and 8 + 8 + 1 warps (317), scores in two
+// halves of 64 positions (293 .. 299).
+#include <atomic>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -30,6 +39,7 @@ namespace {
 using namespace sm100;
 
 constexpr int kTile = 128;                  // positions a tile, rows a stream
+constexpr int kRowTile = 2 * kTile;         // query rows a block takes at a time
 constexpr int kWarpsAt = 20;
 constexpr int kThreadsAt = kWarpsAt * 32;
 // Registers a thread is launched with, and those of a softmax thread, of one that unpacks and of the last
@@ -162,9 +172,10 @@ __device__ __forceinline__ void copy_v(uint32_t to, const Segment& x, int lo, in
 template <int D, bool EDGE>
 __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t to, bool sums, int c0, int c1, float scale,
                                              float& M, float& l) {
-    // 32 columns at a time, the next ones on their way: first the maximum, then the weights.  (Loops of two such
-    // steps: with all four written out the roles' code overflows the instruction cache, 400 us for 322.)
-    float z[1][32];
+    // 32 columns at a time, first for the maximum, then for the weights, each read from tensor memory when its
+    // turn comes.  (Rolled up: the roles share the instruction cache.  With the four steps written out and all
+    // columns in registers, read once, 1024 tokens over 16384 positions took 353 us for 286.)
+    float z[32];
     float high = -INFINITY;
     auto seen = [&](float (&x)[32], int first) {
         if (EDGE) {
@@ -175,10 +186,10 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
     };
 #pragma unroll 1
     for (int c = 0; c < kTile; c += 32) {
-        tmem_ld32(ts + c, z[0]);
-        tmem_wait_ld(z[0]);
-        seen(z[0], c);
-        high = fmaxf(high, max_tree1(z[0]));
+        tmem_ld32(ts + c, z);
+        tmem_wait_ld(z);
+        seen(z, c);
+        high = fmaxf(high, max_tree1(z));
     }
     const float top = high * scale;
     const bool grow = top > M + kGrow || (M == -INFINITY && top > -INFINITY);
@@ -191,7 +202,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
             for (int c = 0; c < D; c += 8) {                 // (few registers: seldom run)
                 float o[8];
                 tmem_ld8(to + c, o);
-                tmem_wait_ld(o);                             // (and for the columns on their way)
+                tmem_wait_ld(o);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) o[k] *= f;
                 tmem_st8(to + c, o);
@@ -218,10 +229,10 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
     };
 #pragma unroll 1
     for (int c = 0; c < kTile; c += 32) {
-        tmem_ld32(ts + c, z[0]);
-        tmem_wait_ld(z[0]);
-        seen(z[0], c);
-        weigh(z[0], c);
+        tmem_ld32(ts + c, z);
+        tmem_wait_ld(z);
+        seen(z, c);
+        weigh(z, c);
     }
     float a, e;
     unpack2(fadd2(l0, l1), a, e);
@@ -229,7 +240,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
 }
 
 template <int D>
-__global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_constant__ AttendBatch b, int tile_rows) {
+__global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_constant__ AttendBatch b) {
     constexpr int kOp = kTile * D * 2;              // bytes of an operand tile
     constexpr bool kOver = D == 128;                // P in S's columns
     extern __shared__ uint8_t raw[];
@@ -242,7 +253,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
     uint8_t* raw_rows = sv + kStages * kOp;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-    attend_units(b, tile_rows, pre);
+    attend_units(b, kRowTile, pre);
     if (threadIdx.x == 0) {
         const Runs runs = attend_runs(pre[b.pairs] * b.n_kv_heads, gridDim.x);
         const int at = min((int)blockIdx.x, runs.blocks);            // (blocks without a unit have an empty run)
@@ -319,7 +330,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
         regs_down<kRegsIssue>();
         while (true) {
             if (threadIdx.x == 17 * 32 && ctl->unit < ctl->run1)
-                attend_segment(b, pre, b.n_kv_heads, 0, ctl->unit, ctl->run1, D, tile_rows, &seg);
+                attend_segment(b, pre, b.n_kv_heads, 0, ctl->unit, ctl->run1, D, kRowTile, &seg);
             __syncwarp();
             if (!begin()) break;
             SEGMENT();
@@ -594,7 +605,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
                     f1 = x.x == -INFINITY ? 0.f : exp2f(x.x - mm);
                     ll = l * f0 + x.y * f1;
                 }
-                    const bool whole = seg.n == seg.units;
+                const bool whole = seg.n == seg.units;
                 const int64_t slot = 2 * (int64_t)blockIdx.x + (ctl->unit == ctl->run0 ? 0 : 1);
                 // 32 columns at a time through shared memory, so that eight lanes write a row's 128 bytes
                 float* stage = reinterpret_cast<float*>(sq + kTile * (D + 4) * 4 + 1024) + warp * 32 * 36;
@@ -624,11 +635,11 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
                         const float my = __shfl_sync(0xFFFFFFFFu, mm, at), ly = __shfl_sync(0xFFFFFFFFu, ll, at);
                         if (rr >= seg.rows) continue;
                         if (whole) attend_write<D>(b, s, seg.g, seg.row0 + rr, d, y, my, ly);
-                        else *reinterpret_cast<float4*>(b.part + (slot * tile_rows + rr) * D + d) = y;
+                        else *reinterpret_cast<float4*>(b.part + (slot * kRowTile + rr) * D + d) = y;
                     }
                     __syncwarp();
                 }
-                if (!whole && r < seg.rows) b.part_ml[slot * tile_rows + r] = make_float2(mm, ll);
+                if (!whole && r < seg.rows) b.part_ml[slot * kRowTile + r] = make_float2(mm, ll);
             }
             finish(n_tiles, items);
         }
@@ -642,9 +653,9 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
 // than cuts, else at the end of run x, and joins the item there if that end is the first in it.  A thread takes
 // four elements of a row.
 template <int D>
-__global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ AttendBatch b, int tile_rows, int grid, int by_item) {
+__global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ AttendBatch b, int grid, int by_item) {
     extern __shared__ int pre[];
-    attend_units(b, tile_rows, pre);
+    attend_units(b, kRowTile, pre);
     const Runs runs = attend_runs(pre[b.pairs] * b.n_kv_heads, grid);
     int u;
     if (by_item) {
@@ -657,18 +668,18 @@ __global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ Att
     const Item item = attend_item(b, pre, b.n_kv_heads, u);
     const int b0 = attend_block(runs, item.first), b1 = attend_block(runs, item.first + item.units - 1);
     if (b0 == b1 || (!by_item && (item.first == u || b0 != (int)blockIdx.x))) return;
-    const int row0 = item.tile * tile_rows, rows = min(tile_rows, b.span[item.seq].m * b.G - row0);
+    const int row0 = item.tile * kRowTile, rows = min(kRowTile, b.span[item.seq].m * b.G - row0);
     const int e = blockIdx.y * 256 + threadIdx.x;
     if (e >= rows * (D / 4)) return;
     const int r = e / (D / 4), d = (e % (D / 4)) * 4;
     const int skip = attend_run(runs, b0) == item.first ? 0 : 1;     // of the first run's two slots
-    const Joined j = attend_join_row<D>(b, 2 * b0, skip, 2, b1 - b0 + 1, tile_rows, r, d);
+    const Joined j = attend_join_row<D>(b, 2 * b0, skip, 2, b1 - b0 + 1, kRowTile, r, d);
     attend_write<D>(b, b.s[item.seq], item.g, row0 + r, d, j.y, j.M, j.l);
 }
 
 template <int D>
-cudaError_t launch(const AttendBatch& b, int blocks, int tile_rows, cudaStream_t st) {
-    static bool set[64] = {};             // (the attribute belongs to the device's function)
+cudaError_t launch(const AttendBatch& b, int blocks, cudaStream_t st) {
+    static std::atomic<bool> set[64];     // (the attribute belongs to the device's function)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
@@ -680,25 +691,22 @@ cudaError_t launch(const AttendBatch& b, int blocks, int tile_rows, cudaStream_t
         if (e != cudaSuccess) return e;
         if (dev < 64) set[dev] = true;
     }
-    k_attend_tc<D><<<blocks, kThreadsAt, smem_bytes<D>(), st>>>(b, tile_rows);
+    k_attend_tc<D><<<blocks, kThreadsAt, smem_bytes<D>(), st>>>(b);
     e = cudaGetLastError();
     if (e != cudaSuccess || blocks == 1) return e;
     const int64_t items = (int64_t)b.pairs * b.n_kv_heads;
     const bool by_item = items < blocks;
-    k_attend_join<D><<<dim3(by_item ? (int)items : blocks - 1, tile_rows * (D / 4) / 256), 256,
-                       (b.pairs + 1) * sizeof(int), st>>>(b, tile_rows, blocks, by_item);
+    k_attend_join<D><<<dim3(by_item ? (int)items : blocks - 1, kRowTile * (D / 4) / 256), 256,
+                       (b.pairs + 1) * sizeof(int), st>>>(b, blocks, by_item);
     return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
-    int m = 0;
-    for (int i = 0; i < b.n; ++i) m = b.span[i].m > m ? b.span[i].m : m;
-    const int tile_rows = m * b.G <= kTile ? kTile : 2 * kTile;
-    const int64_t units = attend_pairs(b, tile_rows);
+    const int64_t units = attend_pairs(b, kRowTile);
     const int blocks = (int)(units < num_sms ? units : num_sms);
-    return head_dim == 128 ? launch<128>(b, blocks, tile_rows, st) : launch<64>(b, blocks, tile_rows, st);
+    return head_dim == 128 ? launch<128>(b, blocks, st) : launch<64>(b, blocks, st);
 }
 
 }  // namespace cbk

@@ -402,3 +402,78 @@ def test_refusals():
         rx.attend([p], [q[:, :4]], [o[:, :4]])
     rx.sync_status()
     assert torch.equal(o, before)
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 4, 1), (64, 2, 2), (128, 16, 4)])
+@pytest.mark.parametrize("m", [1, 4])
+def test_items_of_many_parts(d, Hq, Hkv, m):
+    """Long caches for few heads beside short ones: parts of one item are joined in groups, then the groups."""
+    c = Case(d, Hq, Hkv, [m, m, 1, m], [30001, 300, 0, 12000], page=64)
+    for _ in range(2):                           # (the second call finds the tickets as the first did)
+        for o in c.out:
+            o.fill_(7)
+        c.run()
+        c.check()
+    c.run(window=5000)
+    c.check(window=5000)
+
+
+@pytest.mark.parametrize("m", [2, 40])
+def test_two_contexts_at_once(m):
+    """Each with its own stream and scratch, over the same caches."""
+    a = Case(128, 8, 2, [m, m], [9000, 700])
+    b = Case(128, 8, 2, [m, m], [9000, 700])
+    a.run()
+    a.check()
+    want = [x.clone() for x in a.out]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    b.q, b.caches = a.q, a.caches
+    for _ in range(20):
+        a.run(stream=streams[0])
+        b.run(stream=streams[1])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) and torch.equal(x, z) for x, y, z in zip(want, a.out, b.out))
+    a.rx.sync_status()
+    b.rx.sync_status()
+
+
+@pytest.mark.parametrize("m", [1, 70])
+def test_captured_graphs_share_a_context(m):
+    """Two captured calls of one context, of different shapes, replayed in turn on one stream."""
+    a = Case(128, 8, 2, [m, 1], [5000, 33])
+    b = Case(128, 8, 2, [m], [2222])
+    b.rx = a.rx
+    graphs = []
+    for c in (a, b):
+        c.run()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.run()
+        graphs.append(g)
+    for c in (a, b):
+        for o in c.out:
+            o.fill_(7)
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+    a.check()
+    b.check()
+
+
+def test_more_heads_than_blocks():
+    """KV heads that outnumber the blocks an SM count allows: each takes its whole run."""
+    for m in (1, 20):
+        c = Case(64, 700, 700, [m], [200])
+        c.run()
+        c.check()
+
+
+def test_lists_and_types_that_do_not_fit_are_refused():
+    c = Case(128, 8, 2, [4], [64])
+    for call in (lambda: c.rx.attend(c.caches, c.q * 2, c.out), lambda: c.rx.attend(c.caches, [c.q[0].half()], c.out),
+                 lambda: c.rx.attend(c.caches, c.q, [c.out[0].half()]),
+                 lambda: c.rx.attend(c.caches, c.q, c.out, lses=[c.lse[0].int()])):
+        with pytest.raises(ValueError):
+            call()
