@@ -17,7 +17,7 @@ namespace cbk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
+constexpr int kUnroll = 3;          // vectors a thread has in flight
 constexpr int kMaxTokens = 8;       // tokens a block takes at a time
 
 __device__ __forceinline__ float lo_f(uint32_t w) { return __uint_as_float(w << 16); }
@@ -28,11 +28,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
-// Tokens a block takes at a time: enough vectors (layer, head) for four a thread.
+// Tokens a block takes at a time: enough vectors (layer, head) for kUnroll a thread.
 __host__ __device__ __forceinline__ int tokens_at_once(int rows, int lanes) {
     const int n = (kUnroll * lanes + rows - 1) / rows;
     return n < 1 ? 1 : n < kMaxTokens ? n : kMaxTokens;
 }
+
+// Where two pairs' numbers stand: the same place of eight units in eight different banks.
+__device__ __forceinline__ int place(int q) { return q ^ ((q >> 3) & 3); }
 
 // A unit is 16 elements of a vector, two 16-byte pieces: 8 pairs (8u .. 8u + 7) of the rotary part, whose
 // halves are dims / 2 apart (STYLE 0) or which lie side by side (STYLE 1), or 16 elements behind it.
@@ -40,13 +43,15 @@ __host__ __device__ __forceinline__ int tokens_at_once(int rows, int lanes) {
 // thread, and D / 16 units of 256 / (D / 16) vectors in turn read them there.  (With every thread working out
 // the eight of its unit, 24 vectors a token left the special-function unit more to do than memory: 6001
 // tokens x 8 layers x 24 heads, d = 64, 91 us.)
-// Bound by HBM: those 295 MB now take 52 us, 5.7 TB/s; 16384 tokens x 4 layers x 40
-// heads of 128, 1.3 GB, 204 us, 6.6 TB/s; 47 MB of a short question 14 us, of which starting and ending a kernel of one wave takes half.
+// Bound by HBM: those 295 MB now take 48 us, 6.1 TB/s; 16384 tokens x 4 layers x 40 heads of 128, 1.3 GB, 195 us, 6.9 TB/s;
+// the 47 MB of a short question 10.7 us, 4.4 TB/s, of which starting and ending a kernel of three waves take a part.
+// Three vectors a thread and four blocks an SM: two and five take 10.3, 51 and 194 us, two and six 11.4, 54 and 212,
+// four and three 12.1, 51 and 197.
 // Grid: x = token group (and slice of its vectors, innermost), y = set.
 template <int D, int STYLE>
-__global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ RotaryBatch b, int slices) {
+__global__ void __launch_bounds__(kThreads, 4) k_rotary(const __grid_constant__ RotaryBatch b, int slices) {
     constexpr int U = D / 16, LANES = kThreads / U;
-    __shared__ __align__(16) float2 turn_of[2][kMaxTokens][D / 2];       // cosine, sine
+    __shared__ float4 turn_of[2][kMaxTokens][D / 4];     // cosine, sine of two pairs, at place()
     const RotarySet& s = b.s[blockIdx.y];
     const int u = threadIdx.x % U;
     const bool turn = u * 16 < b.dims;
@@ -60,21 +65,12 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
     for (int64_t t0 = (int64_t)(blockIdx.x / (unsigned)slices) * many; t0 < s.n_tokens;
          t0 += (int64_t)(gridDim.x / (unsigned)slices) * many, buffer ^= 1) {
         const int n = (int)min((int64_t)many, s.n_tokens - t0);
-        for (int i = threadIdx.x; i < n * pairs; i += kThreads) {
-            const int t = i / pairs, k = i - t * pairs;
-            const int64_t pos = s.pos ? (int64_t)__ldg(s.pos + t0 + t) : s.pos0 + t0 + t;
-            const uint64_t turns = (uint64_t)pos * b.turns[k];
-            const float a = (float)(int32_t)(uint32_t)(turns >> 32) * 1.4629180792671596e-09f;   // 2 pi / 2^32
-            turn_of[buffer][t][k] = make_float2(__cosf(a) * b.gain, __sinf(a) * b.sine_gain);
-        }
-        __syncthreads();      // (a buffer is written again two turns later, behind the next turn's barrier)
-        if (idle) continue;
         const int first = (int)(blockIdx.x % (unsigned)slices) * LANES + threadIdx.x / U;
-        int t = first / rows, l = first % rows / H, h = first % rows % H;
-        while (t < n) {
-            uint4 va[kUnroll], vb[kUnroll];
-            uint16_t* out[kUnroll];
-            int at[kUnroll];
+        int t = idle ? n : first / rows, l = first % rows / H, h = first % rows % H;
+        uint4 va[kUnroll], vb[kUnroll];
+        uint16_t* out[kUnroll];
+        int at[kUnroll];
+        auto load = [&]() {
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
                 at[i] = -1;
@@ -92,11 +88,24 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
                 if (h >= H) { h -= H; ++l; }
                 if (l >= NL) { l -= NL; ++t; }
             }
+        };
+        load();               // (the first vectors are on their way while the sines are worked out)
+        for (int i = threadIdx.x; i < n * pairs; i += kThreads) {
+            const int t = i / pairs, k = i - t * pairs;
+            const int64_t pos = s.pos ? (int64_t)__ldg(s.pos + t0 + t) : s.pos0 + t0 + t;
+            const uint64_t turns = (uint64_t)pos * b.turns[k];
+            const float a = (float)(int32_t)(uint32_t)(turns >> 32) * 1.4629180792671596e-09f;   // 2 pi / 2^32
+            reinterpret_cast<float2*>(&turn_of[buffer][t][place(k / 2)])[k % 2] = make_float2(__cosf(a) * b.gain, __sinf(a) * b.sine_gain);
+        }
+        __syncthreads();      // (a buffer is written again two turns later, behind the next turn's barrier)
+        while (at[0] >= 0) {
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
                 if (at[i] < 0) continue;
                 if (turn) {
-                    const float4* f = reinterpret_cast<const float4*>(&turn_of[buffer][at[i]][u * 8]);
+                    float4 f[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = turn_of[buffer][at[i]][place(4 * u + j)];
                     uint32_t a[4] = {va[i].x, va[i].y, va[i].z, va[i].w}, w[4] = {vb[i].x, vb[i].y, vb[i].z, vb[i].w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
@@ -119,6 +128,7 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
                 __stcs(reinterpret_cast<uint4*>(out[i] + e0), va[i]);
                 __stcs(reinterpret_cast<uint4*>(out[i] + e1), vb[i]);
             }
+            load();
         }
     }
 }
