@@ -6,9 +6,11 @@
 // c has 3 bits, so c * s has 8: a bf16 number exactly, and an fp16 number in that range of s.
 //
 // Both are exact in 32-bit arithmetic.  max|x| and 7 s have 8 significant bits, so the quotient
-// max|x| / 7 is a number of 5 bits or at least 2^-8 of itself away from one.  x / s is a whole number
-// and a half, or 2^-12 away from one: the product with 1 / s rounded up lies on the right side, and
-// where it is a whole number and a half it is not below.
+// max|x| / 7 is a number of 5 bits or at least 2^-8 of itself away from one: the product with 1 / 7, both
+// rounded down and off by less than 2^-21, is rounded up to the same number.  x / s is a whole number
+// and a half, or 2^-12 away from one: the product with a number between 1 / s and (1 + 2^-19) / s lies on
+// the right side, and where x / s is a whole number and a half it is not below.  (The reciprocal
+// approximation's error is below 2^-22: times 1 + 2^-21 it is such a number.)
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -21,6 +23,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kRows = 4;                 // rows a thread has in flight
+constexpr float kSeventh = 0.142857134342193603515625f;   // the fp32 number below 1 / 7
 constexpr uint32_t kLargest = 0x4760u;   // 7 * 2^13 as bf16
 
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
@@ -71,24 +74,25 @@ __device__ __forceinline__ uint32_t code_word(const uint32_t (&w)[4], float r) {
     return (m ^ (n * 7u)) + (0x88888888u - n * 7u);
 }
 
-// Rows of a block's tile: where each comes from and goes to (elements or rows from the segment's base on, -1
-// where it is not to be moved).  One thread a row looks up the index, the block tables and the bounds; the 8 or 16
-// threads that move it read the result.
-template <int D, bool PACK>
-__device__ __forceinline__ longlong2 look_up(const PackBatch& bt, const PackSender& sd, int64_t j) {
-    longlong2 r = make_longlong2(-1, -1);
+// Rows of a block's tile.  One thread a row looks up the index, the block tables and the bounds; the 8 or 16 threads
+// that move it read the result.
+constexpr uint32_t kNone = 0xFFFFFFFFu;
+
+// Where row j of a sender comes from (elements from the segment's base on) and goes to (its row in the cache, which
+// are below 2^31; kNone: it does not).
+struct __align__(16) PackRow {
+    int64_t from;
+    uint32_t to;
+};
+__device__ __forceinline__ PackRow pack_row(const PackBatch& bt, const PackSender& sd, int64_t j) {
+    PackRow r{0, kNone};
     if (j >= sd.count) return r;
     const int64_t t = sd.idx ? (int64_t)__ldg(sd.idx + j) : j;
+    const int64_t at = sd.rows ? (int64_t)__ldg(sd.rows + j) : sd.dst_off + j;
     if (t < 0 || t >= sd.T) {
         atomicOr(bt.err, kErrCompactIndex);
         return r;
     }
-    if (!PACK) {
-        const int64_t from = packed_row(sd.held, t);
-        if (from < 0) atomicOr(bt.err, kErrPageIndex);
-        return make_longlong2(from, j);          // (a row of a bad page is restored as zeros)
-    }
-    const int64_t at = sd.rows ? (int64_t)__ldg(sd.rows + j) : sd.dst_off + j;
     if (at < 0 || at >= sd.dst_T) {
         atomicOr(bt.err, kErrPackRow);
         return r;
@@ -98,20 +102,35 @@ __device__ __forceinline__ longlong2 look_up(const PackBatch& bt, const PackSend
         atomicOr(bt.err, kErrPageIndex);
         return r;
     }
-    return make_longlong2(from, to);
+    r.from = from;
+    r.to = (uint32_t)to;
+    return r;
+}
+
+// The row of the cache that row j of the output comes from, and j; kNone: zeros, and nothing to restore.
+__device__ __forceinline__ uint2 unpack_row(const PackBatch& bt, const PackSender& sd, int64_t j) {
+    if (j >= sd.count) return make_uint2(kNone, kNone);
+    const int64_t t = sd.idx ? (int64_t)__ldg(sd.idx + j) : j;
+    if (t < 0 || t >= sd.T) {
+        atomicOr(bt.err, kErrCompactIndex);
+        return make_uint2(kNone, kNone);
+    }
+    const int64_t from = packed_row(sd.held, t);
+    if (from < 0) atomicOr(bt.err, kErrPageIndex);
+    return make_uint2(from < 0 ? kNone : (uint32_t)from, (uint32_t)j);
 }
 
 // Grid: x = (K or V, layer, head) segment, y = sender, z = slice of the segment's rows.
 // A thread takes 8 elements (16 bytes) of four rows of a tile; the four threads of a group each work out the
 // scale of one of the four rows and hand it round, two rows' largest values to a word.
-// Bound by instructions more than by its bytes (2 read and 9/16 written an element): 2048 of 8192
-// positions of 36 layers x 8 heads of 128 take 78 us, 4.9 TB/s; with every thread looking up its own rows and two
-// exchanges a row it was 116 us.
+// Bound by instructions and by its bytes (2 read and 9/16 written an element) alike: 2048 of 8192 positions of 36 layers x
+// 8 heads of 128 take 72 us, 5.3 TB/s; with every thread looking up its own rows and two exchanges a row it was 116.
+// Five blocks an SM: four take 75 us, six 79.
 template <int D>
-__global__ void __launch_bounds__(kThreads) k_pack(const __grid_constant__ PackBatch bt) {
+__global__ void __launch_bounds__(kThreads, 5) k_pack(const __grid_constant__ PackBatch bt) {
     constexpr int CH = D / 8;              // threads a row
     constexpr int ROWS = kThreads / CH, TILE = ROWS * kRows;
-    __shared__ longlong2 where[2][TILE];
+    __shared__ PackRow where[2][TILE];
     const PackSender& sd = bt.s[blockIdx.y];
     const int seg = blockIdx.x;
     const int g = seg % bt.n_kv_heads;
@@ -124,23 +143,23 @@ __global__ void __launch_bounds__(kThreads) k_pack(const __grid_constant__ PackB
     uint16_t* scale = sd.held.scale[kv] + base * (D / 32) + ch / 4;
     int buffer = 0;
     int64_t jb = (int64_t)blockIdx.z * TILE;
-    if (threadIdx.x < TILE) where[0][threadIdx.x] = look_up<D, true>(bt, sd, jb + threadIdx.x);
+    if (threadIdx.x < TILE) where[0][threadIdx.x] = pack_row(bt, sd, jb + threadIdx.x);
     for (; jb < sd.count; jb += (int64_t)gridDim.z * TILE, buffer ^= 1) {
         __syncthreads();
         uint32_t w[kRows][4];
-        int64_t to[kRows];
+        uint32_t to[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const longlong2 r = where[buffer][u * ROWS + threadIdx.x / CH];
-            to[u] = r.y;
+            const PackRow r = where[buffer][u * ROWS + threadIdx.x / CH];
+            to[u] = r.to;
             w[u][0] = w[u][1] = w[u][2] = w[u][3] = 0;
-            if (r.y < 0) continue;
-            const uint4 v = ld_stream(reinterpret_cast<const uint4*>(src + r.x));
+            if (r.to == kNone) continue;
+            const uint4 v = ld_stream(reinterpret_cast<const uint4*>(src + r.from));
             w[u][0] = v.x; w[u][1] = v.y; w[u][2] = v.z; w[u][3] = v.w;
         }
         // the next tile's rows while these are on their way
         if (threadIdx.x < TILE)
-            where[buffer ^ 1][threadIdx.x] = look_up<D, true>(bt, sd, jb + (int64_t)gridDim.z * TILE + threadIdx.x);
+            where[buffer ^ 1][threadIdx.x] = pack_row(bt, sd, jb + (int64_t)gridDim.z * TILE + threadIdx.x);
         uint32_t a01 = top_bits(w[0]) | (top_bits(w[1]) << 16), a23 = top_bits(w[2]) | (top_bits(w[3]) << 16);
         const uint32_t both = __vmaxu2(a01, a23);
         if (__any_sync(0xFFFFFFFFu, max(both & 0xFFFFu, both >> 16) > kLargest)) {
@@ -162,26 +181,28 @@ __global__ void __launch_bounds__(kThreads) k_pack(const __grid_constant__ PackB
         }
         const uint32_t a = mine & 2 ? a23 : a01;
         const float top = __uint_as_float(mine & 1 ? a & 0xFFFF0000u : a << 16);
-        float s = __uint_as_float((__float_as_uint(__fdiv_rn(top, 7.f)) + 0x7FFFFu) & ~0x7FFFFu);
+        float s = __uint_as_float((__float_as_uint(__fmul_rz(top, kSeventh)) + 0x7FFFFu) & ~0x7FFFFu);
         s = fminf(fmaxf(s, 9.5367431640625e-07f), 8192.f);
-        const float inv = __frcp_ru(s);
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+        inv = fmaf(inv, 4.76837158203125e-07f, inv);
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
             const float r = __shfl_sync(0xFFFFFFFFu, inv, u, 4), su = __shfl_sync(0xFFFFFFFFu, s, u, 4);
-            if (to[u] < 0) continue;
-            *reinterpret_cast<uint32_t*>(code + to[u] * (D / 2)) = code_word(w[u], r);
-            if (mine == 0) scale[to[u] * (D / 32)] = (uint16_t)(__float_as_uint(su) >> 16);
+            if (to[u] == kNone) continue;
+            *reinterpret_cast<uint32_t*>(code + (uint64_t)to[u] * (D / 2)) = code_word(w[u], r);
+            if (mine == 0) scale[(uint64_t)to[u] * (D / 32)] = (uint16_t)(__float_as_uint(su) >> 16);
         }
     }
 }
 
 // The same grid and tiles; a thread restores 8 elements of each of four rows: the same
-// 2048 positions back in 64 us, 6.0 TB/s.
+// 2048 positions back in 63 us, 6.1 TB/s (1.8 GB through pages and back: six blocks an SM 144 us, five 151).
 template <int D>
-__global__ void __launch_bounds__(kThreads) k_unpack(const __grid_constant__ PackBatch bt) {
+__global__ void __launch_bounds__(kThreads, 6) k_unpack(const __grid_constant__ PackBatch bt) {
     constexpr int CH = D / 8;
     constexpr int ROWS = kThreads / CH, TILE = ROWS * kRows;
-    __shared__ longlong2 where[2][TILE];
+    __shared__ uint2 where[2][TILE];
     const PackSender& sd = bt.s[blockIdx.y];
     const int seg = blockIdx.x;
     const int g = seg % bt.n_kv_heads;
@@ -194,33 +215,33 @@ __global__ void __launch_bounds__(kThreads) k_unpack(const __grid_constant__ Pac
     uint16_t* dst = bt.out[kv] + (int64_t)l * bt.o_layer + (int64_t)g * bt.o_head + sd.dst_off * D + ch * 8;
     int buffer = 0;
     int64_t jb = (int64_t)blockIdx.z * TILE;
-    if (threadIdx.x < TILE) where[0][threadIdx.x] = look_up<D, false>(bt, sd, jb + threadIdx.x);
+    if (threadIdx.x < TILE) where[0][threadIdx.x] = unpack_row(bt, sd, jb + threadIdx.x);
     for (; jb < sd.count; jb += (int64_t)gridDim.z * TILE, buffer ^= 1) {
         __syncthreads();
         uint32_t w[kRows], s[kRows];
-        int64_t to[kRows];
+        uint32_t to[kRows];
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            const longlong2 r = where[buffer][u * ROWS + threadIdx.x / CH];
+            const uint2 r = where[buffer][u * ROWS + threadIdx.x / CH];
             to[u] = r.y;
             w[u] = 0x88888888u;
             s[u] = 0;
-            if (r.x < 0) continue;
-            w[u] = __ldg(reinterpret_cast<const uint32_t*>(code + r.x * (D / 2)));
-            s[u] = __ldg(scale + r.x * (D / 32));
+            if (r.x == kNone) continue;
+            w[u] = __ldg(reinterpret_cast<const uint32_t*>(code + (uint64_t)r.x * (D / 2)));
+            s[u] = __ldg(scale + (uint64_t)r.x * (D / 32));
         }
         if (threadIdx.x < TILE)
-            where[buffer ^ 1][threadIdx.x] = look_up<D, false>(bt, sd, jb + (int64_t)gridDim.z * TILE + threadIdx.x);
+            where[buffer ^ 1][threadIdx.x] = unpack_row(bt, sd, jb + (int64_t)gridDim.z * TILE + threadIdx.x);
 #pragma unroll
         for (int u = 0; u < kRows; ++u) {
-            if (to[u] < 0) continue;
+            if (to[u] == kNone) continue;
             if (s[u] > kTopScaleBits) {
                 atomicOr(bt.err, kErrPackScale);
                 s[u] = 0;
             }
             uint32_t v[4];
             values_bf16(w[u], s[u] * 0x10001u, v);
-            st_stream(reinterpret_cast<uint4*>(dst + to[u] * D), make_uint4(v[0], v[1], v[2], v[3]));
+            st_stream(reinterpret_cast<uint4*>(dst + (uint64_t)to[u] * D), make_uint4(v[0], v[1], v[2], v[3]));
         }
     }
 }
