@@ -236,6 +236,7 @@ cudaError_t alloc_attend(cb_ctx* ctx, int64_t* total) {
     cudaError_t e = alloc(&ctx->attend_part, (size_t)(rows * ctx->cfg.head_dim), total);
     if (e == cudaSuccess) e = alloc(&ctx->attend_ml, (size_t)rows, total);
     const size_t n = (size_t)ctx->num_sms * cbk::kFewBlocksPerSm * cbk::kFewTickets;
+    if (e == cudaSuccess) e = alloc(&ctx->attend_cuts, (size_t)ctx->num_sms, total);
     if (e == cudaSuccess) e = alloc(&ctx->attend_tickets, n, total);
     // (on a stream of its own: the legacy stream would wait for, and spoil, another stream's capture)
     cudaStream_t st = nullptr;
@@ -266,7 +267,9 @@ cb_status attend_scratch(cb_ctx* ctx, cudaStream_t st) {
         cudaGetLastError();
         cudaFree(ctx->attend_part);
         cudaFree(ctx->attend_ml);
+        cudaFree(ctx->attend_cuts);
         cudaFree(ctx->attend_tickets);
+        ctx->attend_cuts = nullptr;
         ctx->attend_part = nullptr;
         ctx->attend_ml = nullptr;
         ctx->attend_tickets = nullptr;
@@ -429,6 +432,7 @@ void cb_destroy(cb_ctx* ctx) {
         for (uint16_t* p : ctx->old_stages) cudaFree(p);
         cudaFree(ctx->attend_part);
         cudaFree(ctx->attend_ml);
+        cudaFree(ctx->attend_cuts);
         cudaFree(ctx->attend_tickets);
         cudaFree(ctx->err);
         delete ctx->timer;

@@ -5,7 +5,7 @@
 //   0..7    softmax, four a stream (TMEM lane quarter = warp % 4): a thread is a query row
 //   8..11   K: four-bit rows from global memory, as bf16 into shared memory (K-major, 128-byte swizzle)
 //   12..15  V: the same, transposed, as fp16
-//   16      issues tcgen05.mma; 17 finds the next segment (18 and 19 fill the warp group)
+//   16      issues tcgen05.mma; 17 finds the next segment, 18 what the join has to (19 fills the warp group)
 // Two streams alternate on the tensor core, so that one's softmax runs beside the other's products: with
 // more than 128 rows a stream is a half of the rows and both take every tile; with fewer the streams take
 // alternate tiles of the same rows, each with its own maximum and sums, and join at the end.
@@ -17,13 +17,13 @@
 // O is scaled in place when a row's maximum has grown by more than 8 (log2 domain) since M was set: seldom
 // after the first tiles; until then weights are up to 2^15, in fp16's range.
 //
-// Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 286 us, 931 TFLOP/s; 64 tokens
-// over 12352 positions 40 us.  256 rows a block, because each unpacking of a tile serves all of them: with 128
-// the same 1024 tokens take 367 us.  Bound by the chain of waits of a stream (weights, their product, the next
-// scores, its maximum), by fetching the roles' code and by the shared memory that the products read: without
-// softmax and unpacking the products alone take 249 us.  Slower: two warps that issue (335 us), 16 softmax warps
-// of 72 registers (408), registers not moved between the roles and 8 + 8 + 1 warps (317), scores in two
-// halves of 64 positions (293 .. 299).
+// Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 270 us, 988 TFLOP/s, 253 of it before
+// the join; 64 tokens over 12352 positions 41 us, 34 before it. Bound by the chain of waits of a stream (weights, their
+// product, the next scores, its maximum), by fetching the roles' code and by the shared memory that the products read.
+// 256 rows a block, because each unpacking of a tile serves all of them.  Other forms, when this one (with a slower
+// join) took 286 to 292 us: 128 rows 367; two warps that issue 335; 16 softmax warps of 72 registers 408; registers not
+// moved between the roles and 8 + 8 + 1 warps 317; scores in two halves of 64 positions 293 to 299; the products alone,
+// without softmax and unpacking, 249.
 #include <atomic>
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -47,6 +47,7 @@ constexpr int kThreadsAt = kWarpsAt * 32;
 constexpr int kRegs = 96, kRegsSoftmax = 128, kRegsUnpack = 72, kRegsIssue = 72;
 static_assert(256 * kRegsSoftmax + 256 * kRegsUnpack + 128 * kRegsIssue <= kThreadsAt * kRegs, "more registers than at launch");
 constexpr int kStages = 2;
+constexpr int kJoinBlocks = 32;             // blocks that join one item
 constexpr float kBits = 7.f;                // weights are exp2(z - M'), M' = M - 7
 constexpr float kGrow = 8.f;                // growth of a row's maximum that M follows
 constexpr uint32_t kPollNs = 1000000u;
@@ -174,7 +175,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
                                              float& M, float& l) {
     // 32 columns at a time, first for the maximum, then for the weights, each read from tensor memory when its
     // turn comes.  (Rolled up: the roles share the instruction cache.  With the four steps written out and all
-    // columns in registers, read once, 1024 tokens over 16384 positions took 353 us for 286.)
+    // columns in registers, read once, 1024 tokens over 16384 positions took 353 us for 292.)
     float z[32];
     float high = -INFINITY;
     auto seen = [&](float (&x)[32], int first) {
@@ -239,6 +240,35 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
     l += a + e;
 }
 
+// Items no more than blocks: record i is item i's.  Otherwise it is that of the item that goes on behind the run of
+// block i, if one begins in the run and does.
+__host__ __device__ __forceinline__ bool cuts_by_item(const AttendBatch& b, int blocks) { return b.pairs * b.n_kv_heads <= blocks; }
+
+__device__ __forceinline__ AttendCut cut_of(const AttendBatch& b, const int* pre, int block, int blocks) {
+    const Runs runs = attend_runs(pre[b.pairs] * b.n_kv_heads, blocks);
+    const bool by_item = cuts_by_item(b, blocks);
+    AttendCut cut{};
+    int u = -1;
+    if (by_item) {
+        const int p = block / b.n_kv_heads;
+        if (p < b.pairs) u = pre[p] * b.n_kv_heads + block % b.n_kv_heads * (pre[p + 1] - pre[p]);
+    } else if (block + 1 < runs.blocks) {
+        u = attend_run(runs, block + 1) - 1;
+    }
+    if (u < 0) return cut;
+    const Item item = attend_item(b, pre, b.n_kv_heads, u);
+    const int b0 = attend_block(runs, item.first), b1 = attend_block(runs, item.first + item.units - 1);
+    if (b0 == b1 || (!by_item && b0 != block)) return cut;
+    cut.seq = item.seq;
+    cut.g = item.g;
+    cut.row0 = item.tile * kRowTile;
+    cut.rows = min(kRowTile, b.span[item.seq].m * b.G - cut.row0);
+    cut.parts = b1 - b0 + 1;
+    cut.block = b0;
+    cut.skip = attend_run(runs, b0) == item.first ? 0 : 1;
+    return cut;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_constant__ AttendBatch b) {
     constexpr int kOp = kTile * D * 2;              // bytes of an operand tile
@@ -283,6 +313,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmem = ctl->tmem;
     static_assert(kTile * (D + 4) * 4 + 1024 + 8 * 32 * 36 * 4 <= 6 * kOp, "the results' way through the operands' memory");
     // Every role walks the run's segments by itself, in a branch of its own, whose registers are its own; all of
@@ -328,6 +359,8 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
     if (warp >= 16) {
         // ---------------- products ----------------
         regs_down<kRegsIssue>();
+        if (threadIdx.x == 18 * 32) b.cuts[blockIdx.x] = cut_of(b, pre, blockIdx.x, gridDim.x);
+        __syncwarp();
         while (true) {
             if (threadIdx.x == 17 * 32 && ctl->unit < ctl->run1)
                 attend_segment(b, pre, b.n_kv_heads, 0, ctl->unit, ctl->run1, D, kRowTile, &seg);
@@ -649,32 +682,20 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
     if (warp == 16) tmem_dealloc(tmem, 512);
 }
 
-// Joins the parts of the items that runs' ends cut.  Block x looks at one item where there are fewer items
-// than cuts, else at the end of run x, and joins the item there if that end is the first in it.  A thread takes
-// four elements of a row.
+// Joins the parts of the items that runs' ends cut, one record's each (x).  A thread takes four elements of a row.
+// Launched while the products are still running (griddepcontrol): nothing may be read, nor a block leave, before
+// their end.  (With every block counting the units for itself, launched behind the products, 1024 tokens over 16384
+// positions took 285 us for 270.)
 template <int D>
-__global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ AttendBatch b, int grid, int by_item) {
-    extern __shared__ int pre[];
-    attend_units(b, kRowTile, pre);
-    const Runs runs = attend_runs(pre[b.pairs] * b.n_kv_heads, grid);
-    int u;
-    if (by_item) {
-        const int p = blockIdx.x / b.n_kv_heads;
-        u = pre[p] * b.n_kv_heads + blockIdx.x % b.n_kv_heads * (pre[p + 1] - pre[p]);
-    } else {
-        if ((int)blockIdx.x + 1 >= runs.blocks) return;
-        u = attend_run(runs, blockIdx.x + 1);
+__global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ AttendBatch b) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const AttendCut cut = b.cuts[blockIdx.x];
+    if (cut.parts == 0) return;
+    for (int e = blockIdx.y * 256 + threadIdx.x; e < cut.rows * (D / 4); e += kJoinBlocks * 256) {
+        const int r = e / (D / 4), d = (e % (D / 4)) * 4;
+        const Joined j = attend_join_row<D>(b, 2 * cut.block, cut.skip, 2, cut.parts, kRowTile, r, d);
+        attend_write<D>(b, b.s[cut.seq], cut.g, cut.row0 + r, d, j.y, j.M, j.l);
     }
-    const Item item = attend_item(b, pre, b.n_kv_heads, u);
-    const int b0 = attend_block(runs, item.first), b1 = attend_block(runs, item.first + item.units - 1);
-    if (b0 == b1 || (!by_item && (item.first == u || b0 != (int)blockIdx.x))) return;
-    const int row0 = item.tile * kRowTile, rows = min(kRowTile, b.span[item.seq].m * b.G - row0);
-    const int e = blockIdx.y * 256 + threadIdx.x;
-    if (e >= rows * (D / 4)) return;
-    const int r = e / (D / 4), d = (e % (D / 4)) * 4;
-    const int skip = attend_run(runs, b0) == item.first ? 0 : 1;     // of the first run's two slots
-    const Joined j = attend_join_row<D>(b, 2 * b0, skip, 2, b1 - b0 + 1, kRowTile, r, d);
-    attend_write<D>(b, b.s[item.seq], item.g, row0 + r, d, j.y, j.M, j.l);
 }
 
 template <int D>
@@ -694,11 +715,16 @@ cudaError_t launch(const AttendBatch& b, int blocks, cudaStream_t st) {
     k_attend_tc<D><<<blocks, kThreadsAt, smem_bytes<D>(), st>>>(b);
     e = cudaGetLastError();
     if (e != cudaSuccess || blocks == 1) return e;
-    const int64_t items = (int64_t)b.pairs * b.n_kv_heads;
-    const bool by_item = items < blocks;
-    k_attend_join<D><<<dim3(by_item ? (int)items : blocks - 1, kRowTile * (D / 4) / 256), 256,
-                       (b.pairs + 1) * sizeof(int), st>>>(b, blocks, by_item);
-    return cudaGetLastError();
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(cuts_by_item(b, blocks) ? b.pairs * b.n_kv_heads : blocks - 1, kJoinBlocks);
+    config.blockDim = dim3(256);
+    config.stream = st;
+    config.attrs = &early;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, k_attend_join<D>, b);
 }
 
 }  // namespace

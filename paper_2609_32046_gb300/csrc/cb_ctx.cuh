@@ -53,6 +53,7 @@ struct cb_ctx {
     float* attend_part = nullptr;   // cb_attend: partial results (outputs; maxima and sums)
     float2* attend_ml = nullptr;
     int32_t* attend_tickets = nullptr;   // zero between calls
+    cbk::AttendCut* attend_cuts = nullptr;    // and its records of items that several blocks share
     cbk::RopeTable rope;
     cbk::StageTimer* timer = nullptr;
     std::string last_error;

@@ -286,6 +286,13 @@ struct AttendSpan {
     int32_t pair0;            // row tiles of the sequences before
 };
 
+// An item (row tile, head) of k_attend_tc that several blocks' runs share: the parts' blocks are block, block + 1 ...
+struct AttendCut {
+    int32_t seq, g, row0, rows;
+    int32_t parts;            // 0: none
+    int32_t block, skip;      // skip: which of the first block's two slots
+};
+
 struct AttendBatch {
     int32_t n;
     int32_t n_q_heads, n_kv_heads, G;
@@ -296,6 +303,7 @@ struct AttendBatch {
     float* part;              // partial outputs [slot][rows of a tile][d]
     float2* part_ml;          // their (maximum, sum) [slot][rows of a tile]
     int32_t* tickets;         // kFewTickets a block of k_attend_few, zero between calls
+    AttendCut* cuts;          // one a block of k_attend_tc
     int32_t pairs;            // row tiles of all sequences
     uint64_t wait_ns;
     AttendSpan span[kMaxBatch];

@@ -391,6 +391,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         b.part = ctx->attend_part;
         b.part_ml = ctx->attend_ml;
         b.tickets = ctx->attend_tickets;
+        b.cuts = ctx->attend_cuts;
         b.wait_ns = (uint64_t)ctx->wait_ns;
         for (int k = 0; k < b.n; ++k) {
             const cb_packed& p = caches[some[b0 + k]];
