@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+from array import array
 from typing import Optional, Sequence
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -144,7 +145,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.cb_stage_times.restype = ctypes.c_int
     lib.cb_create_receiver.argtypes = lib.cb_create.argtypes
     lib.cb_create_receiver.restype = ctypes.c_int
-    lib.cb_rotary.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_vectors), ctypes.POINTER(cb_rope), P]
+    lib.cb_rotary.argtypes = [P, ctypes.c_int32, P, ctypes.POINTER(cb_rope), P]
     lib.cb_rotary.restype = ctypes.c_int
     lib.cb_pack.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_kv), P, P, ctypes.POINTER(cb_packed), P, P,
                             ctypes.c_int32, ctypes.c_int32, P]
@@ -152,8 +153,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.cb_unpack.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_packed), P, P, P, P, ctypes.c_int64, P,
                               ctypes.c_int64, ctypes.c_int64, P]
     lib.cb_unpack.restype = ctypes.c_int
-    lib.cb_attend.argtypes = [P, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(cb_packed),
-                              ctypes.POINTER(cb_attend_query), ctypes.c_int32, ctypes.c_int64, P]
+    lib.cb_attend.argtypes = [P, ctypes.c_int32, ctypes.c_int32, P, P, ctypes.c_int32, ctypes.c_int64, P]
     lib.cb_attend.restype = ctypes.c_int
     if path is None:
         _LIB = lib
@@ -311,27 +311,30 @@ class PackedKV:
         _require(k.shape == v.shape and k_scale.shape == v_scale.shape and k.shape[:-1] == k_scale.shape[:-1] and
                  k.shape[-1] == 16 * k_scale.shape[-1], "codes hold d / 2 and scales d / 32 elements of the same rows")
         kd, sd = k.shape[-1], k_scale.shape[-1]
-        for x, n in ((k, kd), (v, kd), (k_scale, sd), (v_scale, sd)):
+        shape, kt, st = k.shape, k.stride(), k_scale.stride()
+        like = v.stride() == kt and v_scale.stride() == st and kt[-1] == st[-1] == 1     # (nearly always)
+        for a, b, c in zip(shape[:-1], kt, st):
+            like = like and b % kd == 0 and b // kd * sd == c
+        for x, n in () if like else ((k, kd), (v, kd), (k_scale, sd), (v_scale, sd)):
             _require(x.stride(-1) == 1, "rows are contiguous")
             # (the stride of a dimension of one entry says nothing)
-            _require(all(a == 1 or (s % n == 0 and s // n == t // kd) for a, s, t in
-                         zip(x.shape[:-1], x.stride()[:-1], k.stride()[:-1])),
+            _require(all(a == 1 or (s % n == 0 and s // n == t // kd) for a, s, t in zip(shape[:-1], x.stride()[:-1], kt[:-1])),
                      "codes and scales of K and V need the same strides in rows")
         self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
         self.head_dim = 2 * kd
         self.device = k.device
         if paged:
-            self.page_size, self.n_pages = k.shape[2], k.shape[1]
+            self.page_size, self.n_pages = shape[2], shape[1]
             _require(self.page_size & (self.page_size - 1) == 0, "page_size must be a power of two")
             _require(_is_int32(pages) and pages.dim() == 1 and pages.is_contiguous(), "pages are a row of int32")
-            self.n_layers, self.n_kv_heads = k.shape[0], k.shape[3]
+            self.n_layers, self.n_kv_heads = shape[0], shape[3]
             self.capacity = pages.numel() * self.page_size
             order = (0, 3, 2)
         else:
-            self.n_layers, self.n_kv_heads, self.capacity = k.shape[:3]
+            self.n_layers, self.n_kv_heads, self.capacity = shape[:3]
             order = (0, 1, 2)
-        row = [k.stride(i) // kd * self.head_dim if k.shape[i] > 1 else self.head_dim for i in order]
-        self._page = (k.stride(1) // kd * self.head_dim if k.shape[1] > 1 else self.head_dim) if paged else 0
+        row = [kt[i] // kd * self.head_dim if shape[i] > 1 else self.head_dim for i in order]
+        self._page = (kt[1] // kd * self.head_dim if shape[1] > 1 else self.head_dim) if paged else 0
         # the description with its T left open (bytes of a cb_packed are copied faster than fields are set)
         d = cb_packed(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), 0, row[0], row[1], row[2])
         if paged:
@@ -360,8 +363,10 @@ class PackedKV:
 
     @T.setter
     def T(self, T: int):
-        _require(0 <= T <= self.capacity, "T = %d not in [0, %d]" % (T, self.capacity))
+        if not 0 <= T <= self.capacity:
+            raise ValueError("T = %d not in [0, %d]" % (T, self.capacity))
         self._T = int(T)
+        self._bytes = None
 
     @property
     def length(self):
@@ -372,6 +377,13 @@ class PackedKV:
         _require(x is None or (_is_int32(x) and x.numel() == 1), "length is one int32")
         self._length = x
         self._desc.length = None if x is None else x.data_ptr()
+        self._bytes = None
+
+    def _described(self) -> bytes:
+        """The bytes of desc(): a call joins those of its caches."""
+        if self._bytes is None:
+            self._bytes = bytes(self.desc())
+        return self._bytes
 
     def desc(self, T: Optional[int] = None) -> cb_packed:
         self._desc.T = self._T if T is None else T
@@ -547,17 +559,20 @@ class CacheBack:
         ys = [x if y is None else y for x, y in zip(xs, ys or [None] * n)]
         pos = list(pos) if isinstance(pos, (list, tuple)) else [pos] * n
         _require(len(pos) == n, "one pos (or None) per x")
-        sets = (cb_vectors * n)()
-        for i, (x, y, p) in enumerate(zip(xs, ys, pos)):
-            _require(x.shape == y.shape and x.dim() in (3, 4) and x.shape[-1] == self.cfg.head_dim, "vectors are [nL][tokens][heads][d]")
-            _require(_is_bf16(x) and _is_bf16(y), "vectors are bf16")
-            xt, yt = x.stride(), y.stride()
-            _require(xt[-1] == yt[-1] == 1, "vectors are contiguous")
-            nl, xl, yl = (x.shape[0], xt[0], yt[0]) if x.dim() == 4 else (1, 0, 0)
-            _require(p is None or (_is_int32(p) and p.is_contiguous() and p.numel() == x.shape[-3]), "pos holds one int32 a token")
-            sets[i] = cb_vectors(x.data_ptr(), y.data_ptr(), nl, x.shape[-2], x.shape[-3], xl, xt[-3], xt[-2], yl, yt[-3],
-                                 yt[-2], None if p is None else p.data_ptr(), int(pos0))
-        self._check(self.lib.cb_rotary(self.h, n, sets, ctypes.byref(rope.desc(inverse)),
+        fields = array("q")                   # of cb_vectors, eight bytes each (the two counts of layers and heads share them)
+        for x, y, p in zip(xs, ys, pos):
+            shape, xt = x.shape, x.stride()
+            yt = xt if y is x else y.stride()
+            if not (shape == y.shape and len(shape) in (3, 4) and shape[-1] == self.cfg.head_dim):
+                raise ValueError("vectors are [nL][tokens][heads][d]")
+            if not (_is_bf16(x) and (y is x or _is_bf16(y)) and xt[-1] == yt[-1] == 1):
+                raise ValueError("vectors are bf16 and contiguous")
+            if p is not None and not (_is_int32(p) and p.is_contiguous() and p.numel() == shape[-3]):
+                raise ValueError("pos holds one int32 a token")
+            nl, xl, yl = (shape[0], xt[0], yt[0]) if len(shape) == 4 else (1, 0, 0)
+            fields.extend((x.data_ptr(), y.data_ptr(), nl | shape[-2] << 32, shape[-3], xl, xt[-3], xt[-2], yl, yt[-3], yt[-2],
+                           0 if p is None else p.data_ptr(), pos0))
+        self._check(self.lib.cb_rotary(self.h, n, fields.buffer_info()[0], ctypes.byref(rope.desc(inverse)),
                                       _stream_on(stream, xs[0]) if n else 0))
         return ys
 
@@ -570,21 +585,26 @@ class CacheBack:
         n = len(Ks)
         idx, rows = idx or [None] * n, rows or [None] * n
         counts = counts or [int(K.shape[2]) if x is None else int(x.numel()) for K, x in zip(Ks, idx)]
-        _require(n > 0 and all(len(x) == n for x in (Vs, caches, idx, rows, counts, Ks if offsets is None else offsets)),
-                 "one entry per sender in every list")
+        if not (0 < n == len(Vs) == len(caches) == len(idx) == len(rows) == len(counts) and (offsets is None or len(offsets) == n)):
+            raise ValueError("one entry per sender in every list")
+        layers = Ks[0].shape[0]
         for K, V, x, r, c, p in zip(Ks, Vs, idx, rows, counts, caches):
-            _require(all(t is None or (_is_int32(t) and t.is_contiguous() and t.numel() >= c) for t in (x, r)),
-                     "idx and rows hold an int32 a row")
-            _require(K.dtype == V.dtype and (isinstance(K, PagedKV) or (_is_bf16(K) and K.shape == V.shape)), "K and V are bf16")
+            for t in (x, r):
+                if t is not None and not (_is_int32(t) and t.is_contiguous() and t.numel() >= c):
+                    raise ValueError("idx and rows hold an int32 a row")
+            shape = K.shape
+            if not (isinstance(K, PagedKV) or (_is_bf16(K) and K.dtype == V.dtype and shape == V.shape)):
+                raise ValueError("K and V are bf16 of one shape")
             self._fits(p)
-            _require(K.shape[1] == p.n_kv_heads and K.shape[3] == p.head_dim and K.shape[0] == Ks[0].shape[0], "K and V do not match the cache")
+            if not (shape[1] == p.n_kv_heads and shape[3] == p.head_dim and shape[0] == layers):
+                raise ValueError("K and V do not match the cache")
         kv = (cb_kv * n)(*[kv_desc(K, V) for K, V in zip(Ks, Vs)])
         held = (cb_packed * n)(*[p.desc(min(p.capacity, self.cfg.max_positions)) for p in caches])
         ip = _ptr_array([None if x is None else x.data_ptr() for x in idx])
         rp = _ptr_array([None if r is None else r.data_ptr() for r in rows])
         off = None if offsets is None else _ptr_array(list(map(int, offsets)), ctypes.c_int64)
         self._check(self.lib.cb_pack(self.h, n, kv, ip, _ptr_array(list(map(int, counts)), ctypes.c_int64), held, off, rp,
-                                     int(layer), int(Ks[0].shape[0]), _stream_on(stream, caches[0].k)))
+                                     int(layer), int(layers), _stream_on(stream, caches[0].k)))
 
     def unpack(self, caches: Sequence, k_out, v_out, offsets: Optional[Sequence[int]] = None, idx: Optional[Sequence] = None,
                counts: Optional[Sequence[int]] = None, stream=None):
@@ -616,37 +636,52 @@ class CacheBack:
         `window` of them where window > 0; otherwise all); lses[i] (fp32 [m][Hq], contiguous) receives the
         log-sum-exp.  Qs, outs and lses may be tensors with the sequences in their first dimension."""
         n = len(caches)
-        _require(len(Qs) == len(outs) == n and (lses is None or len(lses) == n), "one query and output per cache")
-        c, shape = self.cfg, self._shape
-        q, held = (cb_attend_query * n)(), (cb_packed * n)()
-        whole = all(hasattr(x, "data_ptr") for x in (Qs, outs)) and (lses is None or hasattr(lses, "data_ptr"))
-        if whole and n:          # one tensor each: the sequences' addresses by arithmetic
-            self._queries(Qs[0], outs[0], None if lses is None else lses[0])
-            m = Qs.shape[1]
-            a, (sa, ta, ha) = Qs.data_ptr(), Qs.stride()[:3]
-            o, (so, to, ho) = outs.data_ptr(), outs.stride()[:3]
-            e, se = (None, 0) if lses is None else (lses.data_ptr(), 4 * lses.stride(0))
-        for i, p in enumerate(caches):
-            if p._shape != shape:
+        cfg, like = self.cfg, self._shape
+        for p in caches:
+            if p._shape != like:
                 self._fits(p)
-            p._desc.T = p._T
-            held[i] = p._desc
-            if whole:
-                q[i] = (a + 2 * i * sa, o + 2 * i * so, None if e is None else e + i * se, m, ta, ha, to, ho)
-            else:
-                q[i] = self._queries(Qs[i], outs[i], None if lses is None else lses[i])
-        self._check(self.lib.cb_attend(self.h, int(layer), n, held, q, 1 if causal else 0, int(window),
+        held = b"".join([p._bytes or p._described() for p in caches])
+        if n and hasattr(Qs, "data_ptr") and hasattr(outs, "data_ptr") and (lses is None or hasattr(lses, "data_ptr")):
+            # one tensor each: the sequences' addresses by arithmetic
+            shape, qt, ot = Qs.shape, Qs.stride(), outs.stride()
+            if not (len(shape) == 4 and shape == outs.shape and shape[0] == n and shape[2] == cfg.n_q_heads and
+                    shape[3] == cfg.head_dim and qt[3] == ot[3] == 1 and _is_bf16(Qs) and _is_bf16(outs)):
+                raise ValueError("queries and outputs are bf16 [sequences][m][Hq][d]")
+            m, a, o, e = shape[1], Qs.data_ptr(), outs.data_ptr(), 0
+            steps = [(0, a, 2 * qt[0]), (1, o, 2 * ot[0])]
+            if lses is not None:
+                lt = lses.stride()
+                if not (lses.shape == shape[:3] and lses.element_size() == 4 and lses.dtype.is_floating_point and
+                        (m == 0 or (lt[2] == 1 and (m == 1 or lt[1] == shape[2])))):
+                    raise ValueError("lse is fp32 [sequences][m][Hq]")
+                e = lses.data_ptr()
+                steps.append((2, e, 4 * lt[0]))
+            fields = array("q", (a, o, e, m, qt[1], qt[2], ot[1], ot[2])) * n      # of cb_attend_query, eight bytes each
+            for at, first, step in steps:
+                if n > 1 and step:
+                    fields[at::8] = array("q", range(first, first + n * step, step))
+        else:
+            _require(len(Qs) == len(outs) == n and (lses is None or len(lses) == n), "one query and output per cache")
+            fields = array("q")
+            for i in range(n):
+                fields.extend(self._queries(Qs[i], outs[i], None if lses is None else lses[i]))
+        self._check(self.lib.cb_attend(self.h, int(layer), n, held, fields.buffer_info()[0], 1 if causal else 0, int(window),
                                        _stream_on(stream, caches[0].k) if n else 0))
 
     def _queries(self, Q, out, lse):
         """One sequence's fields of a cb_attend_query, looked over."""
         qt, ot = Q.stride(), out.stride()
-        m, heads, d = Q.shape
-        _require(out.shape == Q.shape and heads == self.cfg.n_q_heads and d == self.cfg.head_dim and qt[2] == ot[2] == 1 and
-                 _is_bf16(Q) and _is_bf16(out), "queries and outputs are bf16 [m][Hq][d]")
-        _require(lse is None or (lse.shape == (m, heads) and lse.is_contiguous() and lse.element_size() == 4 and lse.dtype.is_floating_point),
-                 "lse is fp32 [m][Hq]")
-        return (Q.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(), m, qt[0], qt[1], ot[0], ot[1])
+        m, heads, d = shape = Q.shape
+        if not (out.shape == shape and heads == self.cfg.n_q_heads and d == self.cfg.head_dim and qt[2] == ot[2] == 1 and
+                _is_bf16(Q) and _is_bf16(out)):
+            raise ValueError("queries and outputs are bf16 [m][Hq][d]")
+        if lse is None:
+            e = 0
+        else:
+            _require(lse.shape == (m, heads) and lse.is_contiguous() and lse.element_size() == 4 and lse.dtype.is_floating_point,
+                     "lse is fp32 [m][Hq]")
+            e = lse.data_ptr()
+        return Q.data_ptr(), out.data_ptr(), e, m, qt[0], qt[1], ot[0], ot[1]
 
     def _fits(self, p: PackedKV):
         _require(p._shape == self._shape, "the cache's layers, heads or head dimension are not the context's")

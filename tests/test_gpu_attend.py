@@ -477,3 +477,39 @@ def test_lists_and_types_that_do_not_fit_are_refused():
                  lambda: c.rx.attend(c.caches, c.q, c.out, lses=[c.lse[0].int()])):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("m", [1, 3])
+def test_sequences_in_one_tensor(m):
+    """Queries, outputs and log-sum-exps with the sequences in their first dimension, in slices of wider tensors too."""
+    c = Case(128, 8, 2, [m] * 3, [70, 5, 300])
+    c.run()
+    c.check()
+    want = [x.clone() for x in c.out], [x.clone() for x in c.lse]
+    for step in (1, 2):
+        Q, out = (torch.zeros((3 * step, m, 10, 128), dtype=torch.bfloat16, device="cuda")[::step, :, 1:9] for _ in range(2))
+        lse = torch.zeros((3 * step, m, 8), device="cuda")[::step]
+        Q.copy_(torch.stack(c.q))
+        c.rx.attend(c.caches, Q, out, lses=lse)
+        c.rx.sync_status()
+        assert torch.equal(out, torch.stack(want[0])) and torch.equal(lse, torch.stack(want[1]))
+        out.zero_()
+        c.rx.attend(c.caches, Q, out)
+        assert torch.equal(out, torch.stack(want[0]))
+    for bad in (lambda: c.rx.attend(c.caches, Q[:2], out[:2]), lambda: c.rx.attend(c.caches, Q.half(), out),
+                lambda: c.rx.attend(c.caches, Q, out, lses=lse.transpose(0, 1)),
+                lambda: c.rx.attend(c.caches, Q, out, lses=lse.double()),
+                lambda: c.rx.attend(c.caches, Q[..., :64], out[..., :64])):
+        with pytest.raises(ValueError):
+            bad()
+    one = Case(128, 8, 2, [m], [70])              # one query for all, by a stride of zero
+    one.caches = one.caches * 3
+    Q, out = one.q[0][None].expand(3, -1, -1, -1), torch.zeros((3, m, 8, 128), dtype=torch.bfloat16, device="cuda")
+    one.rx = cb.Receiver(1, 8, 2, 128, m, 200, 3)
+    one.rx.attend(one.caches, Q, out)
+    one.run = None
+    one.out = [out[2]]
+    one.lse = [torch.zeros((m, 8), device="cuda")]
+    one.rx.attend(one.caches[:1], one.q, [out[0]], lses=one.lse)
+    one.check(which=[0])
+    assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[2])
