@@ -147,10 +147,10 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.cb_create_receiver.restype = ctypes.c_int
     lib.cb_rotary.argtypes = [P, ctypes.c_int32, P, ctypes.POINTER(cb_rope), P]
     lib.cb_rotary.restype = ctypes.c_int
-    lib.cb_pack.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_kv), P, P, ctypes.POINTER(cb_packed), P, P,
+    lib.cb_pack.argtypes = [P, ctypes.c_int32, P, P, P, P, P, P,
                             ctypes.c_int32, ctypes.c_int32, P]
     lib.cb_pack.restype = ctypes.c_int
-    lib.cb_unpack.argtypes = [P, ctypes.c_int32, ctypes.POINTER(cb_packed), P, P, P, P, ctypes.c_int64, P,
+    lib.cb_unpack.argtypes = [P, ctypes.c_int32, P, P, P, P, P, ctypes.c_int64, P,
                               ctypes.c_int64, ctypes.c_int64, P]
     lib.cb_unpack.restype = ctypes.c_int
     lib.cb_attend.argtypes = [P, ctypes.c_int32, ctypes.c_int32, P, P, ctypes.c_int32, ctypes.c_int64, P]
@@ -598,12 +598,16 @@ class CacheBack:
             self._fits(p)
             if not (shape[1] == p.n_kv_heads and shape[3] == p.head_dim and shape[0] == layers):
                 raise ValueError("K and V do not match the cache")
-        kv = (cb_kv * n)(*[kv_desc(K, V) for K, V in zip(Ks, Vs)])
-        held = (cb_packed * n)(*[p.desc(min(p.capacity, self.cfg.max_positions)) for p in caches])
-        ip = _ptr_array([None if x is None else x.data_ptr() for x in idx])
-        rp = _ptr_array([None if r is None else r.data_ptr() for r in rows])
-        off = None if offsets is None else _ptr_array(list(map(int, offsets)), ctypes.c_int64)
-        self._check(self.lib.cb_pack(self.h, n, kv, ip, _ptr_array(list(map(int, counts)), ctypes.c_int64), held, off, rp,
+        kv = b"".join([bytes(kv_desc(K, V)) for K, V in zip(Ks, Vs)])
+        held = b"".join([bytes(p.desc(min(p.capacity, self.cfg.max_positions))) for p in caches])
+        # idx, counts, offsets and rows of the call, one array of eight-byte numbers
+        parts = array("q", [0 if x is None else x.data_ptr() for x in idx])
+        parts.extend(map(int, counts))
+        parts.extend(map(int, offsets or ()))
+        parts.extend([0] * (3 * n - len(parts)))
+        parts.extend([0 if x is None else x.data_ptr() for x in rows])
+        at = parts.buffer_info()[0]
+        self._check(self.lib.cb_pack(self.h, n, kv, at, at + 8 * n, held, None if offsets is None else at + 16 * n, at + 24 * n,
                                      int(layer), int(layers), _stream_on(stream, caches[0].k)))
 
     def unpack(self, caches: Sequence, k_out, v_out, offsets: Optional[Sequence[int]] = None, idx: Optional[Sequence] = None,
@@ -619,15 +623,18 @@ class CacheBack:
         for p, x, c in zip(caches, idx, counts):
             self._fits(p)
             _require(x is None or (_is_int32(x) and x.is_contiguous() and x.numel() >= c), "idx holds an int32 a row")
-        ost = k_out.stride()
-        _require(ost[3] == 1 and ost[2] == k_out.size(3) == self.cfg.head_dim and v_out.stride() == ost and
-                 v_out.shape == k_out.shape and _is_bf16(k_out) and _is_bf16(v_out) and
-                 tuple(k_out.shape[:2]) == (self.cfg.n_layers, self.cfg.n_kv_heads), "k_out, v_out are bf16 [nL][Hkv][capacity][d]")
-        held = (cb_packed * n)(*[p.desc() for p in caches])
-        self._check(self.lib.cb_unpack(self.h, n, held, _ptr_array([None if x is None else x.data_ptr() for x in idx]),
-                                       _ptr_array(list(map(int, counts)), ctypes.c_int64), k_out.data_ptr(), v_out.data_ptr(),
-                                       k_out.size(2), _ptr_array(list(map(int, offsets)), ctypes.c_int64), ost[0], ost[1],
-                                       _stream_on(stream, k_out)))
+        shape, ost = k_out.shape, k_out.stride()
+        if not (len(shape) == 4 and ost[3] == 1 and ost[2] == shape[3] == self.cfg.head_dim and v_out.stride() == ost and
+                v_out.shape == shape and _is_bf16(k_out) and _is_bf16(v_out) and
+                shape[0] == self.cfg.n_layers and shape[1] == self.cfg.n_kv_heads):
+            raise ValueError("k_out, v_out are bf16 [nL][Hkv][capacity][d]")
+        held = b"".join([p._bytes or p._described() for p in caches])
+        parts = array("q", [0 if x is None else x.data_ptr() for x in idx])
+        parts.extend(map(int, counts))
+        parts.extend(map(int, offsets))
+        at = parts.buffer_info()[0]
+        self._check(self.lib.cb_unpack(self.h, n, held, at, at + 8 * n, k_out.data_ptr(), v_out.data_ptr(), shape[2], at + 16 * n,
+                                       ost[0], ost[1], _stream_on(stream, k_out)))
 
     def attend(self, caches: Sequence, Qs: Sequence, outs: Sequence, layer: int = 0, causal: bool = True, window: int = 0,
                lses: Optional[Sequence] = None, stream=None):
