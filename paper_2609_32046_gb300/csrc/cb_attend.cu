@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
             if (last_of(b.tickets + group0 + of_group, members, &last)) {
                 for (int e = threadIdx.x; e < x.rows * (D / 4); e += kWarps * 32) {
                     const int r = e / (D / 4), d = (e % (D / 4)) * 4;
-                    const Joined j = attend_join_row<D>(b, group0, of_group, 2 * b.n_kv_heads, members, ROWS, r, d);
+                    const Joined j = attend_join_row<D, 8>(b, group0, of_group, 2 * b.n_kv_heads, members, ROWS, r, d);
                     if (groups == 1) {
                         attend_write<D>(b, s, g, r, d, j.y, j.M, j.l);
                     } else {
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
                 if (groups > 1 && last_of(b.tickets + 2 * gridDim.x + item0, groups, &last))
                     for (int e = threadIdx.x; e < x.rows * (D / 4); e += kWarps * 32) {
                         const int r = e / (D / 4), d = (e % (D / 4)) * 4;
-                        const Joined j = attend_join_row<D>(b, 2 * ((int64_t)gridDim.x + item0), skip, 2 * size * b.n_kv_heads,
+                        const Joined j = attend_join_row<D, 8>(b, 2 * ((int64_t)gridDim.x + item0), skip, 2 * size * b.n_kv_heads,
                                                             groups, ROWS, r, d);
                         attend_write<D>(b, s, g, r, d, j.y, j.M, j.l);
                     }

@@ -304,22 +304,22 @@ __device__ __forceinline__ void add_part(float4& y, float& l, const float4& v, f
     l = fmaf(sum, f, l);
 }
 
-// Four elements of a row from n parts, in order, eight at a time: parts are slots slot0 + skip, slot0 + step,
+// Four elements of a row from n parts, in order, N at a time: parts are slots slot0 + skip, slot0 + step,
 // slot0 + 2 step ...
 struct Joined {
     float4 y;
     float M, l;
 };
-template <int D>
+template <int D, int N>
 __device__ __forceinline__ Joined attend_join_row(const AttendBatch& b, int64_t slot0, int skip, int step, int n, int tile_rows,
                                                   int r, int d) {
     Joined j{make_float4(0.f, 0.f, 0.f, 0.f), -INFINITY, 0.f};
 #pragma unroll 1
-    for (int k0 = 0; k0 < n; k0 += 8) {
-        float2 x[8];
-        float4 v[8];
+    for (int k0 = 0; k0 < n; k0 += N) {
+        float2 x[N];
+        float4 v[N];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             const int k = k0 + i;
             const int64_t at = (slot0 + (k ? k * step : skip)) * tile_rows + r;
             x[i] = make_float2(-INFINITY, 0.f);
@@ -331,13 +331,13 @@ __device__ __forceinline__ Joined attend_join_row(const AttendBatch& b, int64_t 
         }
         float top = j.M;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = fmaxf(top, x[i].x);
+        for (int i = 0; i < N; ++i) top = fmaxf(top, x[i].x);
         const float f = j.M == -INFINITY ? 0.f : exp2f(j.M - top);
         j.y.x *= f; j.y.y *= f; j.y.z *= f; j.y.w *= f;
         j.l *= f;
         j.M = top;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < N; ++i)
             add_part(j.y, j.l, v[i], x[i].x == -INFINITY ? 0.f : exp2f(x[i].x - j.M), x[i].y);
     }
     return j;

@@ -17,7 +17,7 @@
 // O is scaled in place when a row's maximum has grown by more than 8 (log2 domain) since M was set: seldom
 // after the first tiles; until then weights are up to 2^15, in fp16's range.
 //
-// Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 270 us, 988 TFLOP/s, 253 of it before
+// Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 266 us, 1001 TFLOP/s, 253 of it before
 // the join; 64 tokens over 12352 positions 41 us, 34 before it. Bound by the chain of waits of a stream (weights, their
 // product, the next scores, its maximum), by fetching the roles' code and by the shared memory that the products read.
 // 256 rows a block, because each unpacking of a tile serves all of them.  Other forms, when this one (with a slower
@@ -693,7 +693,9 @@ __global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ Att
     if (cut.parts == 0) return;
     for (int e = blockIdx.y * 256 + threadIdx.x; e < cut.rows * (D / 4); e += kJoinBlocks * 256) {
         const int r = e / (D / 4), d = (e % (D / 4)) * 4;
-        const Joined j = attend_join_row<D>(b, 2 * cut.block, cut.skip, 2, cut.parts, kRowTile, r, d);
+        // (a prompt's items have two or three parts: with eight places each it took 270 us, with four 266)
+        const Joined j = cut.parts <= 4 ? attend_join_row<D, 4>(b, 2 * cut.block, cut.skip, 2, cut.parts, kRowTile, r, d)
+                                        : attend_join_row<D, 8>(b, 2 * cut.block, cut.skip, 2, cut.parts, kRowTile, r, d);
         attend_write<D>(b, b.s[cut.seq], cut.g, cut.row0 + r, d, j.y, j.M, j.l);
     }
 }
