@@ -63,26 +63,12 @@ class cb_rope(ctypes.Structure):
                 ("inverse", ctypes.c_int32)]
 
 
-class cb_vectors(ctypes.Structure):
-    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("n_layers", ctypes.c_int32),
-                ("n_heads", ctypes.c_int32), ("n_tokens", ctypes.c_int64), ("s_layer", ctypes.c_int64),
-                ("s_tok", ctypes.c_int64), ("s_head", ctypes.c_int64), ("o_layer", ctypes.c_int64),
-                ("o_tok", ctypes.c_int64), ("o_head", ctypes.c_int64), ("pos", ctypes.c_void_p),
-                ("pos0", ctypes.c_int64)]
-
-
 class cb_packed(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("T", ctypes.c_int64), ("s_layer", ctypes.c_int64),
                 ("s_head", ctypes.c_int64), ("s_pos", ctypes.c_int64), ("pages", ctypes.c_void_p),
                 ("page_size", ctypes.c_int32), ("s_page", ctypes.c_int64), ("n_pages", ctypes.c_int64),
                 ("length", ctypes.c_void_p)]
-
-
-class cb_attend_query(ctypes.Structure):
-    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("m", ctypes.c_int32),
-                ("s_tok", ctypes.c_int64), ("s_head", ctypes.c_int64), ("o_tok", ctypes.c_int64),
-                ("o_head", ctypes.c_int64)]
 
 
 _LIB = None
@@ -559,7 +545,7 @@ class CacheBack:
         ys = [x if y is None else y for x, y in zip(xs, ys or [None] * n)]
         pos = list(pos) if isinstance(pos, (list, tuple)) else [pos] * n
         _require(len(pos) == n, "one pos (or None) per x")
-        fields = array("q")                   # of cb_vectors, eight bytes each (the two counts of layers and heads share them)
+        fields = array("q")                   # of the header's cb_vectors, eight bytes each (the counts of layers and heads share them)
         for x, y, p in zip(xs, ys, pos):
             shape, xt = x.shape, x.stride()
             yt = xt if y is x else y.stride()
@@ -663,7 +649,7 @@ class CacheBack:
                     raise ValueError("lse is fp32 [sequences][m][Hq]")
                 e = lses.data_ptr()
                 steps.append((2, e, 4 * lt[0]))
-            fields = array("q", (a, o, e, m, qt[1], qt[2], ot[1], ot[2])) * n      # of cb_attend_query, eight bytes each
+            fields = array("q", (a, o, e, m, qt[1], qt[2], ot[1], ot[2])) * n      # of the header's cb_attend_query, eight bytes each
             for at, first, step in steps:
                 if n > 1 and step:
                     fields[at::8] = array("q", range(first, first + n * step, step))
