@@ -508,8 +508,8 @@ typedef struct {
  * stands at position L - m + r (its own row is the cache's row there: pack a step's new K/V first) and
  *     out[r][h] = sum_t a_t v_t,  a = softmax over the rows t that r sees of softmax_scale * <q_{r,h}, k_t>
  *     lse[r][h] = ln sum_t exp(softmax_scale * <q_{r,h}, k_t>)
- * over KV head h / G.  causal: r sees rows up to its own position; window > 0 (only with causal): and
- * no rows at or below position - window.  Otherwise r sees all L rows.  A token that sees no row gets
+ * over KV head h / G.  causal: r sees rows up to its own position; window > 0 (only with causal; any
+ * size): and no rows at or below position - window.  Otherwise r sees all L rows.  A token that sees no row gets
  * out = 0 and lse = -infinity.  Logits, weights' sums and outputs are summed in fp32, weights enter
  * their product with the values as fp16 scaled to the row's largest, and out is rounded once to bf16.  With lse a caller joins
  * attention over several caches.  m may differ between sequences; m = 0 skips a sequence.

@@ -477,6 +477,7 @@ int64_t attend_part_rows(int num_sms) { return (int64_t)num_sms * kPartRowsPerSm
 int64_t attend_pairs(AttendBatch& b, int tile_rows) {
     int64_t units = 0;
     b.pairs = 0;
+    b.window = b.window < kFarWindow ? b.window : kFarWindow;
     for (int i = 0; i < b.n; ++i) {
         AttendSpan& s = b.span[i];
         const int tiles = (s.m * b.G + tile_rows - 1) / tile_rows;

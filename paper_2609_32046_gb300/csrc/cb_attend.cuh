@@ -343,6 +343,10 @@ __device__ __forceinline__ Joined attend_join_row(const AttendBatch& b, int64_t 
     return j;
 }
 
+// A window that no cache and its tokens reach across (fewer than 2^31 rows and 1024 tokens): larger ones are
+// taken for this one, so that neither sums of rows, tokens and window nor their differences leave 64 bits.
+constexpr int64_t kFarWindow = (int64_t)1 << 32;
+
 // Host side, shared by the launchers: row tiles of every sequence, and the most units there can be.
 int64_t attend_pairs(AttendBatch& b, int tile_rows);
 cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms);
