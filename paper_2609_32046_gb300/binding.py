@@ -326,6 +326,9 @@ class PackedKV:
         if paged:
             d.pages, d.page_size, d.s_page, d.n_pages = pages.data_ptr(), self.page_size, self._page, self.n_pages
         self._desc = d
+        # the rows cached, and what _described makes of them once it is asked: an assignment puts a new list in its
+        # place, so that a call of another thread never leaves the bytes of one state in the next
+        self._state = [0, None]
         self.length = length
         self._shape = (self.n_layers, self.n_kv_heads, self.head_dim)
         self.T = self.capacity if T is None else T
@@ -345,14 +348,13 @@ class PackedKV:
 
     @property
     def T(self) -> int:
-        return self._T
+        return self._state[0]
 
     @T.setter
     def T(self, T: int):
         if not 0 <= T <= self.capacity:
             raise ValueError("T = %d not in [0, %d]" % (T, self.capacity))
-        self._T = int(T)
-        self._bytes = None
+        self._state = [int(T), None]
 
     @property
     def length(self):
@@ -363,17 +365,20 @@ class PackedKV:
         _require(x is None or (_is_int32(x) and x.numel() == 1), "length is one int32")
         self._length = x
         self._desc.length = None if x is None else x.data_ptr()
-        self._bytes = None
+        self._state = [self.T, None]
 
     def _described(self) -> bytes:
         """The bytes of desc(): a call joins those of its caches."""
-        if self._bytes is None:
-            self._bytes = bytes(self.desc())
-        return self._bytes
+        state = self._state
+        if state[1] is None:
+            state[1] = bytes(self.desc(state[0]))
+        return state[1]
 
     def desc(self, T: Optional[int] = None) -> cb_packed:
-        self._desc.T = self._T if T is None else T
-        return self._desc
+        """A description of its own, with T rows (default: those cached)."""
+        d = cb_packed.from_buffer_copy(self._desc)
+        d.T = self.T if T is None else T
+        return d
 
 
 class Rotary:
@@ -614,7 +619,7 @@ class CacheBack:
                 v_out.shape == shape and _is_bf16(k_out) and _is_bf16(v_out) and
                 shape[0] == self.cfg.n_layers and shape[1] == self.cfg.n_kv_heads):
             raise ValueError("k_out, v_out are bf16 [nL][Hkv][capacity][d]")
-        held = b"".join([p._bytes or p._described() for p in caches])
+        held = b"".join([p._state[1] or p._described() for p in caches])
         parts = array("q", [0 if x is None else x.data_ptr() for x in idx])
         parts.extend(map(int, counts))
         parts.extend(map(int, offsets))
@@ -633,7 +638,7 @@ class CacheBack:
         for p in caches:
             if p._shape != like:
                 self._fits(p)
-        held = b"".join([p._bytes or p._described() for p in caches])
+        held = b"".join([p._state[1] or p._described() for p in caches])
         if n and hasattr(Qs, "data_ptr") and hasattr(outs, "data_ptr") and (lses is None or hasattr(lses, "data_ptr")):
             # one tensor each: the sequences' addresses by arithmetic
             shape, qt, ot = Qs.shape, Qs.stride(), outs.stride()

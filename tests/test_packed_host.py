@@ -98,3 +98,23 @@ def test_other_types_are_refused():
                 lambda: cb.PackedKV(*_arrays((1, 9, 16, 2), 128), pages=table.float())):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_a_cache_is_described_for_each_call_by_itself():
+    """Two threads' calls share a cache: one asks for its rows, the other for its room, between any two steps of each."""
+    p = cb.PackedKV(*_arrays((1, 2, 50), 128), T=10)
+    mine, other = p.desc(), p.desc(p.capacity)
+    assert (mine.T, other.T) == (10, 50)
+    desc = p.desc
+    for meanwhile, after in ((lambda: desc(p.capacity), 10), (lambda: setattr(p, "T", 20), 20),
+                             (lambda: setattr(p, "length", None), 20)):
+        def late(T=None):
+            d = desc(T)
+            meanwhile()
+            return d
+        p.T = p.T                                 # (forgets what is kept)
+        p.desc = late
+        p._described()
+        p.desc = desc
+        kept = binding.cb_packed.from_buffer_copy(p._described())
+        assert kept.T == p.T == after and kept.k == p.k.data_ptr() and kept.s_head == 50 * 128
