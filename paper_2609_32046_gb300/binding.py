@@ -280,10 +280,12 @@ class PackedKV:
     k_scale, v_scale:    bf16 scales, the same index order with d / 32 in the last place; any strides
                          that step over rows alike in codes and scales
     T:                   rows cached (default: all there is room for); may be assigned as the cache grows, as `length` may
-    pages:               int32 device tensor of a paged cache (the sequence's block table)
+    pages:               int32 device tensor of a paged cache (the sequence's block table); may be assigned as well, a
+                         table that has room for T rows
     length:              optional int32 device tensor of one element: CacheBack.attend reads the first
                          min(T, length) rows, as it is when the kernel runs
-    `capacity` is the number of rows there is room for (pack writes below it).
+    `capacity` is the number of rows there is room for (pack writes below it).  The arrays themselves are the
+    cache's for good (k, v, k_scale and v_scale cannot be assigned): other arrays are another PackedKV.
     """
 
     GROUP = 32
@@ -306,15 +308,13 @@ class PackedKV:
             # (the stride of a dimension of one entry says nothing)
             _require(all(a == 1 or (s % n == 0 and s // n == t // kd) for a, s, t in zip(shape[:-1], x.stride()[:-1], kt[:-1])),
                      "codes and scales of K and V need the same strides in rows")
-        self.k, self.v, self.k_scale, self.v_scale, self.pages = k, v, k_scale, v_scale, pages
+        self._arrays = (k, v, k_scale, v_scale)
         self.head_dim = 2 * kd
         self.device = k.device
         if paged:
             self.page_size, self.n_pages = shape[2], shape[1]
             _require(self.page_size & (self.page_size - 1) == 0, "page_size must be a power of two")
-            _require(_is_int32(pages) and pages.dim() == 1 and pages.is_contiguous(), "pages are a row of int32")
             self.n_layers, self.n_kv_heads = shape[0], shape[3]
-            self.capacity = pages.numel() * self.page_size
             order = (0, 3, 2)
         else:
             self.n_layers, self.n_kv_heads, self.capacity = shape[:3]
@@ -324,11 +324,14 @@ class PackedKV:
         # the description with its T left open (bytes of a cb_packed are copied faster than fields are set)
         d = cb_packed(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), 0, row[0], row[1], row[2])
         if paged:
-            d.pages, d.page_size, d.s_page, d.n_pages = pages.data_ptr(), self.page_size, self._page, self.n_pages
+            d.page_size, d.s_page, d.n_pages = self.page_size, self._page, self.n_pages
         self._desc = d
         # the rows cached, and what _described makes of them once it is asked: an assignment puts a new list in its
         # place, so that a call of another thread never leaves the bytes of one state in the next
         self._state = [0, None]
+        self._pages = None
+        if paged:
+            self._set_pages(pages)
         self.length = length
         self._shape = (self.n_layers, self.n_kv_heads, self.head_dim)
         self.T = self.capacity if T is None else T
@@ -345,6 +348,31 @@ class PackedKV:
     def bytes(self) -> int:
         """Bytes that T rows take (codes and scales of K and V, every layer and head)."""
         return 2 * self.n_layers * self.n_kv_heads * self.T * (self.head_dim // 2 + self.head_dim // 16)
+
+    # what a description holds the addresses of (`p.k_scale *= 2` puts back the array it took)
+    def _put_back(self, x, i):
+        if x is not self._arrays[i]:
+            raise AttributeError("a cache's arrays are its own for good: make another PackedKV")
+
+    k, v, k_scale, v_scale = (property(lambda self, i=i: self._arrays[i], lambda self, x, i=i: self._put_back(x, i))
+                              for i in range(4))
+
+    @property
+    def pages(self):
+        return self._pages
+
+    @pages.setter
+    def pages(self, pages):
+        _require(self._pages is not None and pages is not None, "a cache is paged, or not, for good")
+        self._set_pages(pages)
+
+    def _set_pages(self, pages):
+        _require(_is_int32(pages) and pages.dim() == 1 and pages.is_contiguous(), "pages are a row of int32")
+        _require(self.T <= pages.numel() * self.page_size, "the block table has no room for T rows")
+        self._pages = pages
+        self.capacity = pages.numel() * self.page_size
+        self._desc.pages = pages.data_ptr()
+        self._state = [self.T, None]
 
     @property
     def T(self) -> int:

@@ -21,3 +21,21 @@ def test_windows_of_any_size(window, d, m, Ts):
     c.run(window=window)
     c.check()
     assert all(torch.equal(a, b) for a, b in zip(want, c.out + c.lse))
+
+
+@pytest.mark.parametrize("m", [1, 70])
+def test_a_block_table_that_grows(m):
+    """A sequence that outgrows its block table is given a longer one: the cache's next calls read that."""
+    c = Case(128, 8, 2, [m], [200], page=16, room=400)
+    p, whole = c.caches[0], c.caches[0].pages
+    short = cb.PackedKV(p.k, p.v, p.k_scale, p.v_scale, T=200, pages=whole[:13].clone())
+    c.caches = [short]
+    c.run()
+    c.check()
+    short.pages = whole
+    short.T = 600
+    K, V = (torch.randn((1, 2, 400, 128), device="cuda").to(torch.bfloat16) for _ in range(2))
+    c.rx = cb.Receiver(1, 8, 2, 128, m, 600)
+    c.rx.pack([K], [V], [short], [200])
+    c.run()
+    c.check()

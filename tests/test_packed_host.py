@@ -118,3 +118,34 @@ def test_a_cache_is_described_for_each_call_by_itself():
         p.desc = desc
         kept = binding.cb_packed.from_buffer_copy(p._described())
         assert kept.T == p.T == after and kept.k == p.k.data_ptr() and kept.s_head == 50 * 128
+
+
+def test_a_longer_block_table_is_the_one_that_calls_get():
+    p = cb.PackedKV(*_arrays((1, 9, 16, 2), 128), T=40, pages=torch.arange(3, dtype=torch.int32))
+    assert binding.cb_packed.from_buffer_copy(p._described()).pages == p.pages.data_ptr()
+    longer = torch.arange(5, dtype=torch.int32)
+    p.pages = longer
+    for d in (p.desc(), binding.cb_packed.from_buffer_copy(p._described())):
+        assert d.pages == longer.data_ptr() and d.T == 40
+    assert p.pages is longer and p.capacity == 80
+    p.T = 80
+    for bad in (longer[:4], longer.long(), longer.float(), torch.arange(10, dtype=torch.int32)[::2], longer[None], None):
+        with pytest.raises(ValueError):
+            p.pages = bad
+    assert p.pages is longer and p.desc().pages == longer.data_ptr() and (p.T, p.capacity) == (80, 80)
+    flat = cb.PackedKV(*_arrays((1, 2, 50), 128))
+    with pytest.raises(ValueError):
+        flat.pages = longer
+    assert flat.pages is None and not flat.desc().pages
+
+
+def test_a_caches_arrays_are_its_own_for_good():
+    arrays = _arrays((1, 2, 50), 128)
+    p = cb.PackedKV(*arrays)
+    for name, x in zip(("k", "v", "k_scale", "v_scale"), arrays):
+        assert getattr(p, name) is x
+        with pytest.raises(AttributeError):
+            setattr(p, name, x.clone())
+        assert getattr(p, name) is x
+    p.k_scale += 1                                # in place: the same array
+    assert p.k_scale is arrays[2] and (arrays[2] == 1).all()
