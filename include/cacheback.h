@@ -441,7 +441,8 @@ cb_status cb_rotary(cb_ctx *ctx, int32_t n, const cb_vectors *sets, const cb_rop
  * (pages != NULL) as in cb_kv: row t is row t % page_size of page pages[t / page_size], s_page
  * elements apart; n_pages * s_page may not pass 2^31 * head_dim.
  *   alignment  codes 16 bytes, scales 8 (head_dim 128) or 4 (head_dim 64)
- *   T          rows that may be read or written, >= 0
+ *   T          rows that may be read or written, 0 .. 2^31 - 4096; max_positions bounds it in cb_attend alone (a
+ *              message holds the rows of several senders, each of them up to max_positions)
  *   length     device int32 (4-byte aligned) or NULL.  cb_attend then reads the first
  *              min(max(*length, 0), T) rows, as *length is when the kernel runs: a captured graph
  *              follows a cache that grows.  The other calls do not read it.
@@ -478,7 +479,7 @@ typedef struct {
  *   layer, n_layers   layers of the cache that the call writes: a whole message, or one layer of a
  *             forward pass
  * An idx or rows entry out of range skips its row and is reported by cb_sync_status as CB_EDEVICE.
- * Errors: CB_EINVAL, CB_ESHAPE (layers, T above the limit, too many rows), CB_EBUDGET (count < 0,
+ * Errors: CB_EINVAL, CB_ESHAPE (layers, a T above its limit, too many rows), CB_EBUDGET (count < 0,
  * rows past caches[i].T).
  */
 cb_status cb_pack(cb_ctx *ctx, int32_t n, const cb_kv *senders, const int32_t *const *idx, const int64_t *count,

@@ -618,7 +618,7 @@ class CacheBack:
             if not (shape[1] == p.n_kv_heads and shape[3] == p.head_dim and shape[0] == layers):
                 raise ValueError("K and V do not match the cache")
         kv = b"".join([bytes(kv_desc(K, V)) for K, V in zip(Ks, Vs)])
-        held = b"".join([bytes(p.desc(min(p.capacity, self.cfg.max_positions))) for p in caches])
+        held = b"".join([bytes(p.desc(p.capacity)) for p in caches])
         # idx, counts, offsets and rows of the call, one array of eight-byte numbers
         parts = array("q", [0 if x is None else x.data_ptr() for x in idx])
         parts.extend(map(int, counts))

@@ -66,9 +66,11 @@ cb_status check_page_fields(cb_ctx* ctx, DevicePtrs& ptrs, const int32_t* pages,
     return ptrs.check(pages, "pages", i, 4);
 }
 
-cb_status check_packed(cb_ctx* ctx, DevicePtrs& ptrs, const cb_packed& p, int i) {
+// The most rows of a cache: positions are counted in 32 bits, a few tiles past the last one too.
+constexpr int64_t kMaxHeld = kMaxRows - 4096;
+
+cb_status check_packed(cb_ctx* ctx, DevicePtrs& ptrs, const cb_packed& p, int i, int64_t most = kMaxHeld) {
     const int d = ctx->cfg.head_dim;
-    const int64_t most = ctx->cfg.max_positions < kMaxRows - 4096 ? ctx->cfg.max_positions : kMaxRows - 4096;
     if (p.T < 0 || p.T > most)
         return fail(ctx, CB_ESHAPE, "caches[%d].T = %lld not in [0, %lld]", i, (long long)p.T, (long long)most);
     cb_status st;
@@ -358,7 +360,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
     std::vector<int32_t> some;
     for (int i = 0; i < n; ++i) {
         const cb_attend_query& q = queries[i];
-        if ((st = check_packed(ctx, ptrs, caches[i], i))) return st;
+        if ((st = check_packed(ctx, ptrs, caches[i], i, c.max_positions < kMaxHeld ? c.max_positions : kMaxHeld))) return st;
         if (q.m < 0 || q.m > c.max_query_tokens)
             return fail(ctx, CB_ESHAPE, "queries[%d].m = %d not in [0, %d]", i, q.m, c.max_query_tokens);
         if (q.m == 0) continue;
