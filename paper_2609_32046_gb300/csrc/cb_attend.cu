@@ -266,7 +266,9 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             const uint32_t e = min(max(top, 15u), 253u);    // 2^(141 - e): of normal numbers on both sides
-            const float up = __uint_as_float((268u - e) << 23), down = __uint_as_float((e - 14u) << 23) * b.scale_log2e;
+            // (never 0, which times a masked row's -infinity would be NaN: logits are below 2^38, and 2^-88 is none either)
+            const float up = __uint_as_float((268u - e) << 23);
+            const float down = fmaxf(__uint_as_float((e - 14u) << 23) * b.scale_log2e, 1.17549435e-38f);
 #pragma unroll
             for (int w = 0; w < KW; ++w)
 #pragma unroll

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2609_32046_gb300 as cb
+import packed_reference as ref
 from test_gpu_attend import Case
 
 pytestmark = pytest.mark.gpu
@@ -39,3 +40,23 @@ def test_a_block_table_that_grows(m):
     c.rx.pack([K], [V], [short], [200])
     c.run()
     c.check()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -24, 1e-8, 1e-30, 1e-44])
+@pytest.mark.parametrize("m,T", [(1, 40), (4, 200), (70, 300)])
+def test_softmax_scales_near_zero(scale, m, T):
+    """Logits of next to nothing, queries of zeros among them: every row that is seen weighs the same, and rows that
+    are not seen weigh nothing."""
+    c = Case(128, 8, 2, [m], [T], seed=3)
+    c.q[0][0] = 0                                  # a padded token
+    c.q[0][m - 1, 3] = 0
+    c.q[0][m - 1, 4] = 2.0 ** -130
+    c.rx = cb.Receiver(1, 8, 2, 128, m, T, softmax_scale=scale)
+    c.run()
+    c.rx.sync_status()
+    k, v = c.kv(0, 0, T)
+    o, lse, A, size = ref.attention(c.q[0].double(), k, v, scale)
+    E = 2 * (128 + 8) * 2.0 ** -23 * size + 2.0 ** -20 + T * 2.0 ** -23
+    tol = o.abs() * 2.0 ** -8 + A * (2.0 ** -11 + 2 * E) + 2.0 ** -32 * T * float(v.abs().max())
+    assert ((c.out[0].double() - o).abs() <= tol).all()
+    assert ((c.lse[0].double() - lse).abs() <= E + 2.0 ** -22 * lse.abs() + 2.0 ** -21).all()
