@@ -494,7 +494,8 @@ cb_status cb_unpack(cb_ctx *ctx, int32_t n, const cb_packed *caches, const int32
 
 /* Queries of one sequence: Q[r][h][:] at q + r*s_tok + h*s_head, r < m; the outputs at
  * out + r*o_tok + h*o_head (bf16; not overlapping anything the call reads); lse (fp32 [m][n_q_heads], contiguous,
- * 4-byte aligned) or NULL. */
+ * 4-byte aligned) or NULL.  No row of out or lse may be another sequence's too: two that begin at the same place,
+ * or overlap without gaps between their rows, are refused. */
 typedef struct {
     const void *q;
     void *out;

@@ -1,6 +1,7 @@
 // The context behind the C-ABI's opaque handle, and what the host side of every entry point uses.
 #pragma once
 
+#include <algorithm>
 #include <cstdint>
 #include <string>
 #include <vector>
@@ -98,6 +99,28 @@ struct DeviceGuard {
         if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
     }
 };
+
+// Memory that one part of a call writes; dense: every byte of it.
+struct Written {
+    uintptr_t lo, hi;
+    bool dense;
+};
+// Two parts write the same place: they begin there both, or both are dense and overlap.  (Parts that lie between
+// one another's rows, as the slices of a wider array do, are let pass.)  Sorts `w` unless it is in order and apart.
+inline bool written_twice(std::vector<Written>& w) {
+    bool apart = true;
+    for (size_t i = 1; i < w.size() && apart; ++i) apart = w[i - 1].hi <= w[i].lo;
+    if (apart) return false;
+    std::sort(w.begin(), w.end(), [](const Written& a, const Written& b) { return a.lo < b.lo; });
+    uintptr_t end = 0;
+    for (size_t i = 0; i < w.size(); ++i) {
+        if (i && w[i].lo == w[i - 1].lo) return true;
+        if (!w[i].dense) continue;
+        if (w[i].lo < end) return true;
+        end = w[i].hi;
+    }
+    return false;
+}
 
 inline bool stride_ok(int64_t s) { return s > 0 && (s % 8) == 0; }
 

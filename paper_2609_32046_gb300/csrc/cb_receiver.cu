@@ -358,6 +358,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
     if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
     cb_status st;
     std::vector<int32_t> some;
+    std::vector<Written> outs, lses;
     for (int i = 0; i < n; ++i) {
         const cb_attend_query& q = queries[i];
         if ((st = check_packed(ctx, ptrs, caches[i], i, c.max_positions < kMaxHeld ? c.max_positions : kMaxHeld))) return st;
@@ -367,7 +368,8 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         Dim in[2] = {{q.m, q.s_tok}, {c.n_q_heads, q.s_head}}, out[2] = {{q.m, q.o_tok}, {c.n_q_heads, q.o_head}};
         if (!strides_ok(in, 2) || !strides_ok(out, 2))
             return fail(ctx, CB_EINVAL, "queries[%d]: strides must be positive multiples of 8", i);
-        if (span_of(in, 2, d) < 0 || span_of(out, 2, d) < 0 || !rows_apart(out, 2, d))
+        const int64_t rows = (int64_t)q.m * c.n_q_heads, span = span_of(out, 2, d);
+        if (span_of(in, 2, d) < 0 || span < 0 || !rows_apart(out, 2, d))
             return fail(ctx, CB_EINVAL, "queries[%d]: strides are too large, or rows of out overlap", i);
         if ((st = ptrs.check(q.q, "queries.q", i)) || (st = ptrs.check(q.out, "queries.out", i)))
             return st;
@@ -375,9 +377,14 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         // (units of work are counted in 32 bits)
         if ((caches[i].T / 128 + 2) * c.n_kv_heads * ((int64_t)q.m * ctx->G / 128 + 1) > ((int64_t)1 << 31) / kMaxBatch)
             return fail(ctx, CB_ESHAPE, "sequence %d: too many positions, heads and query tokens for one launch", i);
+        const uintptr_t at = reinterpret_cast<uintptr_t>(q.out), e = reinterpret_cast<uintptr_t>(q.lse);
+        outs.push_back(Written{at, at + 2 * (uintptr_t)span, span == rows * d});
+        if (e) lses.push_back(Written{e, e + 4 * (uintptr_t)rows, true});
         some.push_back(i);
     }
     if (some.empty()) return CB_OK;
+    if (written_twice(outs) || written_twice(lses))
+        return fail(ctx, CB_EINVAL, "two sequences write the same rows of out or lse");
     if ((st = attend_scratch(ctx, strm))) return st;
     for (size_t b0 = 0; b0 < some.size(); b0 += kMaxBatch) {
         AttendBatch b;

@@ -53,3 +53,16 @@ def test_a_window_of_any_size_is_planned_for(tmp_path):
                 assert units == n * tiles * Hkv * (reach // 128 + 2)
                 # what the kernels compute with: no sum or difference of it, rows and tokens leaves 64 bits
                 assert window == w or T + m <= window <= min(w, 2 ** 40)
+
+
+def test_what_two_parts_of_a_call_write(tmp_path):
+    """Parts that begin at the same place or overlap densely are found, in any order; slices beside one another are not."""
+    cases = [([], 0), ([(0, 8, 1)], 0), ([(0, 8, 1), (8, 16, 1), (16, 24, 1)], 0), ([(16, 24, 1), (8, 16, 1), (0, 8, 1)], 0),
+             ([(0, 8, 1), (0, 8, 1)], 1), ([(8, 16, 1), (0, 9, 1)], 1), ([(0, 100, 1), (200, 300, 1), (99, 120, 1)], 1),
+             ([(0, 100, 0), (10, 110, 0), (20, 120, 0)], 0),               # heads of one array, interleaved
+             ([(0, 100, 0), (10, 110, 0), (0, 100, 0)], 1), ([(0, 100, 0), (50, 60, 1)], 0),
+             ([(0, 100, 1), (40, 60, 0), (90, 95, 1)], 1)]
+    body = "".join("{ std::vector<cbk::Written> w = {%s}; std::printf(\"%%d\\n\", (int)cbk::written_twice(w)); }\n" %
+                   ", ".join("{%du, %du, %s}" % (a, b, "true" if c else "false") for a, b, c in w) for w, _ in cases)
+    lines = host_program.run(tmp_path, "#include <cstdio>\n#include \"cb_ctx.cuh\"\nint main() {\n%sreturn 0; }\n" % body)
+    assert [int(x) for x in lines] == [want for _, want in cases]

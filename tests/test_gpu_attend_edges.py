@@ -60,3 +60,30 @@ def test_softmax_scales_near_zero(scale, m, T):
     tol = o.abs() * 2.0 ** -8 + A * (2.0 ** -11 + 2 * E) + 2.0 ** -32 * T * float(v.abs().max())
     assert ((c.out[0].double() - o).abs() <= tol).all()
     assert ((c.lse[0].double() - lse).abs() <= E + 2.0 ** -22 * lse.abs() + 2.0 ** -21).all()
+
+
+@pytest.mark.parametrize("m", [1, 30])
+def test_sequences_that_write_the_same_rows_are_refused(m):
+    c = Case(128, 8, 2, [m] * 3, [70, 50, 300])
+    q, o, e = c.q, c.out, c.lse
+    one = torch.full((m, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    stack, lse = torch.stack(q), torch.full((3, m, 8), 7.0, device="cuda")
+    flat = torch.full((3 * m * 8 * 128,), 7.0, dtype=torch.bfloat16, device="cuda")
+    step = m * 8 * 128 - 128                       # the last row of one sequence is the first of the next
+    for call in (lambda: c.rx.attend(c.caches, stack, one[None].expand(3, -1, -1, -1)),
+                 lambda: c.rx.attend(c.caches, q, [o[0], o[1], o[0]], lses=e),
+                 lambda: c.rx.attend(c.caches, q, o, lses=[e[0], e[0], e[2]]),
+                 lambda: c.rx.attend(c.caches, stack, torch.stack(o), lses=lse[:1].expand(3, -1, -1)),
+                 lambda: c.rx.attend(c.caches, stack, flat.as_strided((3, m, 8, 128), (step, 1024, 128, 1)))):
+        with pytest.raises(cb.CBError, match="CB_EINVAL.*same rows"):
+            call()
+    torch.cuda.synchronize()
+    assert all((x == 7).all() for x in o + e + [one, lse, flat])
+    # tokens of the sequences side by side, the other way round in memory, and a sequence without tokens
+    room = torch.full((m, 3, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    c.out = [room[:, 2 - i] for i in range(3)]
+    c.run()
+    c.check()
+    c.rx.attend(c.caches, [q[0], q[1][:0], q[2]], [o[0], o[0][:0], o[2]], lses=[e[0], e[0][:0], e[2]])
+    c.out = o
+    c.check(which=[0, 2])
