@@ -612,7 +612,8 @@ class CacheBack:
                 if t is not None and not (_is_int32(t) and t.is_contiguous() and t.numel() >= c):
                     raise ValueError("idx and rows hold an int32 a row")
             shape = K.shape
-            if not (isinstance(K, PagedKV) or (_is_bf16(K) and K.dtype == V.dtype and shape == V.shape)):
+            if not (_is_bf16(K.k_pool) and _is_bf16(K.v_pool) if isinstance(K, PagedKV) else
+                    _is_bf16(K) and K.dtype == V.dtype and shape == V.shape):
                 raise ValueError("K and V are bf16 of one shape")
             self._fits(p)
             if not (shape[1] == p.n_kv_heads and shape[3] == p.head_dim and shape[0] == layers):

@@ -68,3 +68,23 @@ def test_rows_behind_max_positions(page):
         rx.pack([K], [V], [p], [room - T + 1])
     rx.pack([K], [V], [p], [room - T])
     rx.sync_status()
+
+
+def test_pages_of_another_type_are_refused():
+    """A paged sender's fp16 rows are no bf16 numbers: refused, as a strided sender's are."""
+    Hkv, d, T = 2, 64, 32
+    rx = cb.Receiver(1, Hkv, Hkv, d, 1, T)
+    p = cb.PackedKV(*[torch.full((1, Hkv, T, w), 9, dtype=t, device="cuda")
+                      for w, t in ((d // 2, torch.uint8),) * 2 + ((d // 32, torch.bfloat16),) * 2])
+    table = torch.arange(2, dtype=torch.int32, device="cuda")
+    pool = torch.ones((1, 2, 16, Hkv, d), dtype=torch.bfloat16, device="cuda")
+    for k, v in ((pool.half(), pool.half()), (pool, pool.half()), (pool.half(), pool)):
+        paged = cb.PagedKV(k, v, table, T)
+        with pytest.raises(ValueError):
+            rx.pack([paged], [paged], [p], [0])
+    rx.sync_status()
+    assert (p.k == 9).all() and (p.v_scale == 9).all()
+    paged = cb.PagedKV(pool, pool, table, T)
+    rx.pack([paged], [paged], [p], [0])
+    rx.sync_status()
+    assert (p.k_scale == 19 / 128).all()          # 1 / 7 rounded up to five bits
