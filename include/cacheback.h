@@ -280,20 +280,22 @@ cb_status cb_stage_times(cb_ctx *ctx, float *ms, int32_t *calls);
 
 /*
  * Bounded device waits (failure detection; the paper has no counterpart: this is a runtime
- * control).  Every mbarrier wait of the tcgen05 score passes gives up after limit_ns
- * nanoseconds (default 1 s): the kernel then records which wait gave up, sets an abort flag
+ * control).  Every mbarrier wait of the tcgen05 kernels (the score passes; cb_attend with more
+ * than 16 query rows a KV head) gives up after limit_ns nanoseconds (default 1 s): the kernel then records which wait gave up, sets an abort flag
  * that every role of its CTA sees, waits (bounded) for its own copies and MMAs in flight,
  * frees its tensor memory and returns, so the context stays usable; the next cb_sync_status
- * reports CB_ETIMEOUT and that call's scores are invalid.
+ * reports CB_ETIMEOUT and that call's results are invalid.
  *   limit_ns          0 restores the default; otherwise 1e3 .. 6e10
- *   stall_next_score  1: the next cb_score that runs the tcgen05 passes makes one wait of its
+ *   stall_next        1: the next cb_score that runs the tcgen05 passes makes one wait of its
  *                     first row-statistics launch (CTA 0's MMA issuer) on a barrier nothing
  *                     arrives on, so that wait runs out after limit_ns and the path above is
  *                     taken; cleared by that call.  For tests of failure detection; it faults
  *                     and hangs nothing.  The mma.sync passes have no waits and ignore it.
+ *                     2: the same for the next cb_attend that runs the tcgen05 kernel (its block 0's
+ *                     MMA issuer); calls on the kernel of few rows, which has no waits, leave it set
  * Errors: CB_EINVAL (NULL ctx, values out of range).  Host-only; affects later calls.
  */
-cb_status cb_set_wait_limit(cb_ctx *ctx, int64_t limit_ns, int32_t stall_next_score);
+cb_status cb_set_wait_limit(cb_ctx *ctx, int64_t limit_ns, int32_t stall_next);
 
 /*
  * SMs the score kernels occupy (a runtime control; the paper has no counterpart).  The

@@ -573,15 +573,15 @@ cb_status cb_score(cb_ctx* ctx, int32_t n, const cb_kv* senders, const cb_query*
     return CB_OK;
 }
 
-cb_status cb_set_wait_limit(cb_ctx* ctx, int64_t limit_ns, int32_t stall_next_score) {
+cb_status cb_set_wait_limit(cb_ctx* ctx, int64_t limit_ns, int32_t stall_next) {
     if (!ctx) return fail(nullptr, CB_EINVAL, "ctx is NULL");
     ctx->last_error.clear();
     if (limit_ns != 0 && (limit_ns < 1000 || limit_ns > 60000000000ll))
         return fail(ctx, CB_EINVAL, "limit_ns = %lld: 0 (the default, 1 s) or 1e3 .. 6e10", (long long)limit_ns);
-    if (stall_next_score != 0 && stall_next_score != 1)
-        return fail(ctx, CB_EINVAL, "stall_next_score must be 0 or 1");
+    if (stall_next < 0 || stall_next > 2) return fail(ctx, CB_EINVAL, "stall_next must be 0, 1 or 2");
     ctx->wait_ns = limit_ns ? limit_ns : kDefaultWaitNs;
-    ctx->stall_next = stall_next_score;
+    ctx->stall_next = stall_next == 1;
+    ctx->stall_attend = stall_next == 2;
     return CB_OK;
 }
 

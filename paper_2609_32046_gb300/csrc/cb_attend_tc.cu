@@ -56,6 +56,7 @@ constexpr uint64_t kDrainNs = 1000000000ull;
 struct Ctl {
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
     uint64_t s_full[2], p_full[2], pv_done[2], done;
+    uint64_t stall;         // failure-detection test: a barrier nothing arrives on
     uint64_t wait_ns;
     uint32_t tmem;
     int abort;
@@ -302,6 +303,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
             mbar_init(&ctl->pv_done[i], 1);
         }
         mbar_init(&ctl->done, 1);
+        mbar_init(&ctl->stall, 1);
         ctl->wait_ns = b.wait_ns;
         ctl->abort = 0;
         fence_barrier_init();
@@ -371,7 +373,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
                 const uint32_t hi = (uint32_t)(smem_desc_sw128(0) >> 32), lo = (uint32_t)smem_desc_sw128(0);
                 const uint32_t q0 = (smem_u32(sq) >> 4) + lo, k0 = (smem_u32(sk) >> 4) + lo, v0 = (smem_u32(sv) >> 4) + lo;
                 const int tiles0 = ctl->tiles;
-                bool ok = true;
+                bool ok = !b.stall || blockIdx.x || wait(&ctl->stall, 0, ctl, b.err, 8);
                 auto score = [&](int i) {               // S of item i
                     const int h = i & 1, j = tiles0 + (both ? i >> 1 : i);
                     if (!wait(&ctl->k_full[j % kStages], (j / kStages) & 1, ctl, b.err, 0)) return false;
@@ -734,7 +736,9 @@ cudaError_t launch(const AttendBatch& b, int blocks, cudaStream_t st) {
 cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
     const int64_t units = attend_pairs(b, kRowTile);
     const int blocks = (int)(units < num_sms ? units : num_sms);
-    return head_dim == 128 ? launch<128>(b, blocks, st) : launch<64>(b, blocks, st);
+    const cudaError_t e = head_dim == 128 ? launch<128>(b, blocks, st) : launch<64>(b, blocks, st);
+    b.stall = 0;
+    return e;
 }
 
 }  // namespace cbk

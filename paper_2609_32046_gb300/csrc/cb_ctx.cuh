@@ -49,6 +49,7 @@ struct cb_ctx {
     int32_t score_path = 0;         // kernels of the last cb_score: 2 tcgen05, 1 mma.sync, 0 none yet
     int64_t wait_ns = cbk::kDefaultWaitNs;   // limit of one bounded device wait (tcgen05 passes)
     int32_t stall_next = 0;         // failure-detection test: stall the next cb_score once
+    int32_t stall_attend = 0;       // the same for the next cb_attend on the tcgen05 kernel
     int32_t score_sms = 0;          // SMs of the persistent score kernels (0: all)
     bool receiver = false;          // no scratch for cb_score and cb_select
     float* attend_part = nullptr;   // cb_attend: partial results (outputs; maxima and sums)

@@ -305,6 +305,7 @@ struct AttendBatch {
     int32_t* tickets;         // kFewTickets a block of k_attend_few, zero between calls
     AttendCut* cuts;          // one a block of k_attend_tc
     int32_t pairs;            // row tiles of all sequences
+    int32_t stall;            // failure-detection test: one wait of k_attend_tc that nothing completes; 0 once it ran
     uint64_t wait_ns;
     AttendSpan span[kMaxBatch];
     AttendSeq s[kMaxBatch];

@@ -402,6 +402,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         b.tickets = ctx->attend_tickets;
         b.cuts = ctx->attend_cuts;
         b.wait_ns = (uint64_t)ctx->wait_ns;
+        b.stall = ctx->stall_attend;
         for (int k = 0; k < b.n; ++k) {
             const cb_packed& p = caches[some[b0 + k]];
             const cb_attend_query& q = queries[some[b0 + k]];
@@ -421,6 +422,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
             s.o_tok = q.o_tok; s.o_head = q.o_head;
         }
         const cudaError_t e = launch_attend(b, d, strm, ctx->num_sms);
+        ctx->stall_attend = b.stall;
         if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "attend launch failed: %s", cudaGetErrorString(e));
     }
     return CB_OK;

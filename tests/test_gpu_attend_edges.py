@@ -87,3 +87,30 @@ def test_sequences_that_write_the_same_rows_are_refused(m):
     c.rx.attend(c.caches, [q[0], q[1][:0], q[2]], [o[0], o[0][:0], o[2]], lses=[e[0], e[0][:0], e[2]])
     c.out = o
     c.check(which=[0, 2])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m,Ts", [(20, [300]), (20, [6000, 40, 1]), (40, [300]), (100, [6000, 500])])
+def test_a_bounded_wait_gives_up_and_the_context_recovers(d, m, Ts):
+    """Failure detection without a GPU fault: the warp that issues the products waits on a barrier that nothing arrives
+    on.  After the limit it gives up, every role leaves its loop and meets the others, tensor memory is freed, and
+    the host reads CB_ETIMEOUT; the same context's next call is right.  (One row tile's two streams, by tiles
+    of up to 128 rows and by halves of more; segments of one block and of many.)"""
+    c = Case(d, 8, 2, [m] * len(Ts), Ts, seed=m)
+    one = Case(d, 8, 2, [1], [100])
+    for _ in range(2):
+        c.rx.set_wait_limit(20_000_000, stall_next_attend=True)          # 20 ms
+        c.rx.attend(one.caches, one.q, one.out, lses=one.lse)            # the kernel of few rows has no waits
+        c.rx.sync_status()
+        one.check()
+        c.run()
+        with pytest.raises(cb.CBError, match="gave up") as e:
+            c.rx.sync_status()
+        assert e.value.status == cb.CB_ETIMEOUT
+        for x in c.out + c.lse:
+            x.fill_(7)
+        c.run()                                    # the stall was for one call; ordinary waits stay far below the limit
+        c.check()
+    with pytest.raises(ValueError):
+        c.rx.set_wait_limit(0, stall_next_score=True, stall_next_attend=True)
+    assert c.rx.lib.cb_set_wait_limit(c.rx.h, 0, 3) == cb.CB_EINVAL
