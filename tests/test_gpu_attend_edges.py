@@ -114,3 +114,73 @@ def test_a_bounded_wait_gives_up_and_the_context_recovers(d, m, Ts):
     with pytest.raises(ValueError):
         c.rx.set_wait_limit(0, stall_next_score=True, stall_next_attend=True)
     assert c.rx.lib.cb_set_wait_limit(c.rx.h, 0, 3) == cb.CB_EINVAL
+
+
+@pytest.mark.parametrize("m", [1, 4, 50, 100])
+def test_a_second_run_writes_every_row_again(m):
+    """The same bits from a second run, on another stream and out of a captured graph, over outputs that were
+    overwritten in between; the outputs of the joins among them."""
+    c = Case(128, 32, 8, [m] * 3, [9000, 100, 1999], page=16)
+    c.run()
+    torch.cuda.synchronize()
+    want = [x.clone() for x in c.out + c.lse]
+    c.check()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.run()
+    for stream, run in ((side, lambda: c.run(stream=side)), (side, graph.replay), (torch.cuda.current_stream(), c.run)):
+        with torch.cuda.stream(stream):
+            for x in c.out + c.lse:
+                x.fill_(7)
+            run()
+        stream.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, c.out + c.lse))
+    c.rx.sync_status()
+
+
+@pytest.mark.parametrize("m", [2, 40])
+def test_two_contexts_on_two_streams_write_their_own(m):
+    """Two contexts at once over the same caches: every round's outputs and log-sum-exps are overwritten before it."""
+    a = Case(128, 8, 2, [m, m], [9000, 700])
+    b = Case(128, 8, 2, [m, m], [9000, 700])
+    b.q, b.caches = a.q, a.caches
+    a.run()
+    a.check()
+    want = [x.clone() for x in a.out + a.lse]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        for s, c in zip(streams, (a, b)):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                for x in c.out + c.lse:
+                    x.fill_(7)
+                for _ in range(4):
+                    c.run()
+        torch.cuda.synchronize()
+        for c in (a, b):
+            assert all(torch.equal(x, y) for x, y in zip(want, c.out + c.lse))
+    a.rx.sync_status()
+    b.rx.sync_status()
+
+
+@pytest.mark.parametrize("m", [1, 70])
+def test_graphs_that_share_a_context_write_every_row(m):
+    a = Case(128, 8, 2, [m, 1], [5000, 33])
+    b = Case(128, 8, 2, [m], [2222])
+    b.rx = a.rx
+    graphs = []
+    for c in (a, b):
+        c.run()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.run()
+        graphs.append(g)
+    for _ in range(3):
+        for x in a.out + a.lse + b.out + b.lse:
+            x.fill_(7)
+        for g in graphs:
+            g.replay()
+        a.check()
+        b.check()
