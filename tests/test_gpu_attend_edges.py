@@ -184,3 +184,48 @@ def test_graphs_that_share_a_context_write_every_row(m):
             g.replay()
         a.check()
         b.check()
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 4, 1), (64, 8, 2), (128, 2, 2)])
+@pytest.mark.parametrize("m,T,window", [(1024, 1024, 0), (1024, 3001, 0), (1023, 5000, 700), (769, 500, 0)])
+def test_as_many_tokens_as_a_context_takes(d, Hq, Hkv, m, T, window):
+    """Up to sixteen row tiles a sequence; more tokens than rows as well."""
+    c = Case(d, Hq, Hkv, [m], [T], seed=m)
+    c.run(window=window)
+    c.check(window=window)
+    c.run(causal=False)
+    c.check(causal=False)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_as_many_row_tiles_as_a_launch_takes(d):
+    """64 sequences of 1024 tokens in groups of 4: 1024 row tiles."""
+    c = Case(d, 4, 1, [1024] * 64, [1 + 37 * i for i in range(64)], page=16)
+    c.run()
+    c.check()
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 32, 8), (128, 8, 8), (64, 32, 8), (64, 16, 16)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 300), (False, 0)])
+def test_more_items_than_blocks(d, Hq, Hkv, causal, window):
+    """More items (row tile, KV head) than blocks: runs end inside items, and those are joined by the block that they
+    begin in."""
+    n = 24
+    c = Case(d, Hq, Hkv, [33 + 3 * (i % 5) for i in range(n)], [40 + 97 * i for i in range(n)], page=32, seed=d)
+    for _ in range(2):
+        for x in c.out + c.lse:
+            x.fill_(7)
+        c.run(causal=causal, window=window)
+        c.check(causal=causal, window=window)
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 32, 8), (64, 8, 4)])
+@pytest.mark.parametrize("longest", [3, 9, 64, 300])
+@pytest.mark.parametrize("window", [0, 129])
+def test_token_counts_that_differ(d, Hq, Hkv, longest, window):
+    """A batch of decoding sequences with one of more tokens among them."""
+    ms = [1] * 12 + [longest, 2, 0, 1]
+    Ts = [1 + 233 * i for i in range(12)] + [longest + 900, 1, 50, 2000]
+    c = Case(d, Hq, Hkv, ms, Ts, page=16, seed=longest)
+    c.run(window=window)
+    c.check(window=window)
