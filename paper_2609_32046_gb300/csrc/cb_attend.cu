@@ -13,7 +13,7 @@
 #include <cuda_runtime.h>
 
 #include "cb_attend.cuh"
-#include "cb_internal.cuh"
+#include "cb_receiver.cuh"
 
 namespace cbk {
 namespace {

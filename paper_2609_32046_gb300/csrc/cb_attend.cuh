@@ -7,8 +7,8 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
-#include "cb_internal.cuh"
-#include "cb_sm100.cuh"
+#include "cb_receiver.cuh"
+#include "cb_sm100_attend.cuh"
 
 namespace cbk {
 

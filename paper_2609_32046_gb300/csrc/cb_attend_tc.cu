@@ -31,8 +31,8 @@
 #include <cuda_runtime.h>
 
 #include "cb_attend.cuh"
-#include "cb_internal.cuh"
-#include "cb_sm100.cuh"
+#include "cb_receiver.cuh"
+#include "cb_sm100_attend.cuh"
 
 namespace cbk {
 namespace {

@@ -10,7 +10,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "cacheback.h"
-#include "cb_internal.cuh"
+#include "cb_receiver.cuh"
 
 namespace cbk {
 constexpr int64_t kDefaultWaitNs = 1000000000;   // 1 s

@@ -11,7 +11,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
-#include "cb_internal.cuh"
+#include "cb_receiver.cuh"
 
 namespace cbk {
 namespace {

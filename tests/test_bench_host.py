@@ -45,3 +45,13 @@ def test_committed_summaries_name_a_full_hash_and_a_byte_count():
         assert re.search(r"traffic_bytes_per_launch:\s*[0-9]+\b", text), name
     assert found >= 2
     assert bench.KERNEL_SOURCES == ("cb_score_tc.cu", "cb_sm100.cuh", "cb_internal.cuh")
+
+
+def test_the_profiled_sources_belong_to_the_score_kernels():
+    """What the hash covers holds nothing of the calls beside cb_score: a change to those would end the traffic
+    figures, although the profiled kernels are as they were."""
+    bench = _bench()
+    import re
+    for name in bench.KERNEL_SOURCES:
+        text = open(os.path.join(ROOT, "paper_2609_32046_gb300", "csrc", name)).read()
+        assert not re.search(r"rotary|packed_row|cb_pack|cb_attend|attendbatch|setmaxnreg", text, re.I), name
