@@ -516,7 +516,9 @@ typedef struct {
  * size): and no rows at or below position - window.  Otherwise r sees all L rows.  A token that sees no row gets
  * out = 0 and lse = -infinity.  Logits, weights' sums and outputs are summed in fp32, weights enter
  * their product with the values as fp16 scaled to the row's largest, and out is rounded once to bf16.  With lse a caller joins
- * attention over several caches.  m may differ between sequences; m = 0 skips a sequence.
+ * attention over several caches.  m may differ between sequences (m = 0 skips one), but the longest decides
+ * the kernel for all of a call's: decoding sequences take less time in a call of their own than in one with a
+ * sequence of more than 16 query rows (m * G) a KV head.
  *   caches    T <= max_positions; sequences may share one cache
  * Errors: CB_EINVAL, CB_ESHAPE (n above max_senders, m above max_query_tokens, T above max_positions,
  * layer), CB_ENOMEM (no room for the partial results: see cb_create_receiver; a first call inside a
