@@ -527,6 +527,123 @@ typedef struct {
 cb_status cb_attend(cb_ctx *ctx, int32_t layer, int32_t n, const cb_packed *caches, const cb_attend_query *queries,
                     int32_t causal, int64_t window, void *stream);
 
+/*
+ * ---- Drafted tokens and a budget: a tree's attention, gathered weights, eviction, kept rows ----
+ *
+ * What a receiver needs that drafts several tokens at a time (cb_attend_tree, then cb_keep of those it
+ * accepts) and that holds its 4-bit cache to a number of rows (cb_weigh after cb_attend, cb_evict now and
+ * then).  Positions are in the keys, so rows of a cache may be moved and left out freely.
+ */
+
+/* What the m query tokens of a sequence see of one another's rows: token r sees token u's where bit u % 32
+ * of seen[r * s_row + u / 32] is set (device, 4-byte aligned, ceil(m / 32) words a token; bits from m on are
+ * not looked at).  Any bits will do: a tree's (each token its ancestors and itself), several trees', none.
+ * seen NULL: each token sees those up to itself.  s_row >= ceil(m / 32) where m > 1. */
+typedef struct {
+    const uint32_t *seen;
+    int64_t s_row;
+} cb_tree;
+
+/*
+ * cb_attend of drafted tokens: the m tokens' own rows are the last m of the L rows in the cache, token u's
+ * is row L - m + u (pack them first), and token r sees every row before them, and of them what trees[i] says.
+ * Where L < m the tokens u < m - L have no rows, and nothing is seen of them.  Everything else is as in
+ * cb_attend (causal, without a window), whose results those of a sequence without bits are.
+ * Errors as cb_attend, and CB_EINVAL (trees NULL, bits misaligned, s_row).
+ */
+cb_status cb_attend_tree(cb_ctx *ctx, int32_t layer, int32_t n, const cb_packed *caches, const cb_attend_query *queries,
+                         const cb_tree *trees, void *stream);
+
+/* Query tokens of one sequence whose attention weights are gathered: Q[r][h][:] at q + r*s_tok + h*s_head, r < m,
+ * and lse (fp32 [m][n_q_heads], contiguous, 4-byte aligned) as cb_attend or cb_attend_tree wrote it.  What the
+ * rows had gathered, before[g * b_head + t], and what they have now, weights[g * w_head + t] (fp32, 4-byte
+ * aligned, t below the cache's T): the same memory with the same strides, or memory that does not touch.
+ * before NULL: nothing yet.  fresh >= 0: so many rows at the cache's end have gathered nothing yet, and
+ * before is not read there (m for tokens whose rows have just been packed). */
+typedef struct {
+    const void *q;
+    const float *lse;
+    const float *before;
+    float *weights;
+    int32_t m;
+    int64_t fresh;
+    int64_t s_tok, s_head;
+    int64_t b_head, w_head;
+} cb_weigh_query;
+
+/*
+ * Gather one layer's attention weights: for the rows t < L of every cache and its KV heads g
+ *     weights[g][t] = decay * before[g][t] + sum_r sum_h exp(softmax_scale * <q_{r,h}, k_t> - lse[r][h])
+ * over the query heads h of KV head g (h / G = g) and the tokens r that see row t, which is as in cb_attend (causal, window) or, with
+ * trees, as in cb_attend_tree.  A token's head whose lse is not finite adds nothing: what saw no row, and
+ * what a caller leaves out by setting its lse to infinity (drafts that were not accepted).  Weights of rows
+ * from L on are not written.  Sums are fp32, in a fixed order.
+ * m = 0 skips a sequence.
+ *   trees   NULL, or one a sequence (then causal = 1 and window = 0)
+ *   decay   within 0 .. 1
+ * Errors: as cb_attend; CB_EINVAL for decay, fresh, strides of weights that overlap, or two sequences that write the same.
+ */
+cb_status cb_weigh(cb_ctx *ctx, int32_t layer, int32_t n, const cb_packed *caches, const cb_weigh_query *queries,
+                   const cb_tree *trees, int32_t causal, int64_t window, float decay, void *stream);
+
+/* How one cache is held to `keep` rows.  weights: fp32, row t of layer l (from the first layer of the call on) and KV head g
+ * at weights + l*w_layer + g*w_head + t; they move with the rows to weights_to (rows in place: the same memory with the
+ * same strides; rows into another cache: memory that does not touch it, with its own; NULL: they do not move).
+ *   first, last   rows at the cache's beginning and end that always stay; first + last <= keep
+ *   idx           device int32 [n_layers][n_kv_heads][keep], 4-byte aligned, written: the rows that stay, ascending;
+ *                 -1 behind them where the cache has fewer than `keep`
+ *   length        device int32 (4-byte aligned) or NULL: receives the number of rows kept.  It may be the
+ *                 cache's own length */
+typedef struct {
+    const float *weights;
+    float *weights_to;
+    int64_t w_layer, w_head, t_layer, t_head;
+    int64_t keep, first, last;
+    int32_t *idx;
+    int32_t *length;
+} cb_eviction;
+
+/*
+ * Eviction: in every layer [layer, layer + n_layers) and KV head, of the L rows in caches[i] (T, or *length as
+ * it is when the kernel runs) min(L, keep) stay: the first `first`, the last `last` and of the others those
+ * of the largest weights, ties to the lowest row, NaN below every number.  They become rows 0, 1, ... in
+ * their order; every head has rows of its own.  Rows behind them stay as they are.
+ *   into   NULL: in the cache itself; or the cache that receives the rows, whose T is at least keep or
+ *          caches[i].T.  into[i] that names caches[i]'s own codes of K is in place too and has to be its equal;
+ *          another's memory may not touch that of any cache of the call
+ * A block-table entry outside [0, n_pages) leaves its rows out and is reported by cb_sync_status as CB_EDEVICE.
+ * Errors: CB_EINVAL (also a cache or a length that is written twice, a length that is written and another cache's), CB_ESHAPE
+ * (layers, T, keep), CB_EBUDGET (first + last above keep, into too small).
+ */
+cb_status cb_evict(cb_ctx *ctx, int32_t layer, int32_t n_layers, int32_t n, const cb_packed *caches, const cb_packed *into,
+                   const cb_eviction *evictions, void *stream);
+
+/* Rows of one cache that stay of its last `drafted`: idx[j] (device int32 [count], 4-byte aligned), counted from
+ * the first of them, ascending; j < min(max(*n_kept, 0), count) where n_kept (device int32) is given, else
+ * j < count.  weights (fp32, row t of layer l and head g at weights + l*w_layer + g*w_head + t; or NULL) move
+ * with them.  length (device int32 or NULL) receives L - drafted + their number; it may be the cache's own. */
+typedef struct {
+    const int32_t *idx;
+    int64_t count;
+    const int32_t *n_kept;
+    int64_t drafted;
+    float *weights;
+    int64_t w_layer, w_head;
+    int32_t *length;
+} cb_kept;
+
+/*
+ * Keep some of a cache's last rows, in the cache, all layers and KV heads alike: with L rows in it (T, or
+ * *length as it is when the kernel runs), row L - drafted + j becomes what row L - drafted + idx[j] was.
+ * After cb_attend_tree: idx is the accepted path; with drafted = T: the rows that stay of a message.
+ * idx[j] has to lie in j .. drafted - 1 (what an ascending list does): an entry that does not, and a
+ * block-table entry outside [0, n_pages), skips its row and is reported by cb_sync_status as CB_EDEVICE, as is a
+ * cache of fewer than `drafted` rows, of which nothing is moved or written.  The rest of the cache stays as it is.
+ * Errors: CB_EINVAL (also a cache that is given twice, lengths as in cb_evict), CB_ESHAPE, CB_EBUDGET (count not within 0 .. drafted,
+ * drafted above T).
+ */
+cb_status cb_keep(cb_ctx *ctx, int32_t n, const cb_packed *caches, const cb_kept *kept, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,10 +15,10 @@ from typing import List, Optional, Sequence
 
 from .binding import (CB_EBUDGET, CB_ECUDA, CB_EDEVICE, CB_EINVAL, CB_ENOMEM, CB_ESHAPE, CB_ETIMEOUT, CB_OK, EXPORTED,
                       LIB_PATH, CacheBack, CBError, PackedKV, PagedKV, Receiver, Rotary, budget, chain_budget,
-                      load_library)
+                      load_library, pack_words, tree_words)
 
 __all__ = ["CacheBack", "CBError", "PagedKV", "budget", "chain_budget", "load_library", "LIB_PATH", "EXPORTED",
-           "Filter", "Chain", "Receiver", "PackedKV", "Rotary",
+           "Filter", "Chain", "Receiver", "PackedKV", "Rotary", "tree_words", "pack_words",
            "CB_OK", "CB_EINVAL", "CB_ESHAPE", "CB_EBUDGET", "CB_ENOMEM", "CB_ECUDA", "CB_ETIMEOUT", "CB_EDEVICE"]
 
 

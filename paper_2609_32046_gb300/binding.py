@@ -24,7 +24,8 @@ EXPORTED = ["cb_config_init", "cb_create", "cb_score", "cb_budget", "cb_select",
             "cb_sync_status", "cb_destroy", "cb_last_error", "cb_scratch_bytes", "cb_score_path", "cb_select_noalloc",
             "cb_select_noalloc_status", "cb_gather", "cb_chain_budget", "cb_compact_rope",
             "cb_enable_stage_timing", "cb_stage_times", "cb_set_wait_limit", "cb_set_score_sms",
-            "cb_create_receiver", "cb_rotary", "cb_pack", "cb_unpack", "cb_attend"]
+            "cb_create_receiver", "cb_rotary", "cb_pack", "cb_unpack", "cb_attend", "cb_attend_tree", "cb_weigh", "cb_evict",
+            "cb_keep"]
 
 
 class CBError(RuntimeError):
@@ -141,6 +142,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.cb_unpack.restype = ctypes.c_int
     lib.cb_attend.argtypes = [P, ctypes.c_int32, ctypes.c_int32, P, P, ctypes.c_int32, ctypes.c_int64, P]
     lib.cb_attend.restype = ctypes.c_int
+    lib.cb_attend_tree.argtypes = [P, ctypes.c_int32, ctypes.c_int32, P, P, P, P]
+    lib.cb_attend_tree.restype = ctypes.c_int
+    lib.cb_weigh.argtypes = [P, ctypes.c_int32, ctypes.c_int32, P, P, P, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, P]
+    lib.cb_weigh.restype = ctypes.c_int
+    lib.cb_evict.argtypes = [P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, P, P, P, P]
+    lib.cb_evict.restype = ctypes.c_int
+    lib.cb_keep.argtypes = [P, ctypes.c_int32, P, P, P]
+    lib.cb_keep.restype = ctypes.c_int
     if path is None:
         _LIB = lib
     return lib
@@ -428,6 +437,48 @@ class Rotary:
         return self._c[1 if inverse else 0]
 
 
+def tree_words(parents, device=None):
+    """What drafted tokens see of one another (CacheBack.attend's `trees`) as int32 words [..][m][ceil(m / 32)]: each
+    itself and its ancestors.  parents: int array or nested list [..][m], parents[r] < r the token that r
+    follows, -1 for one that follows the cache's last row."""
+    import torch
+    p = torch.as_tensor(parents, dtype=torch.int64, device="cpu")
+    _require(p.dim() >= 1 and bool(((p >= -1) & (p < torch.arange(p.shape[-1]))).all()), "a token follows an earlier one, or -1")
+    m = p.shape[-1]
+    flat = p.reshape(-1, m)
+    seen = torch.zeros((flat.shape[0], m, m), dtype=torch.bool)
+    at = torch.arange(flat.shape[0])
+    for r in range(m):
+        up = flat[:, r]
+        seen[:, r] = seen[at, up] & (up >= 0)[:, None]
+        seen[:, r, r] = True
+    return pack_words(seen.reshape(p.shape + (m,))).to(device)
+
+
+def pack_words(seen):
+    """Bits [..][m][m] (bool: token r sees token u) as int32 words [..][m][ceil(m / 32)], on the same device."""
+    import torch
+    x = torch.nn.functional.pad(seen.long(), (0, -seen.shape[-1] % 32)).unflatten(-1, (-1, 32))
+    w = (x << torch.arange(32, device=seen.device)).sum(-1)
+    return torch.where(w >= 1 << 31, w - (1 << 32), w).to(torch.int32)
+
+
+def _is_f32(x) -> bool:
+    return x.element_size() == 4 and x.dtype.is_floating_point
+
+
+def _each(x, n: int, what: str) -> list:
+    """One entry a sequence: of a list, or a number's or None's n times."""
+    if isinstance(x, (list, tuple)):
+        _require(len(x) == n, "one %s per cache" % what)
+        return list(x)
+    return [x] * n
+
+
+def _address(x) -> int:
+    return 0 if x is None else x.data_ptr()
+
+
 def _require(ok: bool, message: str):
     if not ok:
         raise ValueError(message)
@@ -657,12 +708,18 @@ class CacheBack:
                                        ost[0], ost[1], _stream_on(stream, k_out)))
 
     def attend(self, caches: Sequence, Qs: Sequence, outs: Sequence, layer: int = 0, causal: bool = True, window: int = 0,
-               lses: Optional[Sequence] = None, stream=None):
+               lses: Optional[Sequence] = None, stream=None, trees: Optional[Sequence] = None):
         """One layer's attention over 4-bit caches: outs[i] (bf16 [m][Hq][d]) of query tokens Qs[i] (bf16
         [m][Hq][d]), the last m positions of caches[i] (causal: each sees the rows up to its own, the last
         `window` of them where window > 0; otherwise all); lses[i] (fp32 [m][Hq], contiguous) receives the
-        log-sum-exp.  Qs, outs and lses may be tensors with the sequences in their first dimension."""
+        log-sum-exp.  Qs, outs and lses may be tensors with the sequences in their first dimension.
+        trees: drafted tokens, causal and without a window: token r sees every row before the m last, and of
+        those token u's where bit u % 32 of word trees[i][r][u / 32] is set (int32 [m][words]: tree_words; None: up to
+        its own)."""
         n = len(caches)
+        if trees is not None:
+            _require(causal and not window, "trees go with causal and no window")
+            _require(len(trees) == n, "one tree (or None) per cache")
         cfg, like = self.cfg, self._shape
         for p in caches:
             if p._shape != like:
@@ -692,8 +749,167 @@ class CacheBack:
             fields = array("q")
             for i in range(n):
                 fields.extend(self._queries(Qs[i], outs[i], None if lses is None else lses[i]))
+        if trees is not None:
+            bits = self._trees(trees, fields[3::8])
+            self._check(self.lib.cb_attend_tree(self.h, int(layer), n, held, fields.buffer_info()[0], bits.buffer_info()[0],
+                                                _stream_on(stream, caches[0].k) if n else 0))
+            return
         self._check(self.lib.cb_attend(self.h, int(layer), n, held, fields.buffer_info()[0], 1 if causal else 0, int(window),
                                        _stream_on(stream, caches[0].k) if n else 0))
+
+    def _trees(self, trees, ms):
+        """The header's cb_tree of every sequence, as eight-byte numbers."""
+        bits = array("q")
+        if hasattr(trees, "data_ptr"):
+            shape, st = trees.shape, trees.stride()
+            m = max(ms, default=0)
+            _require(_is_int32(trees) and len(shape) == 3 and min(ms, default=0) == m == shape[1] and 32 * shape[2] >= m and
+                     (st[2] == 1 or shape[2] == 1), "trees are int32 [sequences][m][words]")
+            at = trees.data_ptr()
+            for i in range(len(ms)):
+                bits.extend((at + 4 * i * st[0], st[1]))
+            return bits
+        for t, m in zip(trees, ms):
+            if t is None:
+                bits.extend((0, 0))
+                continue
+            _require(_is_int32(t) and t.dim() == 2 and t.shape[0] == m and 32 * t.shape[1] >= m and
+                     (t.stride(1) == 1 or t.shape[1] == 1), "trees are int32 [m][words]")
+            bits.extend((t.data_ptr(), t.stride(0)))
+        return bits
+
+    def weigh(self, caches: Sequence, Qs: Sequence, lses: Sequence, weights: Optional[Sequence], layer: int = 0, causal: bool = True,
+              window: int = 0, trees: Optional[Sequence] = None, fresh=None, decay: float = 1.0, outs: Optional[Sequence] = None,
+              stream=None):
+        """Gather one layer's attention weights: row t of KV head g of caches[i] has gathered
+            outs[i][g][t] = decay * weights[i][g][t] + sum of exp(scale <q, k_t> - lse)
+        over the tokens of Qs[i] (bf16 [m][Hq][d]) that see it and the heads of its group, with lses[i] (fp32 [m][Hq],
+        contiguous) as attend wrote them; a head whose lse is not finite adds nothing.  weights[i], outs[i]: fp32
+        [Hkv][rows], in place where outs or outs[i] is None; weights None: nothing gathered yet (then outs are given).
+        causal, window and trees as in attend.  fresh (a number, or one per cache; None: m): rows at the cache's end
+        that have gathered nothing yet.  All of them may be tensors with the sequences in their first dimension.
+        Returns outs."""
+        n = len(caches)
+        cfg = self.cfg
+        _require(len(Qs) == len(lses) == n and (weights is None or len(weights) == n) and (outs is None or len(outs) == n) and
+                 (trees is None or len(trees) == n), "one entry per cache in every list")
+        _require(weights is not None or outs is not None, "weights or outs")
+        _require(not window or causal, "a window goes with causal")
+        _require(trees is None or (causal and not window), "trees go with causal and no window")
+        fresh = _each(fresh, n, "fresh")
+        fields = array("q")                   # of the header's cb_weigh_query, eight bytes each
+        given = []
+        for i, p in enumerate(caches):
+            self._fits(p)
+            Q, lse = Qs[i], lses[i]
+            before = None if weights is None else weights[i]
+            out = before if outs is None or outs[i] is None else outs[i]
+            shape, qt = Q.shape, Q.stride()
+            if not (len(shape) == 3 and shape[1] == cfg.n_q_heads and shape[2] == cfg.head_dim and qt[2] == 1 and _is_bf16(Q)):
+                raise ValueError("queries are bf16 [m][Hq][d]")
+            if not (lse.shape == shape[:2] and lse.is_contiguous() and _is_f32(lse)):
+                raise ValueError("lse is fp32 [m][Hq]")
+            if out is None:
+                raise ValueError("weights or outs")
+            for x in (out,) if before is None else (out, before):
+                if not (x.dim() == 2 and _is_f32(x) and x.shape[0] == p.n_kv_heads and x.shape[1] >= p.T and
+                        (x.stride(1) == 1 or x.shape[1] == 1)):
+                    raise ValueError("weights are fp32 [Hkv][rows], rows for all that the cache holds")
+            m = shape[0]
+            fields.extend((Q.data_ptr(), lse.data_ptr(), _address(before), out.data_ptr(), m, m if fresh[i] is None else int(fresh[i]),
+                           qt[0], qt[1], 0 if before is None else before.stride(0), out.stride(0)))
+            given.append(out)
+        held = b"".join([p._state[1] or p._described() for p in caches])
+        bits = None if trees is None else self._trees(trees, fields[4::10])
+        self._check(self.lib.cb_weigh(self.h, int(layer), n, held, fields.buffer_info()[0], None if bits is None else bits.buffer_info()[0],
+                                      1 if causal else 0, int(window), float(decay), _stream_on(stream, caches[0].k) if n else 0))
+        return given if outs is None else outs
+
+    def evict(self, caches: Sequence, weights: Sequence, keep, first: int = 0, last: int = 0, into: Optional[Sequence] = None,
+              weights_into: Optional[Sequence] = None, idx: Optional[Sequence] = None, lengths: Optional[Sequence] = None,
+              layer: int = 0, stream=None):
+        """Hold caches to `keep` rows (a number, or one per cache) in the layers from `layer` on, as many as weights have:
+        of each layer and KV head the first `first` rows, the last `last` and the heaviest of the others
+        stay, by weights[i] (fp32 [layers][Hkv][rows]), ties to the lowest, in their order.  They become the
+        first rows of the cache itself, weights with them, or of into[i] (another PackedKV) and weights_into[i] (fp32
+        [layers][Hkv][keep or more]; None: weights do not move).  idx[i] (int32 [layers][Hkv][keep], contiguous) receives the
+        rows that stayed, -1 behind them.  lengths[i] (int32, one element) receives their number; lengths None:
+        the receiving cache's own `length`, where it has one, and its T becomes min(T, keep) where it has none.
+        Evict all layers in one call, or give lengths of their own to all calls but the last.  Returns idx."""
+        n = len(caches)
+        _require(len(weights) == n and all(x is None or len(x) == n for x in (into, weights_into, idx, lengths)),
+                 "one entry per cache in every list")
+        _require(into is not None or weights_into is None, "weights move where the rows do")
+        keep = [int(k) for k in _each(keep, n, "keep")]
+        targets = caches if into is None else into
+        if idx is None:
+            import torch
+            idx = [torch.empty(tuple(w.shape[:2]) + (k,), dtype=torch.int32, device=p.device) for w, k, p in zip(weights, keep, caches)]
+        layers = weights[0].shape[0] if n else 0
+        fields, left = array("q"), []         # of the header's cb_eviction, eight bytes each
+        for i, (p, to, w, k) in enumerate(zip(caches, targets, weights, keep)):
+            self._fits(p)
+            self._fits(to)
+            out = w if to is p else None if weights_into is None else weights_into[i]
+            for x, rows in ((w, p.T),) if out is None or out is w else ((w, p.T), (out, min(k, p.T))):
+                if not (x.dim() == 3 and _is_f32(x) and x.shape[0] == layers and x.shape[1] == p.n_kv_heads and x.shape[2] >= rows and
+                        (x.stride(2) == 1 or x.shape[2] == 1)):
+                    raise ValueError("weights are fp32 [layers][Hkv][rows]")
+            at = idx[i]
+            if not (_is_int32(at) and at.is_contiguous() and tuple(at.shape) == (layers, p.n_kv_heads, k)):
+                raise ValueError("idx is int32 [layers][Hkv][keep]")
+            own = to.length if lengths is None else lengths[i]
+            _require(own is None or (_is_int32(own) and own.numel() == 1), "a length is one int32")
+            _require(own is not None or p.length is None, "a length on the device needs one that receives the rows kept")
+            left.append(own)
+            ws, ts = w.stride(), (0, 0) if out is None else out.stride()
+            fields.extend((w.data_ptr(), _address(out), ws[0], ws[1], ts[0], ts[1], k, int(first), int(last), at.data_ptr(), _address(own)))
+        held = b"".join([bytes(p.desc()) for p in caches])
+        taken = None if into is None else b"".join([bytes(p.desc() if p is q else p.desc(p.capacity)) for p, q in zip(into, caches)])
+        self._check(self.lib.cb_evict(self.h, int(layer), int(layers), n, held, taken, fields.buffer_info()[0],
+                                      _stream_on(stream, caches[0].k) if n else 0))
+        if lengths is None:
+            for p, to, k, own in zip(caches, targets, keep, left):
+                if own is None:
+                    to.T = min(p.T, k)
+        return idx
+
+    def keep(self, caches: Sequence, idx: Sequence, drafted, counts: Optional[Sequence] = None, weights: Optional[Sequence] = None,
+             lengths: Optional[Sequence] = None, stream=None):
+        """Keep some of the last `drafted` rows (a number, or one per cache) of caches, every layer and head: row
+        L - drafted + j becomes what row L - drafted + idx[i][j] was (int32 device tensors, ascending: the accepted
+        path of drafted tokens).  counts[i] (int32, one element): how many of idx[i] count, as it is when the kernel
+        runs; None: all.  weights[i] (fp32 [layers][Hkv][rows]) move with the rows.  lengths[i] (int32, one element)
+        receives the number of rows; lengths None: the cache's own `length`, where it has one, and T becomes
+        it where it has none (counts then are None too).  idx, counts and weights may be tensors with the sequences in their first
+        dimension."""
+        n = len(caches)
+        _require(len(idx) == n and all(x is None or len(x) == n for x in (counts, weights, lengths)), "one entry per cache in every list")
+        drafted = [int(x) for x in _each(drafted, n, "drafted")]
+        fields, left = array("q"), []         # of the header's cb_kept, eight bytes each
+        for i, p in enumerate(caches):
+            self._fits(p)
+            x, count = idx[i], None if counts is None else counts[i]
+            if not (_is_int32(x) and x.dim() == 1 and x.is_contiguous()):
+                raise ValueError("idx holds an int32 a row")
+            _require(count is None or (_is_int32(count) and count.numel() == 1), "a count is one int32")
+            w = None if weights is None else weights[i]
+            if w is not None and not (w.dim() == 3 and _is_f32(w) and w.shape[0] == p.n_layers and w.shape[1] == p.n_kv_heads and
+                                      w.shape[2] >= p.T and (w.stride(2) == 1 or w.shape[2] == 1)):
+                raise ValueError("weights are fp32 [layers][Hkv][rows]")
+            own = p.length if lengths is None else lengths[i]
+            _require(own is None or (_is_int32(own) and own.numel() == 1), "a length is one int32")
+            _require(own is not None or (count is None and p.length is None),
+                     "lengths and counts on the device need a length that receives the rows left")
+            left.append(own)
+            ws = (0, 0) if w is None else w.stride()
+            fields.extend((x.data_ptr(), x.numel(), _address(count), drafted[i], _address(w), ws[0], ws[1], _address(own)))
+        held = b"".join([bytes(p.desc()) for p in caches])
+        self._check(self.lib.cb_keep(self.h, n, held, fields.buffer_info()[0], _stream_on(stream, caches[0].k) if n else 0))
+        if lengths is None:
+            for p, x, own, m in zip(caches, idx, left, drafted):
+                if own is None:
+                    p.T = p.T - m + x.numel()
 
     def _queries(self, Q, out, lse):
         """One sequence's fields of a cb_attend_query, looked over."""

@@ -15,50 +15,23 @@
 #include <cuda_runtime.h>
 
 #include "cb_attend.cuh"
+#include "cb_few.cuh"
 #include "cb_receiver.cuh"
 
 namespace cbk {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kStep = 32;                // positions a warp takes at a time
 constexpr int kStages = 2;               // of them in shared memory
 // Weights are exp2(z - top + 14): up to 2^14, so that fp16 holds those down to 2^-28 of the largest as
 // normal numbers and to 2^-38 at all, and 32-bit sums stay in range.
 constexpr float kWeightBits = 14.f;
 
-// D (16 x 8) += A (16 x 16) B (16 x 8), fp32 sums.
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t y;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-
-// 32 positions of a warp in shared memory: codes of K, of V (rows of D / 2 bytes), scales of K, of V.
-// Thread (gid, tig) = (lane / 4, lane % 4) reads of K the quarter tig of the rows of its two operand rows,
-// of V the eighth gid of four rows.  Operand row r of 16 positions is position place(r), so that those four
-// are 4 i + tig: with the codes' places below both reads meet every bank once.
-__device__ __forceinline__ int place(int r) { return (r & 8) + ((r >> 1) & 3) + 4 * (r & 1); }
-template <int D>
-struct Stage {
-    static constexpr int kCodes = kStep * D / 2, kScales = kStep * D / 16, kBytes = 2 * (kCodes + kScales);
-    // Byte of piece p (16 bytes) of a row's codes.
-    static __device__ __forceinline__ uint32_t at(int row, int p) {
-        if (D == 128) return (row >> 1) * 128 + ((row ^ (row >> 2)) & 1) * 64 + ((p ^ (row & 2)) << 4);
-        return (row >> 2) * 128 + (((row & 3) ^ ((row >> 1) & 2)) << 5) + (p << 4);
-    }
-};
-
 // Copies 32 positions; mine: the row of this lane's.  The codes of a position that has none are some row's: its
 // scales are zeros.
 template <int D>
@@ -108,14 +81,6 @@ __device__ __forceinline__ bool look_over(uint8_t* stage, uint32_t* err) {
     return false;
 }
 
-template <int BYTES> struct Piece;
-template <> struct Piece<16> { using T = uint4; };
-template <> struct Piece<8> { using T = uint2; };
-template <> struct Piece<4> { using T = uint32_t; };
-__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
-__device__ __forceinline__ uint32_t word_of(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
-__device__ __forceinline__ uint32_t word_of(const uint32_t& v, int) { return v; }
-
 // O^T += V^T P^T of 16 positions (rows row0 .. row0 + 15 of the stage).
 template <int D, int NT, bool NEAR>
 __device__ __forceinline__ void add_values(const uint8_t* stage, int row0, const uint32_t (&p)[NT][2], float (&o)[NT][D / 16][4]) {
@@ -150,35 +115,6 @@ __device__ __forceinline__ void add_values(const uint8_t* stage, int row0, const
     }
 }
 
-// Logits of 16 positions, S^T = K Q^T: operand rows are the positions row0 + place(r) of the stage.
-template <int D, int NT, bool NEAR>
-__device__ __forceinline__ void score_keys(const uint8_t* stage, int row0, const uint32_t (&q)[NT][D / 32][4], float (&z)[NT][4]) {
-    constexpr int KW = D / 32;            // words of K a thread takes of a row
-    using S = Stage<D>;
-    using T = typename Piece<D / 8>::T;
-    const int lane = threadIdx.x & 31, tig = lane & 3;
-    const int ra = row0 + place(lane >> 2), rb = ra + 8;
-    const T ca = *reinterpret_cast<const T*>(stage + S::at(ra, tig * (D / 8) / 16) + tig * (D / 8) % 16);
-    const T cb = *reinterpret_cast<const T*>(stage + S::at(rb, tig * (D / 8) / 16) + tig * (D / 8) % 16);
-    const uint16_t* sc = reinterpret_cast<const uint16_t*>(stage + 2 * S::kCodes) + tig * (D / 32) / 4;
-    const uint32_t xa = sc[ra * (D / 32)], xb = sc[rb * (D / 32)];
-    const uint32_t sa = f16_scales(xa, xa), sb = f16_scales(xb, xb);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) z[nt][0] = z[nt][1] = z[nt][2] = z[nt][3] = 0.f;
-#pragma unroll
-    for (int w = 0; w < KW; ++w) {
-        uint32_t u[4], v[4];
-        values_f16<NEAR>(word_of(ca, w), sa, u);
-        values_f16<NEAR>(word_of(cb, w), sb, v);
-        const uint32_t a0[4] = {u[0], v[0], u[1], v[1]}, a1[4] = {u[2], v[2], u[3], v[3]};
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            mma_f16(z[nt], a0, q[nt][w][0], q[nt][w][1]);
-            mma_f16(z[nt], a1, q[nt][w][2], q[nt][w][3]);
-        }
-    }
-}
-
 template <int D, int NT>
 constexpr int few_smem() {
     constexpr int stages = kWarps * kStages * Stage<D>::kBytes, join = kWarps * 8 * NT * (D * 4 + 8);
@@ -206,18 +142,15 @@ __device__ __forceinline__ bool last_of(int32_t* ticket, int n, int* last) {
 // at a time; its four warps take 32 positions in turn, each with its own copies, running maximum and
 // sums, and join at a segment's end.  The last block to leave a part of an item joins the parts, block by
 // block in order.
-//   S^T [16 positions][8 rows] = K Q^T: keys are the operand with 16 rows, so that a group's few
-//     query rows fill the one with 8;
+//   S^T [16 positions][8 rows] = K Q^T (cb_few.cuh);
 //   O^T [D][8 rows] += V^T P^T, with P^T turned by movmatrix from S^T's layout.
-// Queries become fp16 numbers times a power of two that takes a row's largest element to 2^14 .. 2^15:
-// elements down to 2^-29 of it exactly (a bf16 number has 8 bits), smaller ones to 2^-39 of it.
 //
 // Bound by the instructions that turn codes into numbers (half-rate logic and the fp16 fma: some 870 a warp for 32
 // positions), and for one sequence by the joins.  48 sequences in pages, 8 KV heads of 128: 83 us, 3.2 TB/s; one
 // token over 65536 positions 33 us, 2.3 TB/s.  Rows read straight into registers took 291 and 163 us; a third
 // stage of copies 87 us and 34 us.
-template <int D, int NT>
-__global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few(const __grid_constant__ AttendBatch b) {
+template <int D, int NT, class Batch>
+__global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few(const __grid_constant__ Batch b) {
     constexpr int KW = D / 32;            // words of K a thread holds of a row
     constexpr int ROWS = 8 * NT;
     using S = Stage<D>;
@@ -247,38 +180,9 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
             page = segment_page(x, ahead + lane);
         }
 
-        // query rows of column gid: the elements that the thread's pieces of K hold
         uint32_t q[NT][KW][4];
         float zs[NT][2];                  // factor of the logits of columns 2 tig and 2 tig + 1
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int row = nt * 8 + gid;                   // (one row tile: at most 16 rows)
-            const AttendSeq& s = b.s[x.seq];
-            const uint16_t* qp = s.q + (int64_t)(row / b.G) * s.s_tok + (int64_t)(g * b.G + row % b.G) * s.s_head + tig * (D / 4);
-            uint32_t top = 0;
-#pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (row < x.rows) v = __ldg(reinterpret_cast<const uint4*>(qp + w * 8));
-                q[nt][w][0] = v.x; q[nt][w][1] = v.y; q[nt][w][2] = v.z; q[nt][w][3] = v.w;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) top = __vmaxu2(top, q[nt][w][k] & 0x7FFF7FFFu);
-            }
-            top = max(top & 0xFFFFu, top >> 16) >> 7;       // exponent of the largest
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const uint32_t e = min(max(top, 15u), 253u);    // 2^(141 - e): of normal numbers on both sides
-            // (never 0, which times a masked row's -infinity would be NaN: logits are below 2^38, and 2^-88 is none either)
-            const float up = __uint_as_float((268u - e) << 23);
-            const float down = fmaxf(__uint_as_float((e - 14u) << 23) * b.scale_log2e, 1.17549435e-38f);
-#pragma unroll
-            for (int w = 0; w < KW; ++w)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    q[nt][w][k] = pack_f16(__uint_as_float(q[nt][w][k] << 16) * up, __uint_as_float(q[nt][w][k] & 0xFFFF0000u) * up);
-            zs[nt][0] = __shfl_sync(0xFFFFFFFFu, down, 8 * tig);
-            zs[nt][1] = __shfl_sync(0xFFFFFFFFu, down, 8 * tig + 4);
-        }
+        load_queries<D, NT>(b, b.s[x.seq], g, 0, x.rows, q, zs);               // (one row tile: at most 16 rows)
 
         float o[NT][D / 16][4], top[NT][2], sum[NT][2];
 #pragma unroll
@@ -309,6 +213,19 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int64_t at = x.at + (nt * 8 + 2 * tig + h) / b.G;       // position of the column's token
+                        if constexpr (Batch::kTrees) {
+                            const TreeBits& tree = b.tree[x.seq];
+                            if (tree.seen) {
+                                // (columns behind the last token's read that one's bits; nothing is made of them)
+                                const int m = b.span[x.seq].m, r = min((int)(at - x.at), m - 1);
+                                const uint32_t bits = tree_bits(tree.seen + r * tree.s_row, (m + 31) / 32, t0 - x.at);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (t0 + 8 * k + place(gid) >= x.len || !(bits >> (8 * k + place(gid)) & 1u))
+                                        z[k / 2][nt][2 * (k % 2) + h] = -INFINITY;
+                                continue;
+                            }
+                        }
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
                             const int t = t0 + 8 * k + place(gid);
@@ -463,14 +380,14 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
     }
 }
 
-template <int D, int NT>
-cudaError_t launch_few(const AttendBatch& b, int64_t units, int num_sms, cudaStream_t st) {
+template <int D, int NT, class Batch>
+cudaError_t launch_few(const Batch& b, int64_t units, int num_sms, cudaStream_t st) {
     // as many runs as leave no block waiting, one at least
     const int64_t most = num_sms * few_blocks<D, NT>() / b.n_kv_heads, all = units / b.n_kv_heads;
     const int64_t runs = all < most ? all : most;
     const int blocks = (int)(runs > 1 ? runs : 1) * b.n_kv_heads;
     static_assert(few_smem<D, NT>() <= 46 * 1024, "more needs the function's attribute set");
-    k_attend_few<D, NT><<<blocks, kWarps * 32, few_smem<D, NT>(), st>>>(b);
+    k_attend_few<D, NT, Batch><<<blocks, kWarps * 32, few_smem<D, NT>(), st>>>(b);
     return cudaGetLastError();
 }
 
@@ -493,7 +410,8 @@ int64_t attend_pairs(AttendBatch& b, int tile_rows) {
     return units;
 }
 
-cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
+template <class Batch>
+static cudaError_t launch_by_rows(Batch& b, int head_dim, cudaStream_t st, int num_sms) {
     int rows = 0;
     for (int i = 0; i < b.n; ++i) rows = b.span[i].m > rows ? b.span[i].m : rows;
     rows *= b.G;
@@ -511,6 +429,13 @@ cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num
     if (head_dim == 128)
         return tile_rows == 8 ? launch_few<128, 1>(b, units, num_sms, st) : launch_few<128, 2>(b, units, num_sms, st);
     return tile_rows == 8 ? launch_few<64, 1>(b, units, num_sms, st) : launch_few<64, 2>(b, units, num_sms, st);
+}
+
+cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
+    return launch_by_rows(b, head_dim, st, num_sms);
+}
+cudaError_t launch_attend(AttendTreeBatch& b, int head_dim, cudaStream_t st, int num_sms) {
+    return launch_by_rows(b, head_dim, st, num_sms);
 }
 
 }  // namespace cbk

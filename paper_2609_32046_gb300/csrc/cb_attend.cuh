@@ -34,7 +34,12 @@ __device__ __forceinline__ int64_t attend_length(const AttendSpan& s) {
 struct Reach {
     int64_t lo, hi, all_to_here, all_from_here;
 };
-__device__ __forceinline__ Reach attend_reach(const AttendBatch& b, const AttendSpan& s, int64_t L, int tile, int tile_rows) {
+template <class B>
+__device__ __forceinline__ Reach attend_reach(const B& b, int seq, int64_t L, int tile, int tile_rows) {
+    const AttendSpan& s = b.span[seq];
+    if constexpr (B::kTrees) {
+        if (b.tree[seq].seen) return Reach{0, L, 0, max((int64_t)0, L - s.m)};
+    }
     const int first = tile * tile_rows, last = min(first + tile_rows, s.m * b.G) - 1;
     Reach x{0, L, 0, L};
     if (b.causal) {
@@ -75,15 +80,18 @@ __device__ __forceinline__ int attend_seq_of(const AttendBatch& b, int p) {
 }
 
 // Units of pair p.
-__device__ __forceinline__ int attend_units_of(const AttendBatch& b, int tile_rows, int p) {
-    const AttendSpan& s = b.span[attend_seq_of(b, p)];
-    const Reach x = attend_reach(b, s, attend_length(s), p - s.pair0, tile_rows);
+template <class B>
+__device__ __forceinline__ int attend_units_of(const B& b, int tile_rows, int p) {
+    const int seq = attend_seq_of(b, p);
+    const AttendSpan& s = b.span[seq];
+    const Reach x = attend_reach(b, seq, attend_length(s), p - s.pair0, tile_rows);
     const int u = (int)((x.hi - x.lo + kUnit - 1) / kUnit);
     return u > 0 ? u : 1;
 }
 
 // Units of the pairs before each pair, into shared memory: pre[0..pairs].  Whole block.
-__device__ __forceinline__ void attend_units(const AttendBatch& b, int tile_rows, int* pre) {
+template <class B>
+__device__ __forceinline__ void attend_units(const B& b, int tile_rows, int* pre) {
     const bool few = b.pairs <= 32;                    // the first warp alone, out of registers
     if (!few) {
 #pragma unroll 1
@@ -162,14 +170,15 @@ __device__ __forceinline__ Item attend_item(const AttendBatch& b, const int* pre
 }
 
 // The segment that begins with unit u of a run that ends at `end` (one thread); its head counts from g0.
-__device__ __forceinline__ void attend_segment(const AttendBatch& b, const int* pre, int heads, int g0, int u, int end,
+template <class B>
+__device__ __forceinline__ void attend_segment(const B& b, const int* pre, int heads, int g0, int u, int end,
                                                int head_dim, int tile_rows, Segment* x) {
     Item item = attend_item(b, pre, heads, u);
     item.g += g0;
     const AttendSeq& s = b.s[item.seq];
     const AttendSpan& a = b.span[item.seq];
     const int64_t L = attend_length(a);
-    const Reach r = attend_reach(b, a, L, item.tile, tile_rows);
+    const Reach r = attend_reach(b, item.seq, L, item.tile, tile_rows);
     x->first = item.first;
     x->units = item.units;
     x->n = min(end - u, item.units - (u - item.first));
@@ -195,6 +204,15 @@ __device__ __forceinline__ void attend_segment(const AttendBatch& b, const int* 
     x->n_pages = (uint32_t)min(s.kv.n_pages, (int64_t)0x7FFFFFFF);
     x->shift = s.kv.shift;
     x->mask = (1u << s.kv.shift) - 1;
+}
+
+// Bits of the rows u0 .. u0 + 31 of a token (u counts from token 0's row) that `words` of its bits say, bit i that of
+// row u0 + i; rows before token 0's are seen.  (Bits of rows past the last token's are whatever they are.)
+__device__ __forceinline__ uint32_t tree_bits(const uint32_t* row, int words, int64_t u0) {
+    if (u0 < 0) return u0 <= -32 ? 0xFFFFFFFFu : __ldg(row) << (int)-u0 | ((1u << (int)-u0) - 1u);
+    const int w = (int)(u0 >> 5), lo = (int)(u0 & 31);
+    if (w >= words) return 0;
+    return __funnelshift_r(__ldg(row + w), w + 1 < words ? __ldg(row + w + 1) : 0u, lo);
 }
 
 // The block-table entry of position t of the segment, read ahead of the copies that need it, and the row of
@@ -350,5 +368,6 @@ constexpr int64_t kFarWindow = (int64_t)1 << 32;
 // Host side, shared by the launchers: row tiles of every sequence, and the most units there can be.
 int64_t attend_pairs(AttendBatch& b, int tile_rows);
 cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms);
+cudaError_t launch_attend_tc(AttendTreeBatch& b, int head_dim, cudaStream_t st, int num_sms);
 
 }  // namespace cbk

@@ -26,6 +26,7 @@
 // without softmax and unpacking, 249.
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -169,11 +170,24 @@ __device__ __forceinline__ void copy_v(uint32_t to, const Segment& x, int lo, in
     copy_commit();
 }
 
+// Every column of a tile that is seen at all: what a row's bits do not say otherwise.
+struct AllBits {
+    __device__ __forceinline__ uint32_t operator()(int) const { return 0xFFFFFFFFu; }
+};
+// A drafted token's bits for 32 columns from `first` on: column 0 is row u0, counted from token 0's.
+struct RowBits {
+    const uint32_t* row;
+    int words;
+    int64_t u0;
+    __device__ __forceinline__ uint32_t operator()(int first) const { return tree_bits(row, words, u0 + first); }
+};
+
 // A thread's row of one tile: S at ts becomes weights at tp, M and l follow; where M rises by much the sums at
-// `to` (if there are any) are scaled.  EDGE: columns [c0, c1) alone are seen; without it no column is looked at.
-template <int D, bool EDGE>
+// `to` (if there are any) are scaled.  EDGE: columns [c0, c1) alone are seen, and of them those that `bits` says;
+// without it no column is looked at.
+template <int D, bool EDGE, class Bits = AllBits>
 __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t to, bool sums, int c0, int c1, float scale,
-                                             float& M, float& l) {
+                                             float& M, float& l, const Bits& bits = Bits()) {
     // 32 columns at a time, first for the maximum, then for the weights, each read from tensor memory when its
     // turn comes.  (Rolled up: the roles share the instruction cache.  With the four steps written out and all
     // columns in registers, read once, 1024 tokens over 16384 positions took 353 us for 292.)
@@ -184,6 +198,12 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
 #pragma unroll
             for (int k = 0; k < 32; ++k)
                 if (first + k < c0 || first + k >= c1) x[k] = -INFINITY;
+            if constexpr (!std::is_same<Bits, AllBits>::value) {
+                const uint32_t w = bits(first);
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    if (!(w >> k & 1u)) x[k] = -INFINITY;
+            }
         }
     };
 #pragma unroll 1
@@ -270,8 +290,8 @@ __device__ __forceinline__ AttendCut cut_of(const AttendBatch& b, const int* pre
     return cut;
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_constant__ AttendBatch b) {
+template <int D, class Batch>
+__global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_constant__ Batch b) {
     constexpr int kOp = kTile * D * 2;              // bytes of an operand tile
     constexpr bool kOver = D == 128;                // P in S's columns
     extern __shared__ uint8_t raw[];
@@ -584,9 +604,11 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
                     // columns [c0, c1) of the row are seen
                     const bool edge = t0 + kTile > seg.all_from || t0 < seg.all_to;
                     int c0 = 0, c1 = kTile;
+                    bool tree = false;
+                    if constexpr (Batch::kTrees) tree = b.tree[seg.seq].seen != nullptr;
                     if (edge) {
                         int64_t hi = seg.len - t0, lo = 0;
-                        if (b.causal) {
+                        if (b.causal && !tree) {
                             const int64_t at = seg.at + (seg.row0 + min(r0 + lane, seg.rows - 1)) / b.G - t0;   // of the row's token
                             hi = min(hi, at + 1);
                             if (b.window) lo = at - b.window + 1;
@@ -594,7 +616,13 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
                         c0 = (int)max((int64_t)0, min(lo, (int64_t)kTile));
                         c1 = (int)max((int64_t)0, min(hi, (int64_t)kTile));
                     }
-                    if (edge) softmax_tile<D, true>(ts, tp, to, n > 0, c0, c1, b.scale_log2e, M, l);
+                    if (Batch::kTrees && edge && tree) {
+                        if constexpr (Batch::kTrees) {
+                            const int m = b.span[seg.seq].m, token = (seg.row0 + min(r0 + lane, seg.rows - 1)) / b.G;
+                            const RowBits bits{b.tree[seg.seq].seen + token * b.tree[seg.seq].s_row, (m + 31) / 32, t0 - seg.at};
+                            softmax_tile<D, true, RowBits>(ts, tp, to, n > 0, c0, c1, b.scale_log2e, M, l, bits);
+                        }
+                    } else if (edge) softmax_tile<D, true>(ts, tp, to, n > 0, c0, c1, b.scale_log2e, M, l);
                     else softmax_tile<D, false>(ts, tp, to, n > 0, 0, kTile, b.scale_log2e, M, l);
                     tmem_wait_st();
                 }
@@ -702,21 +730,21 @@ __global__ void __launch_bounds__(256) k_attend_join(const __grid_constant__ Att
     }
 }
 
-template <int D>
-cudaError_t launch(const AttendBatch& b, int blocks, cudaStream_t st) {
+template <int D, class Batch>
+cudaError_t launch(const Batch& b, int blocks, cudaStream_t st) {
     static std::atomic<bool> set[64];     // (the attribute belongs to the device's function)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !set[dev]) {
         cudaFuncAttributes a;
-        if ((e = cudaFuncGetAttributes(&a, k_attend_tc<D>)) != cudaSuccess) return e;
+        if ((e = cudaFuncGetAttributes(&a, k_attend_tc<D, Batch>)) != cudaSuccess) return e;
         if (a.numRegs < kRegs) return cudaErrorInvalidKernelImage;      // (the warp groups' shares need them all)
-        e = cudaFuncSetAttribute(k_attend_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>());
+        e = cudaFuncSetAttribute(k_attend_tc<D, Batch>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D>());
         if (e != cudaSuccess) return e;
         if (dev < 64) set[dev] = true;
     }
-    k_attend_tc<D><<<blocks, kThreadsAt, smem_bytes<D>(), st>>>(b);
+    k_attend_tc<D, Batch><<<blocks, kThreadsAt, smem_bytes<D>(), st>>>(b);
     e = cudaGetLastError();
     if (e != cudaSuccess || blocks == 1) return e;
     cudaLaunchAttribute early;
@@ -728,17 +756,25 @@ cudaError_t launch(const AttendBatch& b, int blocks, cudaStream_t st) {
     config.stream = st;
     config.attrs = &early;
     config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, k_attend_join<D>, b);
+    return cudaLaunchKernelEx(&config, k_attend_join<D>, static_cast<const AttendBatch&>(b));
 }
 
-}  // namespace
-
-cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
+template <class Batch>
+cudaError_t launch_by_dim(Batch& b, int head_dim, cudaStream_t st, int num_sms) {
     const int64_t units = attend_pairs(b, kRowTile);
     const int blocks = (int)(units < num_sms ? units : num_sms);
     const cudaError_t e = head_dim == 128 ? launch<128>(b, blocks, st) : launch<64>(b, blocks, st);
     b.stall = 0;
     return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms) {
+    return launch_by_dim(b, head_dim, st, num_sms);
+}
+cudaError_t launch_attend_tc(AttendTreeBatch& b, int head_dim, cudaStream_t st, int num_sms) {
+    return launch_by_dim(b, head_dim, st, num_sms);
 }
 
 }  // namespace cbk

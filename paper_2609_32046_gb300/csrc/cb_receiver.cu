@@ -1,8 +1,10 @@
 // C-ABI of the receiver's side (declared in include/cacheback.h): rotary positions, rows held in 4
 // bits, attention over them.  Validation and launch plumbing.
 #include <cmath>
+#include <cstddef>
 #include <cstring>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "cb_ctx.cuh"
@@ -111,6 +113,16 @@ PackedRows packed_rows(const cb_packed& p, int d) {
         r.s_page = p.s_page / d;
         r.n_pages = p.n_pages;
         r.shift = log2_of(p.page_size);
+    }
+    return r;
+}
+
+// The same from a layer on.
+PackedRows packed_layer(const cb_packed& p, int d, int32_t layer) {
+    PackedRows r = packed_rows(p, d);
+    for (int x = 0; x < 2 && p.T; ++x) {
+        r.code[x] += layer * r.s_layer * (d / 2);
+        r.scale[x] += layer * r.s_layer * (d / 32);
     }
     return r;
 }
@@ -344,8 +356,26 @@ cb_status unpack_impl(cb_ctx* ctx, int32_t n, const cb_packed* caches, const int
     return CB_OK;
 }
 
+// Bits of the m tokens of a sequence.
+cb_status check_tree(cb_ctx* ctx, DevicePtrs& ptrs, const cb_tree& t, int32_t m, int i) {
+    if (!t.seen) return CB_OK;
+    if (m > 1 && (t.s_row < (m + 31) / 32 || t.s_row > kMaxRows))
+        return fail(ctx, CB_EINVAL, "trees[%d].s_row = %lld words for %d tokens", i, (long long)t.s_row, m);
+    return ptrs.check(t.seen, "trees.seen", i, 4);
+}
+
+void set_trees(AttendBatch&, int, const cb_tree*) {}
+void set_trees(AttendTreeBatch& b, int k, const cb_tree* t) { b.tree[k] = TreeBits{t->seen, t->s_row}; }
+
+// (units of work are counted in 32 bits)
+bool too_much_work(const cb_ctx* ctx, int64_t T, int32_t m) {
+    return (T / 128 + 2) * ctx->cfg.n_kv_heads * ((int64_t)m * ctx->G / 128 + 1) > ((int64_t)1 << 31) / kMaxBatch;
+}
+
+// Batch: AttendBatch, or AttendTreeBatch with trees.
+template <class Batch>
 cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* caches, const cb_attend_query* queries,
-                      int32_t causal, int64_t window, cudaStream_t strm) {
+                      const cb_tree* trees, int32_t causal, int64_t window, cudaStream_t strm) {
     const cb_config& c = ctx->cfg;
     const int d = c.head_dim;
     if (n < 1 || n > c.max_senders) return fail(ctx, CB_ESHAPE, "n = %d not in [1, %d]", n, c.max_senders);
@@ -374,8 +404,8 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         if ((st = ptrs.check(q.q, "queries.q", i)) || (st = ptrs.check(q.out, "queries.out", i)))
             return st;
         if (q.lse && (st = ptrs.check(q.lse, "queries.lse", i, 4))) return st;
-        // (units of work are counted in 32 bits)
-        if ((caches[i].T / 128 + 2) * c.n_kv_heads * ((int64_t)q.m * ctx->G / 128 + 1) > ((int64_t)1 << 31) / kMaxBatch)
+        if (trees && (st = check_tree(ctx, ptrs, trees[i], q.m, i))) return st;
+        if (too_much_work(ctx, caches[i].T, q.m))
             return fail(ctx, CB_ESHAPE, "sequence %d: too many positions, heads and query tokens for one launch", i);
         const uintptr_t at = reinterpret_cast<uintptr_t>(q.out), e = reinterpret_cast<uintptr_t>(q.lse);
         outs.push_back(Written{at, at + 2 * (uintptr_t)span, span == rows * d});
@@ -387,7 +417,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
         return fail(ctx, CB_EINVAL, "two sequences write the same rows of out or lse");
     if ((st = attend_scratch(ctx, strm))) return st;
     for (size_t b0 = 0; b0 < some.size(); b0 += kMaxBatch) {
-        AttendBatch b;
+        Batch b;
         std::memset(&b, 0, sizeof b);
         b.n = (int32_t)(some.size() - b0 < (size_t)kMaxBatch ? some.size() - b0 : kMaxBatch);
         b.n_q_heads = c.n_q_heads;
@@ -407,11 +437,7 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
             const cb_packed& p = caches[some[b0 + k]];
             const cb_attend_query& q = queries[some[b0 + k]];
             AttendSeq& s = b.s[k];
-            s.kv = packed_rows(p, d);
-            for (int x = 0; x < 2 && p.T; ++x) {
-                s.kv.code[x] += layer * s.kv.s_layer * (d / 2);
-                s.kv.scale[x] += layer * s.kv.s_layer * (d / 32);
-            }
+            s.kv = packed_layer(p, d, layer);
             b.span[k].T = p.T;
             b.span[k].length = p.length;
             b.span[k].m = q.m;
@@ -420,12 +446,320 @@ cb_status attend_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* ca
             s.lse = q.lse;
             s.s_tok = q.s_tok; s.s_head = q.s_head;
             s.o_tok = q.o_tok; s.o_head = q.o_head;
+            if (trees) set_trees(b, k, trees + some[b0 + k]);
         }
         const cudaError_t e = launch_attend(b, d, strm, ctx->num_sms);
         ctx->stall_attend = b.stall;
         if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "attend launch failed: %s", cudaGetErrorString(e));
     }
     return CB_OK;
+}
+
+// fp32 arrays [n_layers][n_heads][rows] with unit steps over the rows: the elements they span, or -1 where rows overlap
+// or the strides are too large.
+int64_t weights_span(int64_t n_layers, int64_t s_layer, int64_t n_heads, int64_t s_head, int64_t rows) {
+    Dim dims[2] = {{n_layers, s_layer}, {n_heads, s_head}};
+    for (const Dim& x : dims)
+        if (x.count > 1 && x.stride <= 0) return -1;
+    const int64_t span = span_of(dims, 2, rows);
+    return span < 0 || !rows_apart(dims, 2, rows) ? -1 : span;
+}
+
+bool touch(const void* a, int64_t bytes_a, const void* b, int64_t bytes_b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + (uintptr_t)bytes_b && y < x + (uintptr_t)bytes_a;
+}
+
+cb_status weigh_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* caches, const cb_weigh_query* queries,
+                     const cb_tree* trees, int32_t causal, int64_t window, float decay, cudaStream_t strm) {
+    const cb_config& c = ctx->cfg;
+    const int d = c.head_dim;
+    if (n < 1 || n > c.max_senders) return fail(ctx, CB_ESHAPE, "n = %d not in [1, %d]", n, c.max_senders);
+    if (layer < 0 || layer >= c.n_layers) return fail(ctx, CB_ESHAPE, "layer %d not in [0, %d)", layer, c.n_layers);
+    if (!caches || !queries) return fail(ctx, CB_EINVAL, "caches or queries is NULL");
+    if (causal != 0 && causal != 1) return fail(ctx, CB_EINVAL, "causal must be 0 or 1");
+    if (window < 0 || (window && !causal)) return fail(ctx, CB_EINVAL, "window must be >= 0, and 0 unless causal");
+    if (trees && (!causal || window)) return fail(ctx, CB_EINVAL, "trees go with causal = 1 and window = 0");
+    if (!(decay >= 0.f && decay <= 1.f)) return fail(ctx, CB_EINVAL, "decay must be within 0 .. 1");
+    DeviceGuard dg(ctx->device);
+    DevicePtrs ptrs(ctx);
+    if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
+    cb_status st;
+    std::vector<int32_t> some;
+    std::vector<Written> written;
+    for (int i = 0; i < n; ++i) {
+        const cb_weigh_query& q = queries[i];
+        if ((st = check_packed(ctx, ptrs, caches[i], i, c.max_positions < kMaxHeld ? c.max_positions : kMaxHeld))) return st;
+        if (q.m < 0 || q.m > c.max_query_tokens)
+            return fail(ctx, CB_ESHAPE, "queries[%d].m = %d not in [0, %d]", i, q.m, c.max_query_tokens);
+        if (q.fresh < 0) return fail(ctx, CB_EINVAL, "queries[%d].fresh is negative", i);
+        const int64_t T = caches[i].T;
+        if (q.m == 0 || T == 0) continue;
+        Dim in[2] = {{q.m, q.s_tok}, {c.n_q_heads, q.s_head}};
+        if (!strides_ok(in, 2) || span_of(in, 2, d) < 0)
+            return fail(ctx, CB_EINVAL, "queries[%d]: strides must be positive multiples of 8, and not too large", i);
+        if ((st = ptrs.check(q.q, "queries.q", i)) || (st = ptrs.check(q.lse, "queries.lse", i, 4)) ||
+            (st = ptrs.check(q.weights, "queries.weights", i, 4)) ||
+            (q.before && (st = ptrs.check(q.before, "queries.before", i, 4))))
+            return st;
+        const int64_t span = weights_span(1, 0, c.n_kv_heads, q.w_head, T);
+        const int64_t had = q.before ? weights_span(1, 0, c.n_kv_heads, q.b_head, T) : 0;
+        if (span < 0 || had < 0) return fail(ctx, CB_EINVAL, "queries[%d]: rows of weights overlap, or the strides are too large", i);
+        const bool same = q.before == q.weights && (c.n_kv_heads == 1 || q.b_head == q.w_head);
+        if (q.before && !same && touch(q.weights, 4 * span, q.before, 4 * had))
+            return fail(ctx, CB_EINVAL, "queries[%d]: weights overlap before and are not before itself", i);
+        if (trees && (st = check_tree(ctx, ptrs, trees[i], q.m, i))) return st;
+        if (too_much_work(ctx, T, q.m))
+            return fail(ctx, CB_ESHAPE, "sequence %d: too many positions, heads and query tokens for one launch", i);
+        const uintptr_t at = reinterpret_cast<uintptr_t>(q.weights);
+        written.push_back(Written{at, at + 4 * (uintptr_t)span, span == T * c.n_kv_heads});
+        some.push_back(i);
+    }
+    if (some.empty()) return CB_OK;
+    if (written_twice(written)) return fail(ctx, CB_EINVAL, "two sequences write the same weights");
+    for (size_t b0 = 0; b0 < some.size(); b0 += kMaxBatch) {
+        WeighBatch b;
+        std::memset(&b, 0, sizeof b);
+        b.n = (int32_t)(some.size() - b0 < (size_t)kMaxBatch ? some.size() - b0 : kMaxBatch);
+        b.n_q_heads = c.n_q_heads;
+        b.n_kv_heads = c.n_kv_heads;
+        b.G = ctx->G;
+        b.scale_log2e = ctx->scale * 1.4426950408889634f;
+        b.err = ctx->err;
+        b.wait_ns = (uint64_t)ctx->wait_ns;
+        b.sees = causal;
+        b.sees_window = window;
+        b.decay = decay;
+        for (int k = 0; k < b.n; ++k) {
+            const int i = some[b0 + k];
+            const cb_weigh_query& q = queries[i];
+            AttendSeq& s = b.s[k];
+            WeighSeq& w = b.w[k];
+            s.kv = packed_layer(caches[i], d, layer);
+            s.q = static_cast<const uint16_t*>(q.q);
+            s.s_tok = q.s_tok; s.s_head = q.s_head;
+            b.span[k].T = caches[i].T;
+            b.span[k].length = caches[i].length;
+            b.span[k].m = q.m;
+            w.lse = q.lse;
+            w.before = q.before;
+            w.weights = q.weights;
+            w.b_head = q.b_head; w.w_head = q.w_head;
+            w.fresh = q.fresh < kMaxRows ? q.fresh : kMaxRows;
+            if (trees) w.tree = TreeBits{trees[i].seen, trees[i].s_row};
+        }
+        const cudaError_t e = launch_weigh(b, d, strm, ctx->num_sms);
+        if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "weigh launch failed: %s", cudaGetErrorString(e));
+    }
+    return CB_OK;
+}
+
+// Caches whose rows a call moves: nothing that one part writes may be another's.  What can be seen of that on the host: the
+// same codes under the same block table, or rows of unpaged caches that overlap.
+struct Places {
+    std::vector<Written> codes;
+    std::vector<std::pair<uintptr_t, uintptr_t>> paged;     // codes and table of every cache written
+    std::vector<Written> weights, idx;
+    std::vector<uintptr_t> lengths, left;                   // of the caches read, of those left
+
+    void add(const cb_packed& p, int d, const cb_config& c) {
+        if (p.T == 0) return;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p.k);
+        if (p.pages) {
+            paged.emplace_back(at, reinterpret_cast<uintptr_t>(p.pages));
+            return;
+        }
+        Dim dims[3] = {{c.n_layers, p.s_layer}, {c.n_kv_heads, p.s_head}, {p.T, p.s_pos}};
+        const int64_t span = span_of(dims, 3, d), rows = c.n_layers * c.n_kv_heads * p.T;
+        codes.push_back(Written{at, at + (uintptr_t)(span / 2), span == rows * d});
+    }
+    bool clash() {
+        std::sort(paged.begin(), paged.end());
+        for (size_t i = 1; i < paged.size(); ++i)
+            if (paged[i] == paged[i - 1]) return true;
+        std::sort(left.begin(), left.end());
+        for (size_t i = 1; i < left.size(); ++i)
+            if (left[i] == left[i - 1]) return true;
+        return written_twice(codes) || written_twice(weights) || written_twice(idx);
+    }
+    // A length that is written is also another cache's, which reads it.  `own`: what each cache reads and what it writes.
+    bool lengths_clash(const std::vector<std::pair<uintptr_t, uintptr_t>>& own) {
+        std::sort(lengths.begin(), lengths.end());
+        for (const auto& x : own) {
+            if (!x.second) continue;
+            const auto all = std::equal_range(lengths.begin(), lengths.end(), x.second);
+            if (all.second - all.first > (x.second == x.first ? 1 : 0)) return true;
+        }
+        return false;
+    }
+};
+
+cb_status move_all(cb_ctx* ctx, std::vector<MoveSeq>& seqs, int32_t n_layers, cudaStream_t strm) {
+    for (int pass = 0; pass < 2; ++pass)                    // rows, then lengths
+        for (size_t b0 = 0; b0 < seqs.size(); b0 += kMaxPackBatch) {
+            MoveBatch b;
+            std::memset(&b, 0, sizeof b);
+            b.n = (int32_t)(seqs.size() - b0 < (size_t)kMaxPackBatch ? seqs.size() - b0 : kMaxPackBatch);
+            b.n_layers = n_layers;
+            b.n_kv_heads = ctx->cfg.n_kv_heads;
+            b.err = ctx->err;
+            for (int k = 0; k < b.n; ++k) b.s[k] = seqs[b0 + k];
+            const cudaError_t e = pass ? launch_left(b, strm) : launch_move(b, ctx->cfg.head_dim, strm, ctx->num_sms);
+            if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "move launch failed: %s", cudaGetErrorString(e));
+        }
+    return CB_OK;
+}
+
+cb_status evict_impl(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, const cb_packed* caches, const cb_packed* into,
+                     const cb_eviction* evictions, cudaStream_t strm) {
+    const cb_config& c = ctx->cfg;
+    const int d = c.head_dim;
+    if (n < 1 || n > c.max_senders) return fail(ctx, CB_ESHAPE, "n = %d not in [1, %d]", n, c.max_senders);
+    if (!caches || !evictions) return fail(ctx, CB_EINVAL, "caches or evictions is NULL");
+    if (layer < 0 || n_layers < 1 || n_layers > c.n_layers - layer)
+        return fail(ctx, CB_ESHAPE, "layers [%d, %d) not in [0, %d)", layer, layer + n_layers, c.n_layers);
+    DeviceGuard dg(ctx->device);
+    DevicePtrs ptrs(ctx);
+    if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
+    cb_status st;
+    std::vector<MoveSeq> moves;
+    std::vector<RankSeq> ranks;
+    std::vector<std::pair<uintptr_t, uintptr_t>> lengths;
+    Places places;
+    const int64_t lists = (int64_t)n_layers * c.n_kv_heads;
+    for (int i = 0; i < n; ++i) {
+        const cb_packed& p = caches[i];
+        const cb_eviction& e = evictions[i];
+        if ((st = check_packed(ctx, ptrs, p, i))) return st;
+        if (e.keep < 0 || e.keep >= kMaxRows || e.first < 0 || e.last < 0)
+            return fail(ctx, CB_ESHAPE, "evictions[%d]: keep, first and last must be in [0, 2^31)", i);
+        if (e.first > e.keep || e.last > e.keep - e.first)
+            return fail(ctx, CB_EBUDGET, "evictions[%d]: first + last above keep = %lld", i, (long long)e.keep);
+        if (e.length && (st = ptrs.check(e.length, "evictions.length", i, 4))) return st;
+        const bool other = into && into[i].k != p.k;
+        const cb_packed& to = into ? into[i] : p;
+        if (into && (st = check_packed(ctx, ptrs, to, i))) return st;
+        if (into && !other && std::memcmp(&to, &p, offsetof(cb_packed, length)) != 0)
+            return fail(ctx, CB_EINVAL, "into[%d] has the codes of caches[%d] but is not the same cache", i, i);
+        if (to.T < (e.keep < p.T ? e.keep : p.T))
+            return fail(ctx, CB_EBUDGET, "into[%d].T = %lld has no room for %lld rows", i, (long long)to.T, (long long)e.keep);
+        if (p.T > 0 && e.keep > 0) {
+            if ((st = ptrs.check(e.weights, "evictions.weights", i, 4)) || (st = ptrs.check(e.idx, "evictions.idx", i, 4)) ||
+                (e.weights_to && (st = ptrs.check(e.weights_to, "evictions.weights_to", i, 4))))
+                return st;
+            const int64_t rows = e.keep < p.T ? e.keep : p.T;
+            const int64_t span = weights_span(n_layers, e.w_layer, c.n_kv_heads, e.w_head, p.T);
+            const int64_t span_to = e.weights_to ? weights_span(n_layers, e.t_layer, c.n_kv_heads, e.t_head, rows) : 0;
+            if (span < 0 || span_to < 0)
+                return fail(ctx, CB_EINVAL, "evictions[%d]: rows of weights overlap, or the strides are too large", i);
+            const bool same = e.weights == e.weights_to && (n_layers == 1 || e.w_layer == e.t_layer) &&
+                              (c.n_kv_heads == 1 || e.w_head == e.t_head);
+            if (e.weights_to && (other ? touch(e.weights, 4 * span, e.weights_to, 4 * span_to) : !same))
+                return fail(ctx, CB_EINVAL, "evictions[%d]: weights move as the rows do, in place or to memory of their own", i);
+            const uintptr_t w = reinterpret_cast<uintptr_t>(e.weights_to), x = reinterpret_cast<uintptr_t>(e.idx);
+            if (w) places.weights.push_back(Written{w, w + 4 * (uintptr_t)span_to, span_to == lists * rows});
+            places.idx.push_back(Written{x, x + 4 * (uintptr_t)(lists * e.keep), true});
+            places.add(to, d, c);
+        }
+        places.lengths.push_back(reinterpret_cast<uintptr_t>(p.length));
+        if (e.length) places.left.push_back(reinterpret_cast<uintptr_t>(e.length));
+        lengths.emplace_back(reinterpret_cast<uintptr_t>(p.length), reinterpret_cast<uintptr_t>(e.length));
+        MoveSeq m{};
+        m.count = e.keep;
+        m.T = p.T;
+        m.length = p.length;
+        m.left = e.length;
+        m.drafted = -1;
+        if (p.T > 0 && e.keep > 0) {
+            RankSeq r{};
+            r.weights = e.weights;
+            r.w_layer = e.w_layer; r.w_head = e.w_head;
+            r.T = p.T;
+            r.length = p.length;
+            r.keep = e.keep; r.first = e.first; r.last = e.last;
+            r.idx = e.idx;
+            ranks.push_back(r);
+            m.from = packed_layer(p, d, layer);
+            m.to = packed_layer(to, d, layer);
+            m.w = e.weights_to ? e.weights : nullptr;
+            m.w_to = e.weights_to;
+            m.w_layer = e.w_layer; m.w_head = e.w_head;
+            m.t_layer = e.t_layer; m.t_head = e.t_head;
+            m.idx = e.idx;
+            m.idx_list = e.keep;
+            m.in_place = !other;
+        } else {
+            m.count = 0;
+        }
+        moves.push_back(m);
+    }
+    if (places.clash() || places.lengths_clash(lengths)) return fail(ctx, CB_EINVAL, "two parts of the call write the same memory");
+    for (size_t b0 = 0; b0 < ranks.size(); b0 += kMaxBatch) {
+        RankBatch b;
+        std::memset(&b, 0, sizeof b);
+        b.n = (int32_t)(ranks.size() - b0 < (size_t)kMaxBatch ? ranks.size() - b0 : kMaxBatch);
+        b.n_layers = n_layers;
+        b.n_kv_heads = c.n_kv_heads;
+        for (int k = 0; k < b.n; ++k) b.s[k] = ranks[b0 + k];
+        const cudaError_t e = launch_rank(b, strm, ctx->num_sms);
+        if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "rank launch failed: %s", cudaGetErrorString(e));
+    }
+    return move_all(ctx, moves, n_layers, strm);
+}
+
+cb_status keep_impl(cb_ctx* ctx, int32_t n, const cb_packed* caches, const cb_kept* kept, cudaStream_t strm) {
+    const cb_config& c = ctx->cfg;
+    const int d = c.head_dim;
+    if (n < 1 || n > c.max_senders) return fail(ctx, CB_ESHAPE, "n = %d not in [1, %d]", n, c.max_senders);
+    if (!caches || !kept) return fail(ctx, CB_EINVAL, "caches or kept is NULL");
+    DeviceGuard dg(ctx->device);
+    DevicePtrs ptrs(ctx);
+    if (!dg.ok) return fail(ctx, CB_ECUDA, "cannot select device %d", ctx->device);
+    cb_status st;
+    std::vector<MoveSeq> moves;
+    std::vector<std::pair<uintptr_t, uintptr_t>> lengths;
+    Places places;
+    for (int i = 0; i < n; ++i) {
+        const cb_packed& p = caches[i];
+        const cb_kept& e = kept[i];
+        if ((st = check_packed(ctx, ptrs, p, i))) return st;
+        if (e.drafted < 0 || e.drafted > p.T || e.count < 0 || e.count > e.drafted)
+            return fail(ctx, CB_EBUDGET, "kept[%d]: count = %lld of %lld drafted rows of a cache of %lld", i, (long long)e.count,
+                        (long long)e.drafted, (long long)p.T);
+        if (e.length && (st = ptrs.check(e.length, "kept.length", i, 4))) return st;
+        if (e.n_kept && (st = ptrs.check(e.n_kept, "kept.n_kept", i, 4))) return st;
+        places.lengths.push_back(reinterpret_cast<uintptr_t>(p.length));
+        if (e.length) places.left.push_back(reinterpret_cast<uintptr_t>(e.length));
+        lengths.emplace_back(reinterpret_cast<uintptr_t>(p.length), reinterpret_cast<uintptr_t>(e.length));
+        MoveSeq m{};
+        m.T = p.T;
+        m.length = p.length;
+        m.left = e.length;
+        m.drafted = e.drafted;
+        m.n_kept = e.n_kept;
+        m.in_place = 1;
+        if (e.count > 0) {
+            if ((st = ptrs.check(e.idx, "kept.idx", i, 4)) || (e.weights && (st = ptrs.check(e.weights, "kept.weights", i, 4))))
+                return st;
+            if (e.weights) {
+                const int64_t span = weights_span(c.n_layers, e.w_layer, c.n_kv_heads, e.w_head, p.T);
+                if (span < 0) return fail(ctx, CB_EINVAL, "kept[%d]: rows of weights overlap, or the strides are too large", i);
+                const uintptr_t w = reinterpret_cast<uintptr_t>(e.weights);
+                places.weights.push_back(Written{w, w + 4 * (uintptr_t)span, span == (int64_t)c.n_layers * c.n_kv_heads * p.T});
+            }
+            places.add(p, d, c);
+            m.count = e.count;
+            m.from = m.to = packed_rows(p, d);
+            m.w = e.weights;
+            m.w_to = e.weights;
+            m.w_layer = m.t_layer = e.w_layer;
+            m.w_head = m.t_head = e.w_head;
+            m.idx = e.idx;
+        }
+        moves.push_back(m);
+    }
+    if (places.clash() || places.lengths_clash(lengths)) return fail(ctx, CB_EINVAL, "two parts of the call write the same memory");
+    return move_all(ctx, moves, c.n_layers, strm);
 }
 
 // The body of an entry point: the context checked, no exception past the C boundary.
@@ -472,8 +806,34 @@ cb_status cb_unpack(cb_ctx* ctx, int32_t n, const cb_packed* caches, const int32
 cb_status cb_attend(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* caches, const cb_attend_query* queries,
                     int32_t causal, int64_t window, void* stream) {
     return entry(ctx, "cb_attend", [&] {
-        return attend_impl(ctx, layer, n, caches, queries, causal, window, static_cast<cudaStream_t>(stream));
+        return attend_impl<AttendBatch>(ctx, layer, n, caches, queries, nullptr, causal, window, static_cast<cudaStream_t>(stream));
     });
+}
+
+cb_status cb_attend_tree(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* caches, const cb_attend_query* queries,
+                         const cb_tree* trees, void* stream) {
+    return entry(ctx, "cb_attend_tree", [&] {
+        if (!trees) return fail(ctx, CB_EINVAL, "trees is NULL");
+        return attend_impl<AttendTreeBatch>(ctx, layer, n, caches, queries, trees, 1, 0, static_cast<cudaStream_t>(stream));
+    });
+}
+
+cb_status cb_weigh(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* caches, const cb_weigh_query* queries,
+                   const cb_tree* trees, int32_t causal, int64_t window, float decay, void* stream) {
+    return entry(ctx, "cb_weigh", [&] {
+        return weigh_impl(ctx, layer, n, caches, queries, trees, causal, window, decay, static_cast<cudaStream_t>(stream));
+    });
+}
+
+cb_status cb_evict(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, const cb_packed* caches, const cb_packed* into,
+                   const cb_eviction* evictions, void* stream) {
+    return entry(ctx, "cb_evict", [&] {
+        return evict_impl(ctx, layer, n_layers, n, caches, into, evictions, static_cast<cudaStream_t>(stream));
+    });
+}
+
+cb_status cb_keep(cb_ctx* ctx, int32_t n, const cb_packed* caches, const cb_kept* kept, void* stream) {
+    return entry(ctx, "cb_keep", [&] { return keep_impl(ctx, n, caches, kept, static_cast<cudaStream_t>(stream)); });
 }
 
 }  // extern "C"

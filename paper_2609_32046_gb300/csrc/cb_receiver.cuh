@@ -100,6 +100,7 @@ struct AttendCut {
 };
 
 struct AttendBatch {
+    static constexpr bool kTrees = false;
     int32_t n;
     int32_t n_q_heads, n_kv_heads, G;
     float scale_log2e;
@@ -117,11 +118,85 @@ struct AttendBatch {
     AttendSeq s[kMaxBatch];
 };
 
+// What tokens see of one another's rows (cb_tree), sequence by sequence.
+struct TreeBits {
+    const uint32_t* seen;     // or null: each those up to itself
+    int64_t s_row;
+};
+
+// cb_attend_tree: `causal` is 1 and `window` 0.
+struct AttendTreeBatch : AttendBatch {
+    static constexpr bool kTrees = true;
+    TreeBits tree[kMaxBatch];
+};
+
+// cb_weigh.  The work is planned as that of tokens that see every row (AttendBatch: causal and window are 0): what
+// they see is `sees` (causal), `sees_window` and `tree`.
+struct WeighSeq {
+    const float* lse;
+    const float* before;      // or null
+    float* weights;
+    int64_t b_head, w_head;
+    int64_t fresh;            // rows at the end whose `before` is not read
+    TreeBits tree;
+};
+struct WeighBatch : AttendBatch {
+    int32_t sees;
+    float decay;
+    int64_t sees_window;
+    WeighSeq w[kMaxBatch];
+};
+
+// cb_evict: the rows of one cache that stay.
+struct RankSeq {
+    const float* weights;
+    int64_t w_layer, w_head;
+    int64_t T;
+    const int32_t* length;    // or null
+    int64_t keep, first, last;
+    int32_t* idx;             // [layer][head][keep]
+};
+struct RankBatch {
+    int32_t n;
+    int32_t n_layers, n_kv_heads;
+    RankSeq s[kMaxBatch];
+};
+
+// Rows that move within a cache or into another (cb_evict, cb_keep): row base + j of `to` becomes row base + idx[j]
+// of `from`, and so do their weights.
+struct MoveSeq {
+    PackedRows from, to;      // bases at the call's first layer
+    const float* w;           // or null
+    float* w_to;
+    int64_t w_layer, w_head, t_layer, t_head;
+    const int32_t* idx;
+    int64_t idx_list;         // entries of a (layer, head); 0: all have the same
+    int64_t count;            // entries at most; of a list of its own, those before the first -1
+    const int32_t* n_kept;    // or null: entries that count
+    int64_t T;                // rows of `from`
+    const int32_t* length;    // or null
+    int64_t drafted;          // base = rows - drafted; -1: 0
+    int32_t* left;            // or null: receives base + entries (lists of their own: min(rows, count))
+    int32_t in_place;
+};
+struct MoveBatch {
+    int32_t n;
+    int32_t n_layers, n_kv_heads;
+    uint32_t* err;
+    MoveSeq s[kMaxPackBatch];
+};
+
 cudaError_t launch_rotary(const RotaryBatch& b, int head_dim, int style, cudaStream_t st, int num_sms);
 cudaError_t launch_pack(const PackBatch& b, int head_dim, cudaStream_t st, int num_sms);
 cudaError_t launch_unpack(const PackBatch& b, int head_dim, cudaStream_t st, int num_sms);
 // Fills in pair0 and pairs, bounds window, launches, and clears stall where the kernel that has it ran.
 cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num_sms);
+cudaError_t launch_attend(AttendTreeBatch& b, int head_dim, cudaStream_t st, int num_sms);
+// Fills in pair0 and pairs, and launches.
+cudaError_t launch_weigh(WeighBatch& b, int head_dim, cudaStream_t st, int num_sms);
+cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms);
+cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int num_sms);
+cudaError_t launch_left(const MoveBatch& b, cudaStream_t st);     // writes MoveSeq::left, behind every launch_move of a call
 // Query rows of partial results that launch_attend may use on num_sms SMs.
 int64_t attend_part_rows(int num_sms);
 constexpr int kFewBlocksPerSm = 4;   // blocks of k_attend_few an SM holds at most

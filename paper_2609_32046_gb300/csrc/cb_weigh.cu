@@ -1,0 +1,186 @@
+// Attention weights gathered by the rows of a 4-bit cache (cb_weigh):
+//
+//   w_t = decay * w_t + sum over query rows (token, head of the group) that see t of exp2(z_t - lse * log2(e)),
+//   z_t = scale * log2(e) * <q, k_t>
+//
+// Products are exact (a packed key is an fp16 number and a bf16 number), sums are fp32.
+#include <cmath>
+#include <cstdint>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "cb_few.cuh"
+#include "cb_weigh.cuh"
+
+namespace cbk {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kStages = 2;
+
+// Copies 32 positions' keys; mine: the row of this lane's.  The codes of a position that has none are some row's: its
+// scales are zeros.
+template <int D>
+__device__ __forceinline__ void copy_keys(uint32_t to, const Segment& x, int mine) {
+    constexpr int P = D / 32;             // pieces of a row's codes
+    constexpr int N = 32 / P;             // rows a copy of the warp takes
+    using S = Stage<D, 1>;
+    const int lane = threadIdx.x & 31, p = lane % P;
+    const uint32_t row = max(mine, 0);
+#pragma unroll
+    for (int i = 0; i < 32 / N; ++i) {
+        const int at = lane / P + i * N;
+        copy16(to + S::at(at, p), x.code[0] + (uint64_t)__shfl_sync(0xFFFFFFFFu, row, at) * (D / 2) + p * 16);
+    }
+    copy_small<D / 16>(to + S::kCodes + lane * (D / 16),
+                       reinterpret_cast<const uint8_t*>(x.scale[0]) + (uint64_t)row * (D / 16), mine >= 0);
+}
+
+// Looks a lane's scales over: what is none becomes 0.  True where every scale of the warp's rows is within
+// 2^-14 .. 2^7 (values_f16's NEAR).
+template <int D>
+__device__ __forceinline__ bool look_over_keys(uint8_t* stage, uint32_t* err) {
+    constexpr int W = D / 64;             // words of two scales in a row
+    uint32_t* ks = reinterpret_cast<uint32_t*>(stage + Stage<D, 1>::kCodes) + (threadIdx.x & 31) * W;
+    const uint32_t top = __vmaxu2(ks[0], ks[W - 1]), low = __vminu2(ks[0], ks[W - 1]);
+    const bool far = max(top & 0xFFFFu, top >> 16) > 0x4300u || min(low & 0xFFFFu, low >> 16) < 0x3880u;
+    if (!__any_sync(0xFFFFFFFFu, far)) return true;
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) ks[i] = checked_scale(ks[i] & 0xFFFFu, bad) | checked_scale(ks[i] >> 16, bad) << 16;
+    if (bad) atomicOr(err, kErrPackScale);
+    __syncwarp();
+    return false;
+}
+
+// A block takes its run of units (cb_attend.cuh); its four warps take 32 positions in turn, each with its own
+// copies.  S^T [16 positions][8 rows] = K Q^T (cb_few.cuh), the rows' weights are added up over a quad's lanes, and
+// every position's sum is written by one lane.  MANY: more than 8 NT rows, a tile of them after the other.
+template <int D, int NT, bool MANY>
+__global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_constant__ WeighBatch b) {
+    using S = Stage<D, 1>;
+    constexpr int ROWS = 8 * NT;
+    __shared__ __align__(128) uint8_t smem[kWarps * kStages * S::kBytes];
+    __shared__ int pre[kMaxBatch + 1];
+    __shared__ Segment x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
+    attend_units(b, kWeighRows, pre);
+    const int g = blockIdx.x % b.n_kv_heads, run = blockIdx.x / b.n_kv_heads;
+    const Runs runs = attend_runs(pre[b.pairs], gridDim.x / b.n_kv_heads);
+    if (run >= runs.blocks) return;
+    const int run0 = attend_run(runs, run), run1 = attend_run(runs, run + 1);
+    uint8_t* stages = smem + warp * kStages * S::kBytes;
+    const uint32_t to = sm100::smem_u32(stages);
+    for (int unit = run0; unit < run1;) {
+        if (threadIdx.x == 0) attend_segment(b, pre, 1, g, unit, run1, D, kWeighRows, &x);
+        __syncthreads();
+        const WeighSeq& w = b.w[x.seq];
+        const WeighRows rows(b, x);
+        int t0 = warp * kStep, ahead = t0;
+        uint32_t page = segment_page(x, ahead + lane);
+#pragma unroll
+        for (int i = 0; i < kStages; ++i) {
+            if (ahead < x.len && !rows.blind(ahead, kStep)) copy_keys<D>(to + i * S::kBytes, x, segment_row(x, ahead + lane, page, b.err));
+            copy_commit();
+            ahead += kWarps * kStep;
+            page = segment_page(x, ahead + lane);
+        }
+        uint32_t q[NT][D / 32][4];
+        float zs[NT][2], nl[NT][2];       // of columns 2 tig and 2 tig + 1: factor of the logits, -lse * log2(e)
+        auto load = [&](int row0) {
+            load_queries<D, NT>(b, b.s[x.seq], g, row0, x.rows, q, zs,
+                                [&](int row) { return isfinite(rows.lse(w, g, row)); });
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = row0 + nt * 8 + 2 * tig + h;
+                    const float lse = row < x.rows ? rows.lse(w, g, row) : INFINITY;
+                    nl[nt][h] = isfinite(lse) ? lse * -1.4426950408889634f : -INFINITY;
+                }
+        };
+        if (!MANY) load(0);
+        for (int turn = 0; t0 < x.len; t0 += kWarps * kStep) {
+            uint8_t* st = stages + turn * S::kBytes;
+            const int own = t0 + 8 * tig + place(gid);          // the position whose sum this lane writes
+            const float before = rows.before(w, g, own);
+            copy_wait<kStages - 1>();
+            __syncwarp();
+            float s[4] = {};                                    // of positions t0 + 8 k + place(gid)
+            if (!rows.blind(t0, kStep)) {
+                const bool near = look_over_keys<D>(st, b.err), edge = rows.edge(t0, kStep);
+#pragma unroll 1
+                for (int row0 = 0; row0 < (MANY ? x.rows : 1); row0 += ROWS) {
+                    if (MANY) load(row0);
+                    float z[2][NT][4];
+                    if (near) {
+                        score_keys<D, NT, true, 1>(st, 0, q, z[0]);
+                        score_keys<D, NT, true, 1>(st, 16, q, z[1]);
+                    } else {
+                        score_keys<D, NT, false, 1>(st, 0, q, z[0]);
+                        score_keys<D, NT, false, 1>(st, 16, q, z[1]);
+                    }
+                    if (edge) {
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t bits = rows.seen(w, (row0 + nt * 8 + 2 * tig + h) / b.G, t0);
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    if (!(bits >> (8 * k + place(gid)) & 1u)) z[k / 2][nt][2 * (k % 2) + h] = -INFINITY;
+                            }
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            s[k] += ex2(fmaf(z[k / 2][nt][2 * (k % 2)], zs[nt][0], nl[nt][0])) +
+                                    ex2(fmaf(z[k / 2][nt][2 * (k % 2) + 1], zs[nt][1], nl[nt][1]));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], 1);
+                s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], 2);
+            }
+            const float sum = tig == 0 ? s[0] : tig == 1 ? s[1] : tig == 2 ? s[2] : s[3];
+            if (own < x.len) w.weights[(int64_t)g * w.w_head + x.begin + own] = fmaf(b.decay, before, sum);
+            __syncwarp();
+            if (ahead < x.len && !rows.blind(ahead, kStep)) copy_keys<D>(to + turn * S::kBytes, x, segment_row(x, ahead + lane, page, b.err));
+            copy_commit();
+            ahead += kWarps * kStep;
+            page = segment_page(x, ahead + lane);
+            turn = turn + 1 == kStages ? 0 : turn + 1;
+        }
+        copy_wait<0>();
+        unit += x.n;
+        __syncthreads();
+    }
+}
+
+template <int D, int NT, bool MANY>
+cudaError_t launch_few(const WeighBatch& b, int64_t units, int num_sms, cudaStream_t st) {
+    const int64_t most = num_sms * 4 / b.n_kv_heads, all = units / b.n_kv_heads;
+    const int64_t runs = all < most ? all : most;
+    k_weigh_few<D, NT, MANY><<<(int)(runs > 1 ? runs : 1) * b.n_kv_heads, kWarps * 32, 0, st>>>(b);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_weigh(WeighBatch& b, int head_dim, cudaStream_t st, int num_sms) {
+    int rows = 0;
+    for (int i = 0; i < b.n; ++i) rows = b.span[i].m > rows ? b.span[i].m : rows;
+    rows *= b.G;
+    if (rows == 0) return cudaSuccess;
+    b.sees_window = b.sees_window < kFarWindow ? b.sees_window : kFarWindow;
+    const int64_t units = attend_pairs(b, kWeighRows);
+    if (head_dim == 128)
+        return rows <= 8 ? launch_few<128, 1, false>(b, units, num_sms, st)
+                         : rows <= 16 ? launch_few<128, 2, false>(b, units, num_sms, st) : launch_few<128, 2, true>(b, units, num_sms, st);
+    return rows <= 8 ? launch_few<64, 1, false>(b, units, num_sms, st)
+                     : rows <= 16 ? launch_few<64, 2, false>(b, units, num_sms, st) : launch_few<64, 2, true>(b, units, num_sms, st);
+}
+
+}  // namespace cbk
