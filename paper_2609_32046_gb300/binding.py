@@ -335,9 +335,9 @@ class PackedKV:
         if paged:
             d.page_size, d.s_page, d.n_pages = self.page_size, self._page, self.n_pages
         self._desc = d
-        # the rows cached, and what _described makes of them once it is asked: an assignment puts a new list in its
+        # the rows cached, and what _described and _described_room make of them once they are asked: an assignment puts a new list in its
         # place, so that a call of another thread never leaves the bytes of one state in the next
-        self._state = [0, None]
+        self._state = [0, None, None]
         self._pages = None
         if paged:
             self._set_pages(pages)
@@ -381,7 +381,7 @@ class PackedKV:
         self._pages = pages
         self.capacity = pages.numel() * self.page_size
         self._desc.pages = pages.data_ptr()
-        self._state = [self.T, None]
+        self._state = [self.T, None, None]
 
     @property
     def T(self) -> int:
@@ -391,7 +391,7 @@ class PackedKV:
     def T(self, T: int):
         if not 0 <= T <= self.capacity:
             raise ValueError("T = %d not in [0, %d]" % (T, self.capacity))
-        self._state = [int(T), None]
+        self._state = [int(T), None, None]
 
     @property
     def length(self):
@@ -402,7 +402,7 @@ class PackedKV:
         _require(x is None or (_is_int32(x) and x.numel() == 1), "length is one int32")
         self._length = x
         self._desc.length = None if x is None else x.data_ptr()
-        self._state = [self.T, None]
+        self._state = [self.T, None, None]
 
     def _described(self) -> bytes:
         """The bytes of desc(): a call joins those of its caches."""
@@ -410,6 +410,13 @@ class PackedKV:
         if state[1] is None:
             state[1] = bytes(self.desc(state[0]))
         return state[1]
+
+    def _described_room(self) -> bytes:
+        """The bytes of desc(capacity)."""
+        state = self._state
+        if state[2] is None:
+            state[2] = bytes(self.desc(self.capacity))
+        return state[2]
 
     def desc(self, T: Optional[int] = None) -> cb_packed:
         """A description of its own, with T rows (default: those cached)."""
@@ -670,7 +677,7 @@ class CacheBack:
             if not (shape[1] == p.n_kv_heads and shape[3] == p.head_dim and shape[0] == layers):
                 raise ValueError("K and V do not match the cache")
         kv = b"".join([bytes(kv_desc(K, V)) for K, V in zip(Ks, Vs)])
-        held = b"".join([bytes(p.desc(p.capacity)) for p in caches])
+        held = b"".join([p._described_room() for p in caches])
         # idx, counts, offsets and rows of the call, one array of eight-byte numbers
         parts = array("q", [0 if x is None else x.data_ptr() for x in idx])
         parts.extend(map(int, counts))
@@ -790,40 +797,65 @@ class CacheBack:
         that have gathered nothing yet.  All of them may be tensors with the sequences in their first dimension.
         Returns outs."""
         n = len(caches)
-        cfg = self.cfg
+        cfg, like = self.cfg, self._shape
         _require(len(Qs) == len(lses) == n and (weights is None or len(weights) == n) and (outs is None or len(outs) == n) and
                  (trees is None or len(trees) == n), "one entry per cache in every list")
         _require(weights is not None or outs is not None, "weights or outs")
         _require(not window or causal, "a window goes with causal")
         _require(trees is None or (causal and not window), "trees go with causal and no window")
-        fresh = _each(fresh, n, "fresh")
-        fields = array("q")                   # of the header's cb_weigh_query, eight bytes each
-        given = []
-        for i, p in enumerate(caches):
-            self._fits(p)
-            Q, lse = Qs[i], lses[i]
-            before = None if weights is None else weights[i]
-            out = before if outs is None or outs[i] is None else outs[i]
-            shape, qt = Q.shape, Q.stride()
-            if not (len(shape) == 3 and shape[1] == cfg.n_q_heads and shape[2] == cfg.head_dim and qt[2] == 1 and _is_bf16(Q)):
-                raise ValueError("queries are bf16 [m][Hq][d]")
-            if not (lse.shape == shape[:2] and lse.is_contiguous() and _is_f32(lse)):
-                raise ValueError("lse is fp32 [m][Hq]")
-            if out is None:
-                raise ValueError("weights or outs")
-            for x in (out,) if before is None else (out, before):
-                if not (x.dim() == 2 and _is_f32(x) and x.shape[0] == p.n_kv_heads and x.shape[1] >= p.T and
-                        (x.stride(1) == 1 or x.shape[1] == 1)):
-                    raise ValueError("weights are fp32 [Hkv][rows], rows for all that the cache holds")
-            m = shape[0]
-            fields.extend((Q.data_ptr(), lse.data_ptr(), _address(before), out.data_ptr(), m, m if fresh[i] is None else int(fresh[i]),
-                           qt[0], qt[1], 0 if before is None else before.stride(0), out.stride(0)))
-            given.append(out)
+        to = weights if outs is None else outs
+        most = 0
+        for p in caches:
+            if p._shape != like:
+                self._fits(p)
+            if p.T > most:
+                most = p.T
+        if n and hasattr(Qs, "data_ptr") and hasattr(lses, "data_ptr") and hasattr(to, "data_ptr") and \
+                (weights is None or hasattr(weights, "data_ptr")) and not isinstance(fresh, (list, tuple)):
+            # one tensor each: the sequences' addresses by arithmetic
+            shape, qt, lt = Qs.shape, Qs.stride(), lses.stride()
+            if not (len(shape) == 4 and shape[2] == cfg.n_q_heads and shape[3] == cfg.head_dim and qt[3] == 1 and _is_bf16(Qs)):
+                raise ValueError("queries are bf16 [sequences][m][Hq][d]")
+            m = shape[1]
+            if not (lses.shape == shape[:3] and _is_f32(lses) and (m == 0 or (lt[2] == 1 and (m == 1 or lt[1] == shape[2])))):
+                raise ValueError("lse is fp32 [sequences][m][Hq]")
+            wt = to.stride()
+            bt = wt if weights is None or weights is to else weights.stride()
+            for x, t in ((to, wt),) if weights is None or weights is to else ((to, wt), (weights, bt)):
+                if not (len(t) == 3 and _is_f32(x) and x.shape[1] == cfg.n_kv_heads and x.shape[2] >= most and (t[2] == 1 or x.shape[2] == 1)):
+                    raise ValueError("weights are fp32 [sequences][Hkv][rows], rows for all that a cache holds")
+            before = _address(weights)
+            start = (Qs.data_ptr(), lses.data_ptr(), before, to.data_ptr())
+            fields = array("q", start + (m, m if fresh is None else int(fresh), qt[1], qt[2], bt[1], wt[1])) * n
+            for at, step in enumerate((2 * qt[0], 4 * lt[0], 4 * bt[0] if before else 0, 4 * wt[0])):
+                if n > 1 and step:
+                    fields[at::10] = array("q", range(start[at], start[at] + n * step, step))
+        else:
+            fresh = _each(fresh, n, "fresh")
+            fields = array("q")               # of the header's cb_weigh_query, eight bytes each
+            for i, p in enumerate(caches):
+                Q, lse = Qs[i], lses[i]
+                before = None if weights is None else weights[i]
+                out = before if outs is None or outs[i] is None else outs[i]
+                shape, qt = Q.shape, Q.stride()
+                if not (len(shape) == 3 and shape[1] == cfg.n_q_heads and shape[2] == cfg.head_dim and qt[2] == 1 and _is_bf16(Q)):
+                    raise ValueError("queries are bf16 [m][Hq][d]")
+                if not (lse.shape == shape[:2] and lse.is_contiguous() and _is_f32(lse)):
+                    raise ValueError("lse is fp32 [m][Hq]")
+                if out is None:
+                    raise ValueError("weights or outs")
+                for x in (out,) if before is None or before is out else (out, before):
+                    if not (x.dim() == 2 and _is_f32(x) and x.shape[0] == cfg.n_kv_heads and x.shape[1] >= p.T and
+                            (x.stride(1) == 1 or x.shape[1] == 1)):
+                        raise ValueError("weights are fp32 [Hkv][rows], rows for all that the cache holds")
+                m = shape[0]
+                fields.extend((Q.data_ptr(), lse.data_ptr(), _address(before), out.data_ptr(), m, m if fresh[i] is None else int(fresh[i]),
+                               qt[0], qt[1], 0 if before is None else before.stride(0), out.stride(0)))
         held = b"".join([p._state[1] or p._described() for p in caches])
         bits = None if trees is None else self._trees(trees, fields[4::10])
         self._check(self.lib.cb_weigh(self.h, int(layer), n, held, fields.buffer_info()[0], None if bits is None else bits.buffer_info()[0],
                                       1 if causal else 0, int(window), float(decay), _stream_on(stream, caches[0].k) if n else 0))
-        return given if outs is None else outs
+        return [w if o is None else o for w, o in zip(weights, outs)] if isinstance(outs, (list, tuple)) and weights is not None else to
 
     def evict(self, caches: Sequence, weights: Sequence, keep, first: int = 0, last: int = 0, into: Optional[Sequence] = None,
               weights_into: Optional[Sequence] = None, idx: Optional[Sequence] = None, lengths: Optional[Sequence] = None,
@@ -864,8 +896,8 @@ class CacheBack:
             left.append(own)
             ws, ts = w.stride(), (0, 0) if out is None else out.stride()
             fields.extend((w.data_ptr(), _address(out), ws[0], ws[1], ts[0], ts[1], k, int(first), int(last), at.data_ptr(), _address(own)))
-        held = b"".join([bytes(p.desc()) for p in caches])
-        taken = None if into is None else b"".join([bytes(p.desc() if p is q else p.desc(p.capacity)) for p, q in zip(into, caches)])
+        held = b"".join([p._state[1] or p._described() for p in caches])
+        taken = None if into is None else b"".join([p._described() if p is q else p._described_room() for p, q in zip(into, caches)])
         self._check(self.lib.cb_evict(self.h, int(layer), int(layers), n, held, taken, fields.buffer_info()[0],
                                       _stream_on(stream, caches[0].k) if n else 0))
         if lengths is None:
@@ -885,32 +917,63 @@ class CacheBack:
         dimension."""
         n = len(caches)
         _require(len(idx) == n and all(x is None or len(x) == n for x in (counts, weights, lengths)), "one entry per cache in every list")
-        drafted = [int(x) for x in _each(drafted, n, "drafted")]
-        fields, left = array("q"), []         # of the header's cb_kept, eight bytes each
+        drafted = _each(drafted, n, "drafted")
+        like, left = self._shape, []
+        many = hasattr(idx, "data_ptr"), hasattr(counts, "data_ptr"), hasattr(weights, "data_ptr")      # one tensor each
+        fields = array("q")                   # of the header's cb_kept, eight bytes each
+        if many[0]:
+            st = idx.stride()
+            _require(_is_int32(idx) and idx.dim() == 2 and (st[1] == 1 or idx.shape[1] < 2), "idx holds an int32 a row")
+            at, step, rows = idx.data_ptr(), 4 * st[0], idx.shape[1]
+        if many[1]:
+            _require(_is_int32(counts) and counts.numel() == n, "a count is one int32")
+            count, count_step = counts.data_ptr(), 4 * counts.stride(0) if counts.dim() else 0
+        elif counts is None:
+            count = count_step = 0
+        if many[2]:
+            ws = weights.stride()
+            most = max([p.T for p in caches], default=0)
+            _require(len(ws) == 4 and _is_f32(weights) and tuple(weights.shape[1:3]) == like[:2] and weights.shape[3] >= most and
+                     (ws[3] == 1 or weights.shape[3] == 1), "weights are fp32 [sequences][layers][Hkv][rows]")
+            w, w_step, ws = weights.data_ptr(), 4 * ws[0], ws[1:3]
+        elif weights is None:
+            w = w_step = 0
+            ws = (0, 0)
         for i, p in enumerate(caches):
-            self._fits(p)
-            x, count = idx[i], None if counts is None else counts[i]
-            if not (_is_int32(x) and x.dim() == 1 and x.is_contiguous()):
-                raise ValueError("idx holds an int32 a row")
-            _require(count is None or (_is_int32(count) and count.numel() == 1), "a count is one int32")
-            w = None if weights is None else weights[i]
-            if w is not None and not (w.dim() == 3 and _is_f32(w) and w.shape[0] == p.n_layers and w.shape[1] == p.n_kv_heads and
-                                      w.shape[2] >= p.T and (w.stride(2) == 1 or w.shape[2] == 1)):
-                raise ValueError("weights are fp32 [layers][Hkv][rows]")
+            if p._shape != like:
+                self._fits(p)
+            if not many[0]:
+                x = idx[i]
+                if not (_is_int32(x) and x.dim() == 1 and x.is_contiguous()):
+                    raise ValueError("idx holds an int32 a row")
+                at, step, rows = x.data_ptr(), 0, x.numel()
+            if not many[1] and counts is not None:
+                x = counts[i]
+                _require(x is None or (_is_int32(x) and x.numel() == 1), "a count is one int32")
+                count, count_step = _address(x), 0
+            if not many[2] and weights is not None:
+                x = weights[i]
+                w, w_step, ws = _address(x), 0, (0, 0)
+                if x is not None:
+                    ws = x.stride()
+                    _require(len(ws) == 3 and _is_f32(x) and tuple(x.shape[:2]) == like[:2] and x.shape[2] >= p.T and
+                             (ws[2] == 1 or x.shape[2] == 1), "weights are fp32 [layers][Hkv][rows]")
             own = p.length if lengths is None else lengths[i]
-            _require(own is None or (_is_int32(own) and own.numel() == 1), "a length is one int32")
-            _require(own is not None or (count is None and p.length is None),
-                     "lengths and counts on the device need a length that receives the rows left")
-            left.append(own)
-            ws = (0, 0) if w is None else w.stride()
-            fields.extend((x.data_ptr(), x.numel(), _address(count), drafted[i], _address(w), ws[0], ws[1], _address(own)))
-        held = b"".join([bytes(p.desc()) for p in caches])
+            if own is None:
+                _require(not count and p.length is None, "lengths and counts on the device need a length that receives the rows left")
+                left.append(rows)
+                to = 0
+            else:
+                _require(own.numel() == 1 and _is_int32(own), "a length is one int32")
+                left.append(None)
+                to = own.data_ptr()
+            fields.extend((at + i * step, rows, count + i * count_step, drafted[i], w + i * w_step, ws[0], ws[1], to))
+        held = b"".join([p._state[1] or p._described() for p in caches])
         self._check(self.lib.cb_keep(self.h, n, held, fields.buffer_info()[0], _stream_on(stream, caches[0].k) if n else 0))
         if lengths is None:
-            for p, x, own, m in zip(caches, idx, left, drafted):
-                if own is None:
-                    p.T = p.T - m + x.numel()
-
+            for p, rows, m in zip(caches, left, drafted):
+                if rows is not None:
+                    p.T = p.T - m + rows
     def _queries(self, Q, out, lse):
         """One sequence's fields of a cb_attend_query, looked over."""
         qt, ot = Q.stride(), out.stride()

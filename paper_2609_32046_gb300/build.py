@@ -22,7 +22,7 @@ LIB_NAME = "libcacheback.so"
 LIB_PATH = os.path.join(PKG, LIB_NAME)
 SOURCES = ["cb_api.cu", "cb_score.cu", "cb_score_tc.cu", "cb_select.cu", "cb_compact.cu", "cb_gather.cu", "cb_rope.cu",
            "cb_depage.cu", "cb_receiver.cu", "cb_rotary.cu", "cb_pack.cu", "cb_attend.cu",
-           "cb_attend_tc.cu", "cb_weigh.cu", "cb_evict.cu"]
+           "cb_attend_tc.cu", "cb_weigh.cu", "cb_weigh_tc.cu", "cb_evict.cu"]
 # files compiled in several parts at the same time: a macro and its values
 PARTS = {"cb_score_tc.cu": ("CB_TC_PART", (0, 64, 128))}
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

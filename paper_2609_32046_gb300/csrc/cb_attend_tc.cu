@@ -34,6 +34,7 @@
 #include "cb_attend.cuh"
 #include "cb_receiver.cuh"
 #include "cb_sm100_attend.cuh"
+#include "cb_tc_roles.cuh"
 
 namespace cbk {
 namespace {
@@ -51,9 +52,6 @@ constexpr int kStages = 2;
 constexpr int kJoinBlocks = 32;             // blocks that join one item
 constexpr float kBits = 7.f;                // weights are exp2(z - M'), M' = M - 7
 constexpr float kGrow = 8.f;                // growth of a row's maximum that M follows
-constexpr uint32_t kPollNs = 1000000u;
-constexpr uint64_t kDrainNs = 1000000000ull;
-
 struct Ctl {
     uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
     uint64_t s_full[2], p_full[2], pv_done[2], done;
@@ -71,52 +69,6 @@ constexpr int kCtlBytes = 1024 + (kMaxPairs + 1) * 4;
 template <int D>
 constexpr int smem_bytes() {
     return 2 * kTile * D * 2 + kStages * 2 * kTile * D * 2 + 8 * (32 * D / 2 + 256) + kCtlBytes + 1024;
-}
-
-__device__ __forceinline__ uint64_t now_ns() {
-    uint64_t t;
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-    return t;
-}
-
-// Bounded wait: false when it gave up or another role did (bits 8 + tag of the error word name the wait).
-// (Inline: a call would have to do with the registers of every role.)
-__device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity, Ctl* c, uint32_t* err, int tag) {
-    const uint64_t t0 = now_ns();
-    do {
-        if (mbar_try_wait_hint(bar, parity, kPollNs)) return true;
-        if (*reinterpret_cast<volatile int*>(&c->abort)) return false;
-    } while (now_ns() - t0 <= c->wait_ns);
-    *reinterpret_cast<volatile int*>(&c->abort) = 1;
-    atomicOr(err, kErrTimeout | (1u << (8 + tag)));
-    return false;
-}
-__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, Ctl* c, uint32_t* err, int tag) {
-    return mbar_try_wait(bar, parity) || poll(bar, parity, c, err, tag);
-}
-// The same for a whole warp, which stays together whatever its lanes saw.
-__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl* c, uint32_t* err, int tag) {
-    return __all_sync(0xFFFFFFFFu, wait(bar, parity, c, err, tag));
-}
-__device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
-    const uint64_t t0 = now_ns();
-    while (!mbar_try_wait(bar, parity))
-        if (now_ns() - t0 > kDrainNs) return;
-}
-
-__device__ __forceinline__ uint64_t desc(uint32_t lo, uint32_t hi) {
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(lo), "r"(hi));
-    return d;
-}
-
-// A 16-byte piece of a K-major operand with 128-byte rows (64 elements a block): row, piece 0..7 of block.
-__device__ __forceinline__ uint32_t piece(int block, int rows, int row, int p) {
-    return (uint32_t)(block * rows * 128 + row * 128 + ((p ^ (row & 7)) << 4));
-}
-
-__device__ __forceinline__ void st_piece(uint8_t* base, uint32_t at, const uint32_t (&w)[4]) {
-    *reinterpret_cast<uint4*>(base + at) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Codes and scales of a tile on their way: each of the eight warps that unpack copies its own share of the
@@ -171,9 +123,7 @@ __device__ __forceinline__ void copy_v(uint32_t to, const Segment& x, int lo, in
 }
 
 // Every column of a tile that is seen at all: what a row's bits do not say otherwise.
-struct AllBits {
-    __device__ __forceinline__ uint32_t operator()(int) const { return 0xFFFFFFFFu; }
-};
+struct AllBits {};
 // A drafted token's bits for 32 columns from `first` on: column 0 is row u0, counted from token 0's.
 struct RowBits {
     const uint32_t* row;

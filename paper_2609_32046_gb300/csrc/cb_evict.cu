@@ -20,7 +20,7 @@ __device__ __forceinline__ int64_t rows_of(int64_t T, const int32_t* length) {
 constexpr int kRankThreads = 512;
 constexpr int kBins = 2048;
 constexpr int kRankPasses = 3;
-constexpr int kRankKeys = 24 * 1024;         // keys of a block's slice held in shared memory (96 KB)
+constexpr int kRankKeys = 24 * 1024;         // keys of a block's slice held in shared memory at most (96 KB)
 constexpr int kRankCluster = 8;
 
 // Larger weights have larger keys; -0 is 0, NaN below all.
@@ -56,9 +56,9 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t& before, uin
 // 10 bits from the top finds the key where the budget runs out (histograms joined in the first block's shared
 // memory); rows above it stay, and of those at it the lowest.
 template <int C>
-__global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ RankBatch b) {
-    extern __shared__ uint32_t keys[];                   // [kRankKeys]
-    __shared__ uint32_t own[kBins], all[kRankPasses][kBins];
+__global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ RankBatch b, uint32_t held) {
+    extern __shared__ uint32_t keys[];                   // [held]
+    __shared__ uint32_t own[kBins], all[C > 1 ? kRankPasses : 1][C > 1 ? kBins : 1];
     __shared__ uint32_t scan[kRankThreads / 32];
     __shared__ uint32_t found[3];                        // bin, keys above it, keys in it
     __shared__ uint32_t counts[2];                       // this block's keys above the last, and at it
@@ -84,10 +84,12 @@ __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ R
     const uint32_t per = ((n + C - 1) / C + 3) & ~3u;
     const uint32_t lo = min(n, rank * per), len = min(n, lo + per) - lo;
     w += lo;
-    auto key = [&](uint32_t i) { return i < kRankKeys ? keys[i] : rank_key(__ldg(w + i)); };
+    auto key = [&](uint32_t i) { return i < held ? keys[i] : rank_key(__ldg(w + i)); };
 
-    for (int i = threadIdx.x; i < kRankPasses * kBins; i += kRankThreads) all[i / kBins][i % kBins] = 0;
-    for (uint32_t i = threadIdx.x; i < min(len, (uint32_t)kRankKeys); i += kRankThreads) keys[i] = rank_key(__ldg(w + i));
+    if (C > 1)
+        for (int i = threadIdx.x; i < kRankPasses * kBins; i += kRankThreads) all[i / kBins][i % kBins] = 0;
+#pragma unroll 8
+    for (uint32_t i = threadIdx.x; i < min(len, held); i += kRankThreads) keys[i] = rank_key(__ldg(w + i));
     if (C > 1) cluster.sync();
     uint32_t need = want, prefix = 0, above = 0, equal = 0;      // above, equal: this block's
     int shift = 32;
@@ -102,7 +104,7 @@ __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ R
             if (pass == 0 || k >> up == prefix) atomicAdd(&own[(k >> shift) & ((1u << bits) - 1)], 1u);
         }
         __syncthreads();
-        uint32_t* joined = C > 1 ? cluster.map_shared_rank(all[pass], 0) : own;
+        uint32_t* joined = C > 1 ? cluster.map_shared_rank(all[C > 1 ? pass : 0], 0) : own;
         if (C > 1) {
             for (int i = threadIdx.x; i < kBins; i += kRankThreads)
                 if (own[i]) atomicAdd(joined + i, own[i]);
@@ -215,17 +217,19 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
     const MoveSeq& s = b.s[blockIdx.z];
     const int lists = b.n_layers * b.n_kv_heads;
     const int t = threadIdx.x % GROUP;
-    const int unit = GROUP == 32 ? blockIdx.x * (256 / 32) + threadIdx.x / 32 : blockIdx.x / blocks;
-    const int part = GROUP == 32 ? 0 : blockIdx.x % blocks;
-    const int64_t L = rows_of(s.T, s.length);
-    const int64_t base = s.drafted < 0 ? 0 : L - s.drafted;
+    const int group = GROUP == 32 ? blockIdx.x * (256 / 32) + threadIdx.x / 32 : blockIdx.x;
+    const int unit = group / blocks, part = group % blocks;
+    // (of lists of their own, only the thread that writes the number of rows reads the length)
+    const bool lists_own = s.drafted < 0, says = group == 0 && t == 0 && s.left && !s.left_later;
+    const int64_t L = !lists_own || says ? rows_of(s.T, s.length) : 0;
+    const int64_t base = lists_own ? 0 : L - s.drafted, limit = lists_own ? s.T : s.drafted;
     int64_t count = s.count;
     if (s.n_kept) count = max((int64_t)0, min((int64_t)*s.n_kept, count));
-    if (s.drafted < 0) count = min(count, L);
     if (base < 0) {
-        if (unit == 0 && t == 0) atomicOr(b.err, kErrPackRow);
+        if (group == 0 && t == 0) atomicOr(b.err, kErrPackRow);
         return;
     }
+    if (says) *s.left = (int32_t)(lists_own ? min(L, count) : base + count);
     if (unit >= 2 * lists) return;            // (a whole group)
     const int kv = unit % 2, list = unit / 2, l = list / b.n_kv_heads, g = list % b.n_kv_heads;
     const int64_t from0 = l * s.from.s_layer + g * s.from.s_head, to0 = l * s.to.s_layer + g * s.to.s_head;
@@ -237,7 +241,7 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
     const float* w = weigh ? s.w + l * s.w_layer + g * s.w_head + base : nullptr;
     float* w_to = weigh ? s.w_to + l * s.t_layer + g * s.t_head + base : nullptr;
     const int32_t* idx = s.idx + list * s.idx_list;
-    uint2* rows[2] = {where[0] + threadIdx.x / GROUP * GROUP, where[1] + threadIdx.x / GROUP * GROUP};
+    uint2* rows = where[0] + threadIdx.x / GROUP * GROUP;      // and 256 on
 
     // the row of the thread at step j0, looked up: its entry (-1: none)
     auto look_up = [&](int64_t j0, uint2* to) {
@@ -246,7 +250,8 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
         int64_t i = -1;
         if (j < count) {
             i = idx[j];
-            if (i < j || i >= (s.drafted < 0 ? L : s.drafted)) {
+            if (lists_own && i == -1) {
+            } else if (i < j || i >= limit) {
                 atomicOr(b.err, kErrCompactIndex);
                 i = -1;
             }
@@ -282,16 +287,16 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
             if (weigh) h.weight = ld4(w + i);
         }
     };
-    const int64_t step = (int64_t)GROUP * (GROUP == 32 ? 1 : blocks);
+    const int64_t step = (int64_t)GROUP * blocks;
     int64_t j0 = (int64_t)part * GROUP;
     const int64_t steps = (count + step - 1) / step;      // (the same for all of a cluster)
-    int64_t i = look_up(j0, rows[0]);
+    int64_t i = look_up(j0, rows);
     meet();
     Held<D> h;
-    load(rows[0], i, h);
+    load(rows, i, h);
     for (int64_t n = 0; n < steps; ++n, j0 += step) {
-        uint2* here = rows[n & 1];
-        uint2* next = rows[~n & 1];
+        uint2* here = rows + (n & 1) * 256;
+        uint2* next = rows + (~n & 1) * 256;
         const int64_t i1 = n + 1 < steps ? look_up(j0 + step, next) : -1;
         if (GROUP != 32 && clustered) cg::this_cluster().sync();
         else meet();
@@ -314,16 +319,14 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
     }
 }
 
-// How many rows are left: behind k_move, which reads the lengths.
+// How many rows are left of the caches whose lengths k_move's groups read.
 __global__ void k_left(const __grid_constant__ MoveBatch b) {
     const int i = threadIdx.x;
-    const bool mine = i < b.n && b.s[i].left;
-    const MoveSeq& s = b.s[mine ? i : 0];
-    const int64_t L = mine ? rows_of(s.T, s.length) : 0;
+    if (i >= b.n || !b.s[i].left_later) return;
+    const MoveSeq& s = b.s[i];
+    const int64_t L = rows_of(s.T, s.length);
     int64_t count = s.count;
-    if (mine && s.n_kept) count = max((int64_t)0, min((int64_t)*s.n_kept, count));
-    __syncwarp();                       // (lengths are read before any is written)
-    if (!mine) return;
+    if (s.n_kept) count = max((int64_t)0, min((int64_t)*s.n_kept, count));
     if (s.drafted < 0) *s.left = (int32_t)min(L, count);
     else if (L >= s.drafted) *s.left = (int32_t)(L - s.drafted + count);
 }
@@ -331,16 +334,22 @@ __global__ void k_left(const __grid_constant__ MoveBatch b) {
 template <int D>
 cudaError_t launch(const MoveBatch& b, int64_t most, bool in_place, int num_sms, cudaStream_t st) {
     const int units = 2 * b.n_layers * b.n_kv_heads;
-    if (most <= 64) {
-        k_move<D, 32><<<dim3((units + 7) / 8, 1, b.n), 256, 0, st>>>(b, 1, 0);
+    if (!in_place || most <= 64) {
+        // warps of a list: as many as fill the GPU, a step's rows each at least
+        int64_t warps = 1;
+        if (!in_place) {
+            warps = 48 * (int64_t)num_sms / ((int64_t)units * b.n);
+            if (warps > (most + 31) / 32) warps = (most + 31) / 32;
+            if (warps < 1) warps = 1;
+        }
+        k_move<D, 32><<<dim3((unsigned)((units * warps + 7) / 8), 1, b.n), 256, 0, st>>>(b, (int)warps, 0);
         return cudaGetLastError();
     }
     // blocks of a list: as many as fill the GPU, a step's rows each at least
     int blocks = 1;
-    const int limit = in_place ? 8 : 64;
-    while (blocks < limit && (int64_t)units * b.n * blocks < 4 * num_sms && most > 256 * blocks) blocks *= 2;
-    if (!in_place || blocks == 1) {
-        k_move<D, 256><<<dim3(units * blocks, 1, b.n), 256, 0, st>>>(b, blocks, 0);
+    while (blocks < 8 && (int64_t)units * b.n * blocks < 4 * num_sms && most > 256 * blocks) blocks *= 2;
+    if (blocks == 1) {
+        k_move<D, 256><<<dim3(units, 1, b.n), 256, 0, st>>>(b, 1, 0);
         return cudaGetLastError();
     }
     cudaLaunchAttribute cluster;
@@ -357,9 +366,11 @@ cudaError_t launch(const MoveBatch& b, int64_t most, bool in_place, int num_sms,
 }
 
 template <int C>
-cudaError_t launch_rank_by(const RankBatch& b, cudaStream_t st) {
+cudaError_t launch_rank_by(const RankBatch& b, int64_t most, cudaStream_t st) {
     const cudaError_t e = cudaFuncSetAttribute(k_rank<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRankKeys * 4);
     if (e != cudaSuccess) return e;
+    const int64_t slice = (most + C - 1) / C + 4;
+    const uint32_t held = (uint32_t)(slice < kRankKeys ? slice : kRankKeys);
     cudaLaunchAttribute cluster;
     cluster.id = cudaLaunchAttributeClusterDimension;
     cluster.val.clusterDim.x = C;
@@ -367,11 +378,11 @@ cudaError_t launch_rank_by(const RankBatch& b, cudaStream_t st) {
     cudaLaunchConfig_t config = {};
     config.gridDim = dim3(b.n_layers * b.n_kv_heads * C, b.n);
     config.blockDim = dim3(kRankThreads);
-    config.dynamicSmemBytes = kRankKeys * 4;
+    config.dynamicSmemBytes = held * 4;
     config.stream = st;
     config.attrs = &cluster;
     config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, k_rank<C>, b);
+    return cudaLaunchKernelEx(&config, k_rank<C>, b, held);
 }
 
 }  // namespace
@@ -379,7 +390,12 @@ cudaError_t launch_rank_by(const RankBatch& b, cudaStream_t st) {
 cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms) {
     int64_t most = 0;
     for (int i = 0; i < b.n; ++i) most = b.s[i].T > most ? b.s[i].T : most;
-    return most <= 8192 ? launch_rank_by<1>(b, st) : launch_rank_by<kRankCluster>(b, st);
+    // blocks of a list: as many as hold it, and while the lists leave SMs idle
+    const int64_t lists = (int64_t)b.n * b.n_layers * b.n_kv_heads;
+    int c = 1;
+    while (c < kRankCluster && (most > (int64_t)c * kRankKeys || (2 * lists * c <= num_sms && most > 2048 * c))) c *= 2;
+    return c == 1 ? launch_rank_by<1>(b, most, st) : c == 2 ? launch_rank_by<2>(b, most, st)
+         : c == 4 ? launch_rank_by<4>(b, most, st) : launch_rank_by<8>(b, most, st);
 }
 
 cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int num_sms) {
@@ -389,14 +405,16 @@ cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int n
         most = b.s[i].count > most ? b.s[i].count : most;
         in_place |= b.s[i].in_place != 0;
     }
-    if (most == 0) return cudaSuccess;
+    bool left = false;
+    for (int i = 0; i < b.n; ++i) left |= b.s[i].left && !b.s[i].left_later;
+    if (most == 0 && !left) return cudaSuccess;
     return head_dim == 128 ? launch<128>(b, most, in_place, num_sms, st) : launch<64>(b, most, in_place, num_sms, st);
 }
 
 cudaError_t launch_left(const MoveBatch& b, cudaStream_t st) {
     static_assert(kMaxPackBatch == 32, "a warp");
     for (int i = 0; i < b.n; ++i)
-        if (b.s[i].left) {
+        if (b.s[i].left_later) {
             k_left<<<1, kMaxPackBatch, 0, st>>>(b);
             return cudaGetLastError();
         }

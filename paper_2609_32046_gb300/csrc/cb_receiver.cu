@@ -737,6 +737,7 @@ cb_status keep_impl(cb_ctx* ctx, int32_t n, const cb_packed* caches, const cb_ke
         m.left = e.length;
         m.drafted = e.drafted;
         m.n_kept = e.n_kept;
+        m.left_later = e.length && e.length == p.length;
         m.in_place = 1;
         if (e.count > 0) {
             if ((st = ptrs.check(e.idx, "kept.idx", i, 4)) || (e.weights && (st = ptrs.check(e.weights, "kept.weights", i, 4))))

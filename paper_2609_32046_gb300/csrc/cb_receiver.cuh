@@ -171,12 +171,13 @@ struct MoveSeq {
     int64_t w_layer, w_head, t_layer, t_head;
     const int32_t* idx;
     int64_t idx_list;         // entries of a (layer, head); 0: all have the same
-    int64_t count;            // entries at most; of a list of its own, those before the first -1
+    int64_t count;            // entries at most (of lists of their own -1 is none)
     const int32_t* n_kept;    // or null: entries that count
     int64_t T;                // rows of `from`
     const int32_t* length;    // or null
     int64_t drafted;          // base = rows - drafted; -1: 0
     int32_t* left;            // or null: receives base + entries (lists of their own: min(rows, count))
+    int32_t left_later;       // not before every group has read `length`
     int32_t in_place;
 };
 struct MoveBatch {
@@ -196,7 +197,7 @@ cudaError_t launch_attend(AttendTreeBatch& b, int head_dim, cudaStream_t st, int
 cudaError_t launch_weigh(WeighBatch& b, int head_dim, cudaStream_t st, int num_sms);
 cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms);
 cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int num_sms);
-cudaError_t launch_left(const MoveBatch& b, cudaStream_t st);     // writes MoveSeq::left, behind every launch_move of a call
+cudaError_t launch_left(const MoveBatch& b, cudaStream_t st);     // those that are left_later, behind every launch_move of a call
 // Query rows of partial results that launch_attend may use on num_sms SMs.
 int64_t attend_part_rows(int num_sms);
 constexpr int kFewBlocksPerSm = 4;   // blocks of k_attend_few an SM holds at most

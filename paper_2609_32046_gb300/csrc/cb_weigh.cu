@@ -175,6 +175,7 @@ cudaError_t launch_weigh(WeighBatch& b, int head_dim, cudaStream_t st, int num_s
     rows *= b.G;
     if (rows == 0) return cudaSuccess;
     b.sees_window = b.sees_window < kFarWindow ? b.sees_window : kFarWindow;
+    if (rows > 16) return launch_weigh_tc(b, head_dim, st, num_sms);
     const int64_t units = attend_pairs(b, kWeighRows);
     if (head_dim == 128)
         return rows <= 8 ? launch_few<128, 1, false>(b, units, num_sms, st)

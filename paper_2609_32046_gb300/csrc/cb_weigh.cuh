@@ -59,4 +59,6 @@ struct WeighRows {
     }
 };
 
+cudaError_t launch_weigh_tc(WeighBatch& b, int head_dim, cudaStream_t st, int num_sms);
+
 }  // namespace cbk
