@@ -280,8 +280,8 @@ cb_status cb_stage_times(cb_ctx *ctx, float *ms, int32_t *calls);
 
 /*
  * Bounded device waits (failure detection; the paper has no counterpart: this is a runtime
- * control).  Every mbarrier wait of the tcgen05 kernels (the score passes; cb_attend with more
- * than 16 query rows a KV head) gives up after limit_ns nanoseconds (default 1 s): the kernel then records which wait gave up, sets an abort flag
+ * control).  Every mbarrier wait of the tcgen05 kernels (the score passes; cb_attend, cb_attend_tree and
+ * cb_weigh with more than 16 query rows a KV head) gives up after limit_ns nanoseconds (default 1 s): the kernel then records which wait gave up, sets an abort flag
  * that every role of its CTA sees, waits (bounded) for its own copies and MMAs in flight,
  * frees its tensor memory and returns, so the context stays usable; the next cb_sync_status
  * reports CB_ETIMEOUT and that call's results are invalid.
@@ -293,6 +293,7 @@ cb_status cb_stage_times(cb_ctx *ctx, float *ms, int32_t *calls);
  *                     and hangs nothing.  The mma.sync passes have no waits and ignore it.
  *                     2: the same for the next cb_attend that runs the tcgen05 kernel (its block 0's
  *                     MMA issuer); calls on the kernel of few rows, which has no waits, leave it set
+ *                     3: the same for the next cb_weigh that runs its tcgen05 kernel
  * Errors: CB_EINVAL (NULL ctx, values out of range).  Host-only; affects later calls.
  */
 cb_status cb_set_wait_limit(cb_ctx *ctx, int64_t limit_ns, int32_t stall_next);

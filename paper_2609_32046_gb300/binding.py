@@ -992,12 +992,14 @@ class CacheBack:
     def _fits(self, p: PackedKV):
         _require(p._shape == self._shape, "the cache's layers, heads or head dimension are not the context's")
 
-    def set_wait_limit(self, limit_ns: int = 0, stall_next_score: bool = False, stall_next_attend: bool = False):
+    def set_wait_limit(self, limit_ns: int = 0, stall_next_score: bool = False, stall_next_attend: bool = False,
+                       stall_next_weigh: bool = False):
         """cb_set_wait_limit: limit of one bounded device wait (0: the 1 s default); with
-        stall_next_score (stall_next_attend) the next tcgen05 cb_score (cb_attend) makes one wait run out
-        (failure-detection test)."""
-        _require(not (stall_next_score and stall_next_attend), "one stall at a time")
-        self._check(self.lib.cb_set_wait_limit(self.h, int(limit_ns), 1 if stall_next_score else 2 if stall_next_attend else 0))
+        stall_next_score (stall_next_attend, stall_next_weigh) the next tcgen05 cb_score (cb_attend, cb_weigh) makes one
+        wait run out (failure-detection test)."""
+        stalls = (stall_next_score, stall_next_attend, stall_next_weigh)
+        _require(sum(map(bool, stalls)) <= 1, "one stall at a time")
+        self._check(self.lib.cb_set_wait_limit(self.h, int(limit_ns), sum(i + 1 for i, x in enumerate(stalls) if x)))
 
     def set_score_sms(self, n_sms: int = 0):
         """cb_set_score_sms: SMs the persistent score kernels occupy (0: all)."""

@@ -50,6 +50,7 @@ struct cb_ctx {
     int64_t wait_ns = cbk::kDefaultWaitNs;   // limit of one bounded device wait (tcgen05 passes)
     int32_t stall_next = 0;         // failure-detection test: stall the next cb_score once
     int32_t stall_attend = 0;       // the same for the next cb_attend on the tcgen05 kernel
+    int32_t stall_weigh = 0;        // and for the next cb_weigh on its
     int32_t score_sms = 0;          // SMs of the persistent score kernels (0: all)
     bool receiver = false;          // no scratch for cb_score and cb_select
     float* attend_part = nullptr;   // cb_attend: partial results (outputs; maxima and sums)

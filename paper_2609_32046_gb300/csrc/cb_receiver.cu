@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "cb_ctx.cuh"
+#include "cb_weigh.cuh"
 
 using namespace cbk;
 
@@ -527,8 +528,9 @@ cb_status weigh_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* cac
         b.scale_log2e = ctx->scale * 1.4426950408889634f;
         b.err = ctx->err;
         b.wait_ns = (uint64_t)ctx->wait_ns;
+        b.stall = ctx->stall_weigh;
         b.sees = causal;
-        b.sees_window = window;
+        b.sees_window = window < kNoWindow ? (int32_t)window : 0;
         b.decay = decay;
         for (int k = 0; k < b.n; ++k) {
             const int i = some[b0 + k];
@@ -549,6 +551,7 @@ cb_status weigh_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* cac
             if (trees) w.tree = TreeBits{trees[i].seen, trees[i].s_row};
         }
         const cudaError_t e = launch_weigh(b, d, strm, ctx->num_sms);
+        ctx->stall_weigh = b.stall;
         if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "weigh launch failed: %s", cudaGetErrorString(e));
     }
     return CB_OK;

@@ -142,8 +142,8 @@ struct WeighSeq {
 };
 struct WeighBatch : AttendBatch {
     int32_t sees;
+    int32_t sees_window;      // 0: none
     float decay;
-    int64_t sees_window;
     WeighSeq w[kMaxBatch];
 };
 

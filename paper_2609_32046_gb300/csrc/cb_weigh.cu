@@ -55,11 +55,10 @@ __device__ __forceinline__ bool look_over_keys(uint8_t* stage, uint32_t* err) {
 
 // A block takes its run of units (cb_attend.cuh); its four warps take 32 positions in turn, each with its own
 // copies.  S^T [16 positions][8 rows] = K Q^T (cb_few.cuh), the rows' weights are added up over a quad's lanes, and
-// every position's sum is written by one lane.  MANY: more than 8 NT rows, a tile of them after the other.
-template <int D, int NT, bool MANY>
+// every position's sum is written by one lane.
+template <int D, int NT>
 __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_constant__ WeighBatch b) {
     using S = Stage<D, 1>;
-    constexpr int ROWS = 8 * NT;
     __shared__ __align__(128) uint8_t smem[kWarps * kStages * S::kBytes];
     __shared__ int pre[kMaxBatch + 1];
     __shared__ Segment x;
@@ -87,19 +86,15 @@ __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_const
         }
         uint32_t q[NT][D / 32][4];
         float zs[NT][2], nl[NT][2];       // of columns 2 tig and 2 tig + 1: factor of the logits, -lse * log2(e)
-        auto load = [&](int row0) {
-            load_queries<D, NT>(b, b.s[x.seq], g, row0, x.rows, q, zs,
-                                [&](int row) { return isfinite(rows.lse(w, g, row)); });
+        load_queries<D, NT>(b, b.s[x.seq], g, 0, x.rows, q, zs, [&](int row) { return isfinite(rows.lse(w, g, row)); });
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = row0 + nt * 8 + 2 * tig + h;
-                    const float lse = row < x.rows ? rows.lse(w, g, row) : INFINITY;
-                    nl[nt][h] = isfinite(lse) ? lse * -1.4426950408889634f : -INFINITY;
-                }
-        };
-        if (!MANY) load(0);
+            for (int h = 0; h < 2; ++h) {
+                const int row = nt * 8 + 2 * tig + h;
+                const float lse = row < x.rows ? rows.lse(w, g, row) : INFINITY;
+                nl[nt][h] = isfinite(lse) ? lse * -1.4426950408889634f : -INFINITY;
+            }
         for (int turn = 0; t0 < x.len; t0 += kWarps * kStep) {
             uint8_t* st = stages + turn * S::kBytes;
             const int own = t0 + 8 * tig + place(gid);          // the position whose sum this lane writes
@@ -109,35 +104,31 @@ __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_const
             float s[4] = {};                                    // of positions t0 + 8 k + place(gid)
             if (!rows.blind(t0, kStep)) {
                 const bool near = look_over_keys<D>(st, b.err), edge = rows.edge(t0, kStep);
-#pragma unroll 1
-                for (int row0 = 0; row0 < (MANY ? x.rows : 1); row0 += ROWS) {
-                    if (MANY) load(row0);
-                    float z[2][NT][4];
-                    if (near) {
-                        score_keys<D, NT, true, 1>(st, 0, q, z[0]);
-                        score_keys<D, NT, true, 1>(st, 16, q, z[1]);
-                    } else {
-                        score_keys<D, NT, false, 1>(st, 0, q, z[0]);
-                        score_keys<D, NT, false, 1>(st, 16, q, z[1]);
-                    }
-                    if (edge) {
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t bits = rows.seen(w, (row0 + nt * 8 + 2 * tig + h) / b.G, t0);
-#pragma unroll
-                                for (int k = 0; k < 4; ++k)
-                                    if (!(bits >> (8 * k + place(gid)) & 1u)) z[k / 2][nt][2 * (k % 2) + h] = -INFINITY;
-                            }
-                    }
+                float z[2][NT][4];
+                if (near) {
+                    score_keys<D, NT, true, 1>(st, 0, q, z[0]);
+                    score_keys<D, NT, true, 1>(st, 16, q, z[1]);
+                } else {
+                    score_keys<D, NT, false, 1>(st, 0, q, z[0]);
+                    score_keys<D, NT, false, 1>(st, 16, q, z[1]);
+                }
+                if (edge) {
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            s[k] += ex2(fmaf(z[k / 2][nt][2 * (k % 2)], zs[nt][0], nl[nt][0])) +
-                                    ex2(fmaf(z[k / 2][nt][2 * (k % 2) + 1], zs[nt][1], nl[nt][1]));
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t bits = rows.seen(w, (nt * 8 + 2 * tig + h) / b.G, t0);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                if (!(bits >> (8 * k + place(gid)) & 1u)) z[k / 2][nt][2 * (k % 2) + h] = -INFINITY;
+                        }
                 }
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        s[k] += ex2(fmaf(z[k / 2][nt][2 * (k % 2)], zs[nt][0], nl[nt][0])) +
+                                ex2(fmaf(z[k / 2][nt][2 * (k % 2) + 1], zs[nt][1], nl[nt][1]));
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
@@ -159,11 +150,11 @@ __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_const
     }
 }
 
-template <int D, int NT, bool MANY>
+template <int D, int NT>
 cudaError_t launch_few(const WeighBatch& b, int64_t units, int num_sms, cudaStream_t st) {
     const int64_t most = num_sms * 4 / b.n_kv_heads, all = units / b.n_kv_heads;
     const int64_t runs = all < most ? all : most;
-    k_weigh_few<D, NT, MANY><<<(int)(runs > 1 ? runs : 1) * b.n_kv_heads, kWarps * 32, 0, st>>>(b);
+    k_weigh_few<D, NT><<<(int)(runs > 1 ? runs : 1) * b.n_kv_heads, kWarps * 32, 0, st>>>(b);
     return cudaGetLastError();
 }
 
@@ -174,14 +165,11 @@ cudaError_t launch_weigh(WeighBatch& b, int head_dim, cudaStream_t st, int num_s
     for (int i = 0; i < b.n; ++i) rows = b.span[i].m > rows ? b.span[i].m : rows;
     rows *= b.G;
     if (rows == 0) return cudaSuccess;
-    b.sees_window = b.sees_window < kFarWindow ? b.sees_window : kFarWindow;
     if (rows > 16) return launch_weigh_tc(b, head_dim, st, num_sms);
     const int64_t units = attend_pairs(b, kWeighRows);
     if (head_dim == 128)
-        return rows <= 8 ? launch_few<128, 1, false>(b, units, num_sms, st)
-                         : rows <= 16 ? launch_few<128, 2, false>(b, units, num_sms, st) : launch_few<128, 2, true>(b, units, num_sms, st);
-    return rows <= 8 ? launch_few<64, 1, false>(b, units, num_sms, st)
-                     : rows <= 16 ? launch_few<64, 2, false>(b, units, num_sms, st) : launch_few<64, 2, true>(b, units, num_sms, st);
+        return rows <= 8 ? launch_few<128, 1>(b, units, num_sms, st) : launch_few<128, 2>(b, units, num_sms, st);
+    return rows <= 8 ? launch_few<64, 1>(b, units, num_sms, st) : launch_few<64, 2>(b, units, num_sms, st);
 }
 
 }  // namespace cbk

@@ -241,6 +241,49 @@ def test_repeated_and_concurrent_runs_are_alike(m):
             assert torch.equal(a[:, :p.T], b[:, :p.T])
 
 
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 4, 1), (64, 4, 1), (64, 2, 2)])
+@pytest.mark.parametrize("m,T", [(64, 700), (65, 2000), (128, 3333), (129, 129), (500, 1500), (1024, 1024), (1024, 3000)])
+@pytest.mark.parametrize("see", [dict(), dict(window=40), dict(window=700), dict(causal=False)])
+def test_many_query_rows(d, Hq, Hkv, m, T, see):
+    """Rows that stay in shared memory while positions pass, and rows that pass; tiles that no token sees."""
+    c = Weighed(d, Hq, Hkv, [m, 20, m], [T, 5000, T // 2 + m], seed=m, page=16, see=see)
+    c.weigh(decay=0.5)
+    c.check(decay=0.5)
+
+
+@pytest.mark.parametrize("m", [150, 600, 1024])
+def test_many_drafts(m):
+    bits = [bits_of("tree", m, 0), None, bits_of("any", m, 2)]
+    c = Weighed(128, 4, 1, [m] * 3, [m, 900 + m, 2000], see=dict(trees=[None if x is None else cb.pack_words(x).cuda() for x in bits]))
+    c.weigh()
+    c.check(bits)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_segments_than_blocks(d):
+    """Runs of a few tiles that end inside items, many items a block, rows that pass and rows that stay in one call."""
+    n = 40
+    c = Weighed(d, 16, 8, [9 + 53 * (i % 6) for i in range(n)], [300 + 97 * i for i in range(n)], page=32)
+    c.weigh()
+    c.check()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("m", [30, 300])
+def test_a_wait_that_gives_up(d, m):
+    """A bounded wait runs out on a barrier that nothing arrives on: an error status, and the context goes on."""
+    c = Weighed(d, 8, 2, [m, m], [1500, 700 + m])
+    c.rx.set_wait_limit(20_000_000, stall_next_weigh=True)           # 20 ms
+    c.weigh()
+    with pytest.raises(cb.CBError) as e:
+        c.rx.sync_status()
+    assert e.value.status == cb.CB_ETIMEOUT
+    for w, b in zip(c.weights, c.before):
+        w.copy_(b)
+    c.weigh()
+    c.check()
+
+
 def test_weights_of_a_softmax_sum_to_one():
     c = Weighed(128, 32, 8, [70], [3000])
     w = torch.zeros(8, 3000, device="cuda")
