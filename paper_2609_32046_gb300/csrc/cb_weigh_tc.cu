@@ -37,10 +37,23 @@ template <int D> constexpr int kStages = D == 128 ? 2 : 4;    // tiles of query 
 constexpr int kLse = 16;
 static_assert(kLse >= 4 + kBuffers + 2, "");
 
+// Positions that pass are in two of the tiles' places by turns; the other two hold their packed rows on their way, each of
+// the warps that unpack its own share.
+template <int D>
+struct Share {
+    static constexpr int kRows = kTile / kLoadWarps, kBytes = kRows * (D / 2 + D / 16);
+    static constexpr int kAhead = 6;
+    static_assert(kAhead * kBytes * kLoadWarps <= 2 * kTile * D * 2 && kBytes % 16 == 0, "");
+    // Byte of piece p (16 bytes) of a row's codes: what eight lanes read at once (one quarter of eight rows) is in banks of its own.
+    static __device__ __forceinline__ uint32_t at(int row, int p) {
+        return row * (D / 2) + ((p ^ (D == 128 ? (row >> 1) & 3 : (row >> 2) & 1)) << 4);
+    }
+};
+
 struct Ctl {
     uint64_t k_full[kTiles], k_empty[kTiles], q_full[4], q_empty[4];
     uint64_t d_full[kBuffers], d_empty[kBuffers], sum_full[kTiles], sum_empty[kTiles];
-    uint64_t seg_full[2], seg_empty[2];
+    uint64_t seg_full[2], seg_empty[2], shares;
     uint64_t done, stall;
     uint64_t wait_ns;
     uint32_t tmem;
@@ -69,13 +82,27 @@ struct View {
           resident(p.q1 - p.q0 <= stages) {}
     __device__ __forceinline__ int first_token(int q) const { return (q * kTile) >> log2g; }
     __device__ __forceinline__ int last_token(int q) const { return (min(rows, (q + 1) * kTile) - 1) >> log2g; }
-    // Some token of first .. last sees one of the n positions from t0 on.
-    __device__ __forceinline__ bool see(int first, int last, int t0, int n) const {
-        return w.tree || !w.causal || (t0 <= w.at + last && !(w.window && t0 + n - 1 <= w.at + first - w.window));
+    // Tiles of positions [first, last) that some token of a .. b sees a position of; those before `low` and from `high` on
+    // not every one of them sees whole.
+    struct Span {
+        int first, last, low, high;
+    };
+    __device__ __forceinline__ Span span(int a, int b) const {
+        if (w.tree) return Span{0, tiles, 0, max(w.at, 0) / kTile};
+        if (!w.causal) return Span{0, tiles, 0, tiles};
+        // (position t is seen by the tokens from t - at on and before t - at + window)
+        Span s{0, min(tiles, max(0, w.at + b + kTile) / kTile), 0, max(0, w.at + a + 1) / kTile};
+        if (w.window) {
+            s.first = max(0, w.at + a - w.window + 1) / kTile;
+            s.low = max(0, w.at + b - w.window + kTile) / kTile;
+        }
+        return s;
     }
-    // Tile q of rows and tile k of positions have something to add; tile k has with some tile of rows.
-    __device__ __forceinline__ bool met(int q, int k) const { return see(first_token(q), last_token(q), k * kTile, kTile); }
-    __device__ __forceinline__ bool used(int k) const { return q0 < q1 && see(first_token(q0), last_token(q1 - 1), k * kTile, kTile); }
+    __device__ __forceinline__ Span span_of(int q) const { return span(first_token(q), last_token(q)); }
+    // Those that some tile of rows has something to add to.
+    __device__ __forceinline__ Span used() const {
+        return q0 < q1 ? span(first_token(q0), last_token(q1 - 1)) : Span{0, 0, 0, 0};
+    }
 };
 
 // Copies 16 bytes into shared memory, or zeros.
@@ -123,6 +150,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
             mbar_init(&ctl->seg_full[i], 1);
             mbar_init(&ctl->seg_empty[i], kReaders);
         }
+        mbar_init(&ctl->shares, kLoadWarps);
         mbar_init(&ctl->done, 1);
         mbar_init(&ctl->stall, 1);
         ctl->wait_ns = b.wait_ns;
@@ -155,17 +183,17 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
         const int group = warp >> 2, mine = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + 32 * group;      // (lane 32 (warp % 4) << 16)
         const uint64_t cc = pack2(b.scale_log2e, b.scale_log2e);
+        float* sums = s_sum + group * kTile + mine;
         uint32_t item = 0, n_q = 0, n_tile = 0;
         bool ok = true;
         while (ok && begin()) {
             const Part& part = parts[nth & 1];
             const View v(b, part, kStages<D>);
-            const TreeBits tree = b.w[part.x.seq].tree;
             // bit e: query row row0 + e sees the thread's position of tile k
-            auto sees = [&](int q, int k, int row0) {
+            auto sees = [&](int row0, int k) {
                 const int t = k * kTile + mine;
                 if (v.w.tree) {
-                    if ((k + 1) * kTile <= v.w.at) return 0xFFFFFFFFu;
+                    const TreeBits tree = b.w[part.x.seq].tree;
                     uint32_t bits = 0, rows = 0;
 #pragma unroll 1
                     for (int e = 0; e < 32; ++e) {
@@ -176,56 +204,50 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                     }
                     return bits;
                 }
-                const bool edge = v.w.causal && ((k + 1) * kTile - 1 > v.w.at + v.first_token(q) ||
-                                                 (v.w.window && k * kTile <= v.w.at + v.last_token(q) - v.w.window));
-                if (!edge) return 0xFFFFFFFFu;
                 // tokens from t - at on, and before t - at + window
                 const int64_t lo = ((int64_t)(t - v.w.at) << v.log2g) - row0;
                 const int64_t hi = v.w.window ? lo + ((int64_t)v.w.window << v.log2g) : 32;
                 const int c0 = (int)max((int64_t)0, min(lo, (int64_t)32)), c1 = (int)max((int64_t)0, min(hi, (int64_t)32));
                 return c0 >= c1 ? 0u : (0xFFFFFFFFu << c0) & (0xFFFFFFFFu >> (32 - c1));
             };
-            // the sum of the thread's columns of one product
-            auto gather = [&](int q, int k) {
+            // the sum of the thread's columns of one product; some: its group has any
+            auto gather = [&](int row0, int k, bool some, bool edge, const float* lse) {
                 const uint32_t d = item % kBuffers, phase = item / kBuffers & 1;
                 ++item;
                 if (!(ok = wait_warp(&ctl->d_full[d], phase, ctl, b.err, 10))) return 0.f;
-                const int row0 = q * kTile + 32 * group;
-                float sum = 0.f;
-                if (row0 < v.rows) {
-                    const uint32_t bits = sees(q, k, row0);
-                    tc_fence_after();
-                    float z[32];
-                    tmem_ld32(from + d * 128, z);
-                    tmem_wait_ld(z);
-                    tc_fence_before();
-                    __syncwarp();
+                if (!some) {
                     if (lane == 0) mbar_arrive(&ctl->d_empty[d]);
-                    if (bits != 0xFFFFFFFFu) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!(bits >> e & 1u)) z[e] = -INFINITY;
-                    }
-                    const float* lse = s_lse + (n_q + q - v.q0) % kLse * kTile + 32 * group;
-                    uint64_t l0 = 0, l1 = 0;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 nl = *reinterpret_cast<const float4*>(lse + e);
-                        float y0, y1, y2, y3;
-                        unpack2(ffma2(pack2(z[e], z[e + 1]), cc, pack2(nl.x, nl.y)), y0, y1);
-                        unpack2(ffma2(pack2(z[e + 2], z[e + 3]), cc, pack2(nl.z, nl.w)), y2, y3);
-                        l0 = fadd2(l0, pack2(ex2(y0), ex2(y1)));
-                        l1 = fadd2(l1, pack2(ex2(y2), ex2(y3)));
-                    }
-                    float a0, a1;
-                    unpack2(fadd2(l0, l1), a0, a1);
-                    sum = a0 + a1;
-                } else {
-                    if (lane == 0) mbar_arrive(&ctl->d_empty[d]);
+                    return 0.f;
                 }
-                return sum;
+                tc_fence_after();
+                float z[32];
+                tmem_ld32(from + d * 128, z);
+                uint32_t bits = 0xFFFFFFFFu;
+                if (edge) bits = sees(row0, k);
+                tmem_wait_ld(z);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->d_empty[d]);
+                if (edge) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (!(bits >> e & 1u)) z[e] = -INFINITY;
+                }
+                uint64_t l0 = 0, l1 = 0;
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 nl = *reinterpret_cast<const float4*>(lse + e);
+                    float y0, y1, y2, y3;
+                    unpack2(ffma2(pack2(z[e], z[e + 1]), cc, pack2(nl.x, nl.y)), y0, y1);
+                    unpack2(ffma2(pack2(z[e + 2], z[e + 3]), cc, pack2(nl.z, nl.w)), y2, y3);
+                    l0 = fadd2(l0, pack2(ex2(y0), ex2(y1)));
+                    l1 = fadd2(l1, pack2(ex2(y2), ex2(y3)));
+                }
+                float a0, a1;
+                unpack2(fadd2(l0, l1), a0, a1);
+                return a0 + a1;
             };
-            auto place = [&](int k) { return s_sum + ((n_tile + k) % kTiles * kGroups + group) * kTile + mine; };
+            auto place = [&](int k) { return sums + (n_tile + k) % kTiles * kGroups * kTile; };
             // a tile's place in shared memory, which the writer has left
             auto open = [&](int k) {
                 const uint32_t n = n_tile + k;
@@ -236,19 +258,27 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl->sum_full[(n_tile + k) % kTiles]);
             };
+            auto lse_at = [&](int q) { return s_lse + (n_q + q - v.q0) % kLse * kTile + 32 * group; };
             if (v.resident) {
                 for (int k = 0; k < v.tiles && open(k); ++k) {
                     float sum = 0.f;
-                    for (int q = v.q0; q < v.q1 && ok; ++q)
-                        if (v.met(q, k)) sum += gather(q, k);
+                    for (int q = v.q0; q < v.q1 && ok; ++q) {
+                        const View::Span s = v.span_of(q);
+                        const int row0 = q * kTile + 32 * group;
+                        if (k >= s.first && k < s.last) sum += gather(row0, k, row0 < v.rows, k < s.low || k >= s.high, lse_at(q));
+                    }
                     *place(k) = sum;
                     close(k);
                 }
             } else {
                 for (int k = 0; k < v.tiles && open(k); ++k) *place(k) = 0.f;
-                for (int q = v.q0; q < v.q1 && ok; ++q)
-                    for (int k = 0; k < v.tiles && ok; ++k)
-                        if (v.met(q, k)) *place(k) += gather(q, k);
+                for (int q = v.q0; q < v.q1 && ok; ++q) {
+                    const View::Span s = v.span_of(q);
+                    const int row0 = q * kTile + 32 * group;
+                    const float* lse = lse_at(q);
+#pragma unroll 1
+                    for (int k = s.first; k < s.last && ok; ++k) *place(k) += gather(row0, k, row0 < v.rows, k < s.low || k >= s.high, lse);
+                }
                 for (int k = 0; k < v.tiles; ++k) close(k);
             }
             n_tile += v.tiles;
@@ -261,47 +291,42 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
         // rows 16 lw + 8 y + lane % 8 of a tile (whose last three bits the swizzle takes), pieces quarter (D / 32) + e
         const uint32_t at = piece(quarter * (D / 32) / 8, kTile, 16 * lw, 0) + (lane % 8) * 128;
         const uint32_t col = ((quarter * (D / 32) % 8) ^ (lane % 8)) << 4;
-        // query rows: thread u has piece u % P of rows u / P, u / P + N ...
+        // query rows: thread u has piece u % P of rows u / P, u / P + N ..., which all are of one head
         constexpr int P = D / 8, N = kLoadThreads / P, R = kTile / N;
+        static_assert(N % 8 == 0, "");
         const int u = threadIdx.x - kSumWarps * 32;
-        uint32_t n_q = 0, n_k = 0, bad = 0;
+        const uint32_t q_at = smem_u32(sq) + piece(u % P / 8, kTile, u / P, u % P % 8);
+        uint8_t* share = sk + 2 * kOp + lw * (Share<D>::kAhead * Share<D>::kBytes);
+        const uint32_t share32 = smem_u32(share);
+        uint32_t n_q = 0, k_parity = 0, k_used = 0, bad = 0;      // bits: uses of a tile's place, any use
         bool ok = true;
         while (ok && begin()) {
             const Part& part = parts[nth & 1];
             const Segment& x = part.x;
             const View v(b, part, kStages<D>);
             const AttendSeq& s = b.s[x.seq];
-            const float* lses = b.w[x.seq].lse;
-            auto page_of = [&](int k, uint32_t (&page)[2]) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y) page[y] = segment_page(x, k * kTile + 16 * lw + 8 * y + lane % 8);
+            const int head = (x.g << v.log2g) + ((u / P) & (b.G - 1));
+            const float* lses = b.w[x.seq].lse + head;
+            const uint16_t* q_from = s.q + (int64_t)head * s.s_head + u % P * 8;
+            const int64_t tok_bytes = s.s_tok;
+            // (tiles that stay take the place of the shares: every warp has read what its last segment left there)
+            if (nth && !(ok = wait_warp(&ctl->shares, (nth - 1) & 1, ctl, b.err, 13))) break;
+            auto vacant = [&](int slot) {
+                return !(k_used >> slot & 1) || wait_warp(&ctl->k_empty[slot], (k_parity >> slot & 1) ^ 1, ctl, b.err, 13);
             };
-            auto read_keys = [&](int k, const uint32_t (&page)[2], Codes<D>& c) {
-#pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    c.x[y] = make_uint4(0, 0, 0, 0);
-                    c.scale[y] = 0;
-                    const int r = segment_row(x, k * kTile + 16 * lw + 8 * y + lane % 8, page[y], b.err);
-                    if (r < 0) continue;
-                    const uint8_t* from = x.code[0] + (uint64_t)r * (D / 2) + quarter * (D / 8);
-                    if (D == 128) {
-                        c.x[y] = __ldg(reinterpret_cast<const uint4*>(from));
-                    } else {
-                        const uint2 w = __ldg(reinterpret_cast<const uint2*>(from));
-                        c.x[y].x = w.x;
-                        c.x[y].y = w.y;
-                    }
-                    c.scale[y] = __ldg(x.scale[0] + (uint64_t)r * (D / 32) + quarter * (D / 32) / 4);
-                }
+            auto filled = [&](int slot) {
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ctl->k_full[slot]);
+                k_parity ^= 1u << slot;
+                k_used |= 1u << slot;
             };
             auto lse_of = [&](int q, float (&lse)[R]) {
+                const int row0 = q * kTile + u / P;
+                const float* from = lses + (int64_t)(row0 >> v.log2g) * b.n_q_heads;
+                const int step = (N >> v.log2g) * b.n_q_heads;
 #pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    const int row = q * kTile + u / P + i * N;
-                    lse[i] = INFINITY;
-                    if (row < v.rows)
-                        lse[i] = __ldg(lses + (int64_t)(row >> v.log2g) * b.n_q_heads + (x.g << v.log2g) + (row & (b.G - 1)));
-                }
+                for (int i = 0; i < R; ++i) lse[i] = row0 + i * N < v.rows ? __ldg(from + i * step) : INFINITY;
             };
             auto copy_rows = [&](int q, const float (&lse)[R]) {       // into a stage that the products have left
                 const uint32_t n = n_q + q - v.q0;
@@ -309,17 +334,15 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                     ok = false;
                     return;
                 }
-                const uint32_t to = smem_u32(sq) + n % kStages<D> * kOp;
+                const uint32_t to = q_at + n % kStages<D> * kOp;
+                const uint16_t* from = q_from + (int64_t)((q * kTile + u / P) >> v.log2g) * tok_bytes;
+                const int64_t step = (N >> v.log2g) * tok_bytes;
+                float* l = s_lse + n % kLse * kTile + u / P;
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
-                    const int r = u / P + i * N, row = q * kTile + r;
                     const bool there = isfinite(lse[i]);
-                    copy16_or_0(to + piece(u % P / 8, kTile, r, u % P % 8),
-                                there ? s.q + (int64_t)(row >> v.log2g) * s.s_tok +
-                                            (int64_t)((x.g << v.log2g) + (row & (b.G - 1))) * s.s_head + u % P * 8
-                                      : s.q,
-                                there);
-                    if (u % P == 0) s_lse[n % kLse * kTile + r] = there ? lse[i] * -1.4426950408889634f : -INFINITY;
+                    copy16_or_0(to + i * N * 128, there ? from + i * step : s.q, there);
+                    if (u % P == 0) l[i * N] = there ? lse[i] * -1.4426950408889634f : -INFINITY;
                 }
             };
             auto landed = [&](int q) {
@@ -329,60 +352,128 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl->q_full[(n_q + q - v.q0) % kStages<D>]);
             };
-            // tiles of positions that are used: k, and the next one on its way
-            auto next = [&](int k) {
-                do ++k;
-                while (k < v.tiles && !v.used(k));
-                return k;
-            };
-            Codes<D> c0, c1;
-            uint32_t page[2];
-            int k0 = next(-1), k1 = next(k0), k2 = next(k1);
-            page_of(k0, page);
-            read_keys(k0, page, c0);
-            page_of(k1, page);
-            read_keys(k1, page, c1);
-            page_of(k2, page);
-            float lse[R];
-            const int q_first = min(v.q1, v.q0 + kStages<D>);           // the rows that stay, or the first that pass
-            for (int q = v.q0; q < q_first && ok; ++q) {
-                lse_of(q, lse);
-                copy_rows(q, lse);
-                if (ok) landed(q);
-            }
-            while (k0 < v.tiles && ok) {
-                const uint32_t slot = n_k % kTiles;
-                if (n_k >= kTiles && !(ok = wait_warp(&ctl->k_empty[slot], (n_k / kTiles - 1) & 1, ctl, b.err, 13))) break;
-                ++n_k;
-                uint8_t* to = sk + slot * kOp + at;
+            // a quarter of a row: codes as numbers
+            auto unpack = [&](uint8_t* to, const uint32_t (&word)[4], uint32_t scale) {
+                const uint32_t s2 = checked_scale(scale, bad) * 0x10001u;
 #pragma unroll
-                for (int y = 0; y < 2; ++y, to += 8 * 128) {
-                    const uint32_t s2 = checked_scale(c0.scale[y], bad) * 0x10001u;
-                    const uint32_t word[4] = {c0.x[y].x, c0.x[y].y, c0.x[y].z, c0.x[y].w};
-#pragma unroll
-                    for (int e = 0; e < D / 32; ++e) {
-                        uint32_t w[4];
-                        values_bf16(word[e], s2, w);
-                        st_piece(to, col ^ (e << 4), w);
-                    }
+                for (int e = 0; e < D / 32; ++e) {
+                    uint32_t w[4];
+                    values_bf16(word[e], s2, w);
+                    st_piece(to, col ^ (e << 4), w);
                 }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl->k_full[slot]);
-                c0 = c1;
-                k0 = k1;
-                k1 = k2;
-                read_keys(k1, page, c1);
-                k2 = next(k2);
-                page_of(k2, page);
-            }
-            lse_of(min(q_first, max(v.q1 - 1, 0)), lse);
-            for (int q = q_first; q < v.q1 && ok; ++q) {
-                copy_rows(q, lse);
-                lse_of(min(q + 1, v.q1 - 1), lse);
-                if (ok) landed(q);
+            };
+            float lse[R];
+            const View::Span used = v.used();
+            const int q_first = min(v.q1, v.q0 + kStages<D>);           // the rows that stay, or the first that pass
+            if (v.resident) {
+                // tiles of positions pass: their packed rows kAhead tiles ahead, the block-table entries one more
+                ok = vacant(2) && vacant(3);
+                const int mine = 16 * lw + lane % 16;                   // (lanes 16 on look the same rows up)
+                int ahead = used.first;
+                uint32_t page = segment_page(x, ahead * kTile + mine);
+                auto copy_keys = [&]() {
+                    if (ahead < used.last) {
+                        constexpr int C = D / 32;                       // pieces of a row's codes
+                        const uint32_t to = share32 + ahead % Share<D>::kAhead * Share<D>::kBytes;
+                        const int row = segment_row(x, ahead * kTile + mine, page, b.err);
+#pragma unroll
+                        for (int i = 0; i < C / 2; ++i) {
+                            const int r = lane / C + i * (32 / C);
+                            const int from = max(0, __shfl_sync(0xFFFFFFFFu, row, r));
+                            copy16(to + Share<D>::at(r, lane % C), x.code[0] + (uint64_t)from * (D / 2) + lane % C * 16);
+                        }
+                        if (lane < 16)
+                            copy_small<D / 16>(to + Share<D>::kRows * (D / 2) + lane * (D / 16),
+                                               reinterpret_cast<const uint8_t*>(x.scale[0]) + (uint64_t)max(0, row) * (D / 16), row >= 0);
+                    }
+                    copy_commit();
+                    ++ahead;
+                    page = segment_page(x, ahead * kTile + mine);
+                };
+                // the rows' log-sum-exps, and the first packed rows, while they are on their way
+                if (v.q0 < v.q1) lse_of(v.q0, lse);
+                if (ok)
+                    for (int i = 0; i < Share<D>::kAhead - 1; ++i) copy_keys();
+                for (int q = v.q0; q < q_first && ok; ++q) {
+                    if (q > v.q0) lse_of(q, lse);
+                    copy_rows(q, lse);
+                    if (ok) landed(q);
+                }
+                for (int k = used.first; k < used.last && ok; ++k) {
+                    const int slot = (k - used.first) & 1;
+                    copy_keys();
+                    copy_wait<Share<D>::kAhead - 1>();
+                    __syncwarp();
+                    if (!(ok = vacant(slot))) break;
+                    const uint8_t* rows = share + k % Share<D>::kAhead * Share<D>::kBytes;
+                    uint8_t* to = sk + slot * kOp + at;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y, to += 8 * 128) {
+                        const int row = 8 * y + lane % 8;
+                        const uint8_t* c = rows + Share<D>::at(row, D == 128 ? quarter : quarter / 2) + (D == 128 ? 0 : quarter % 2 * 8);
+                        uint32_t word[4] = {};
+                        if (D == 128) {
+                            const uint4 w = *reinterpret_cast<const uint4*>(c);
+                            word[0] = w.x; word[1] = w.y; word[2] = w.z; word[3] = w.w;
+                        } else {
+                            const uint2 w = *reinterpret_cast<const uint2*>(c);
+                            word[0] = w.x; word[1] = w.y;
+                        }
+                        unpack(to, word, reinterpret_cast<const uint16_t*>(rows + Share<D>::kRows * (D / 2))[row * (D / 32) + quarter * (D / 32) / 4]);
+                    }
+                    filled(slot);
+                }
+                copy_wait<0>();
+            } else {
+                // at most kTiles tiles stay: read ahead into registers
+                auto read_keys = [&](int k, Codes<D>& c) {
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const int t = k * kTile + 16 * lw + 8 * y + lane % 8;
+                        c.x[y] = make_uint4(0, 0, 0, 0);
+                        c.scale[y] = 0;
+                        const int r = k < used.last ? segment_row(x, t, segment_page(x, t), b.err) : -1;
+                        if (r < 0) continue;
+                        const uint8_t* from = x.code[0] + (uint64_t)r * (D / 2) + quarter * (D / 8);
+                        if (D == 128) {
+                            c.x[y] = __ldg(reinterpret_cast<const uint4*>(from));
+                        } else {
+                            const uint2 w = __ldg(reinterpret_cast<const uint2*>(from));
+                            c.x[y].x = w.x;
+                            c.x[y].y = w.y;
+                        }
+                        c.scale[y] = __ldg(x.scale[0] + (uint64_t)r * (D / 32) + quarter * (D / 32) / 4);
+                    }
+                };
+                Codes<D> c0, c1;
+                lse_of(v.q0, lse);
+                read_keys(used.first, c0);
+                read_keys(used.first + 1, c1);
+                copy_rows(v.q0, lse);
+                if (ok) landed(v.q0);
+                for (int k = used.first; k < used.last && ok; ++k) {
+                    const int slot = k - used.first;
+                    if (!(ok = vacant(slot))) break;
+                    uint8_t* to = sk + slot * kOp + at;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y, to += 8 * 128) {
+                        const uint32_t word[4] = {c0.x[y].x, c0.x[y].y, c0.x[y].z, c0.x[y].w};
+                        unpack(to, word, c0.scale[y]);
+                    }
+                    filled(slot);
+                    c0 = c1;
+                    read_keys(k + 2, c1);
+                }
+                lse_of(v.q0 + 1, lse);
+                for (int q = v.q0 + 1; q < v.q1 && ok; ++q) {
+                    copy_rows(q, lse);
+                    lse_of(min(q + 1, v.q1 - 1), lse);
+                    if (ok) landed(q);
+                }
             }
             n_q += v.q1 - v.q0;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ctl->shares);
             finish();
         }
         copy_wait<0>();
@@ -391,23 +482,26 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
         // ---------------- products ----------------
         const uint32_t hi = (uint32_t)(smem_desc_sw128(0) >> 32), lo = (uint32_t)smem_desc_sw128(0);
         const uint32_t kd = (smem_u32(sk) >> 4) + lo, qd = (smem_u32(sq) >> 4) + lo;
-        uint32_t item = 0, n_q = 0, n_k = 0;
+        uint32_t item = 0, n_q = 0, k_parity = 0;
         bool ok = !b.stall || blockIdx.x || wait_warp(&ctl->stall, 0, ctl, b.err, 14);
         while (ok && begin()) {
             const View v(b, parts[nth & 1], kStages<D>);
-            uint32_t n_used = 0;
             if (lane == 0) {
+                const View::Span used = v.used();
                 auto q_there = [&](int q) {
                     const uint32_t n = n_q + q - v.q0;
                     return wait(&ctl->q_full[n % kStages<D>], n / kStages<D> & 1, ctl, b.err, 14);
                 };
-                auto k_there = [&](uint32_t n) { return wait(&ctl->k_full[n % kTiles], n / kTiles & 1, ctl, b.err, 15); };
-                auto product = [&](int q, uint32_t nk) {
+                auto k_there = [&](int slot) { return wait(&ctl->k_full[slot], k_parity >> slot & 1, ctl, b.err, 15); };
+                auto k_done = [&](int slot) {
+                    umma_commit(&ctl->k_empty[slot]);
+                    k_parity ^= 1u << slot;
+                };
+                auto product = [&](uint32_t qa, uint32_t idesc, int slot) {
                     const uint32_t d = item % kBuffers;
                     if (item >= kBuffers && !wait(&ctl->d_empty[d], (item / kBuffers - 1) & 1, ctl, b.err, 16)) return false;
                     tc_fence_after();
-                    const uint32_t idesc = idesc_bf16_f32(kTile, (min(kTile, v.rows - q * kTile) + 31) & ~31);   // (what the sums read)
-                    const uint32_t ka = kd + nk % kTiles * (kOp >> 4), qa = qd + (n_q + q - v.q0) % kStages<D> * (kOp >> 4);
+                    const uint32_t ka = kd + slot * (kOp >> 4);
 #pragma unroll
                     for (int y = 0; y < D / 16; ++y) {
                         const uint32_t off = (y / 4) * (kTile * 128 >> 4) + (y % 4) * 2;
@@ -417,43 +511,37 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                     ++item;
                     return true;
                 };
+                auto rows_at = [&](int q) { return qd + (n_q + q - v.q0) % kStages<D> * (kOp >> 4); };
+                auto idesc_of = [&](int q) { return idesc_bf16_f32(kTile, (min(kTile, v.rows - q * kTile) + 31) & ~31); };   // (what the sums read)
                 if (v.resident) {
-                    bool first = true;
-                    for (int k = 0; k < v.tiles && ok; ++k) {
-                        if (!v.used(k)) continue;
-                        if (first)
-                            for (int q = v.q0; q < v.q1 && ok; ++q) ok = q_there(q);
-                        first = false;
-                        const uint32_t n = n_k + n_used;
-                        if (!ok || !(ok = k_there(n))) break;
-                        for (int q = v.q0; q < v.q1 && ok; ++q)
-                            if (v.met(q, k)) ok = product(q, n);
-                        umma_commit(&ctl->k_empty[n % kTiles]);
-                        ++n_used;
+                    for (int q = v.q0; q < v.q1 && ok; ++q) ok = q_there(q);
+                    for (int k = used.first; k < used.last && ok; ++k) {
+                        const int slot = (k - used.first) & 1;
+                        if (!(ok = k_there(slot))) break;
+                        for (int q = v.q0; q < v.q1 && ok; ++q) {
+                            const View::Span s = v.span_of(q);
+                            if (k >= s.first && k < s.last) ok = product(rows_at(q), idesc_of(q), slot);
+                        }
+                        k_done(slot);
                     }
                     for (int q = v.q0; q < v.q1; ++q) umma_commit(&ctl->q_empty[(n_q + q - v.q0) % kStages<D>]);
                 } else {
                     uint32_t there = 0;
-                    for (int k = 0; k < v.tiles; ++k) n_used += v.used(k);
                     for (int q = v.q0; q < v.q1 && ok; ++q) {
                         if (!(ok = q_there(q))) break;
-                        uint32_t n = n_k;
-                        for (int k = 0; k < v.tiles && ok; ++k) {
-                            if (!v.used(k)) continue;
-                            if (v.met(q, k)) {
-                                if (!(there >> k & 1)) ok = k_there(n);
-                                there |= 1u << k;
-                                if (ok) ok = product(q, n);
-                            }
-                            ++n;
+                        const View::Span s = v.span_of(q);
+                        for (int k = s.first; k < s.last && ok; ++k) {
+                            const int slot = k - used.first;
+                            if (!(there >> slot & 1)) ok = k_there(slot);
+                            there |= 1u << slot;
+                            if (ok) ok = product(rows_at(q), idesc_of(q), slot);
                         }
                         umma_commit(&ctl->q_empty[(n_q + q - v.q0) % kStages<D>]);
                     }
-                    for (uint32_t n = 0; n < n_used; ++n) umma_commit(&ctl->k_empty[(n_k + n) % kTiles]);
+                    for (int k = used.first; k < used.last; ++k) k_done(k - used.first);
                 }
             }
             ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0);
-            n_k += n_used;                          // (lane 0's; it alone uses them)
             n_q += v.q1 - v.q0;
             finish();
         }
@@ -515,8 +603,12 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                         part.x.len = min(part.x.len, kTiles * kTile);
                     }
                     const View v(b, part, kStages<D>);
-                    while (part.q0 < part.q1 && !v.see(v.first_token(part.q0), v.last_token(part.q0), 0, part.x.len)) ++part.q0;
-                    while (part.q1 > part.q0 && !v.see(v.first_token(part.q1 - 1), v.last_token(part.q1 - 1), 0, part.x.len)) --part.q1;
+                    auto idle = [&](int q) {
+                        const View::Span s = v.span_of(q);
+                        return s.first >= s.last;
+                    };
+                    while (part.q0 < part.q1 && idle(part.q0)) ++part.q0;
+                    while (part.q1 > part.q0 && idle(part.q1 - 1)) --part.q1;
                     unit += part.x.n;
                 }
                 mbar_arrive(&ctl->seg_full[nth & 1]);
