@@ -482,11 +482,13 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
         // ---------------- products ----------------
         const uint32_t hi = (uint32_t)(smem_desc_sw128(0) >> 32), lo = (uint32_t)smem_desc_sw128(0);
         const uint32_t kd = (smem_u32(sk) >> 4) + lo, qd = (smem_u32(sq) >> 4) + lo;
-        uint32_t item = 0, n_q = 0, k_parity = 0;
-        bool ok = !b.stall || blockIdx.x || wait_warp(&ctl->stall, 0, ctl, b.err, 14);
-        while (ok && begin()) {
-            const View v(b, parts[nth & 1], kStages<D>);
-            if (lane == 0) {
+        // (one thread for all of it, by elect: with a lane chosen otherwise the descriptors are not kept in the
+        // registers that the instruction takes them from)
+        if (elect_one()) {
+            uint32_t item = 0, n_q = 0, k_parity = 0;
+            bool ok = !b.stall || blockIdx.x || wait(&ctl->stall, 0, ctl, b.err, 14);
+            for (; ok && wait(&ctl->seg_full[nth & 1], nth >> 1 & 1, ctl, b.err, 9) && parts[nth & 1].x.n > 0; ++nth) {
+                const View v(b, parts[nth & 1], kStages<D>);
                 const View::Span used = v.used();
                 auto q_there = [&](int q) {
                     const uint32_t n = n_q + q - v.q0;
@@ -540,12 +542,9 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                     }
                     for (int k = used.first; k < used.last; ++k) k_done(k - used.first);
                 }
+                n_q += v.q1 - v.q0;
+                mbar_arrive(&ctl->seg_empty[nth & 1]);
             }
-            ok = __shfl_sync(0xFFFFFFFFu, (int)ok, 0);
-            n_q += v.q1 - v.q0;
-            finish();
-        }
-        if (lane == 0) {
             umma_commit(&ctl->done);
             drain(&ctl->done, 0);
         }
