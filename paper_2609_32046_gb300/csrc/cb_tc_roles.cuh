@@ -20,26 +20,27 @@ __device__ __forceinline__ uint64_t now_ns() {
 }
 
 // Bounded wait: false when it gave up or another role did (bits 8 + tag of the error word name the wait).
-// (Inline: a call would have to do with the registers of every role.)
-template <class Ctl>
+// (Inline: a call would have to do with the registers of every role.)  SLEEP: nanoseconds between looks.
+template <int SLEEP, class Ctl>
 __device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity, Ctl* c, uint32_t* err, int tag) {
     const uint64_t t0 = now_ns();
     do {
-        if (sm100::mbar_try_wait_hint(bar, parity, kPollNs)) return true;
+        if (SLEEP ? sm100::mbar_try_wait(bar, parity) : sm100::mbar_try_wait_hint(bar, parity, kPollNs)) return true;
+        if (SLEEP) __nanosleep(SLEEP);
         if (*reinterpret_cast<volatile int*>(&c->abort)) return false;
     } while (now_ns() - t0 <= c->wait_ns);
     *reinterpret_cast<volatile int*>(&c->abort) = 1;
     atomicOr(err, kErrTimeout | (1u << (8 + tag)));
     return false;
 }
-template <class Ctl>
+template <int SLEEP = 0, class Ctl>
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, Ctl* c, uint32_t* err, int tag) {
-    return sm100::mbar_try_wait(bar, parity) || poll(bar, parity, c, err, tag);
+    return sm100::mbar_try_wait(bar, parity) || poll<SLEEP>(bar, parity, c, err, tag);
 }
 // The same for a whole warp, which stays together whatever its lanes saw.
-template <class Ctl>
+template <int SLEEP = 0, class Ctl>
 __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl* c, uint32_t* err, int tag) {
-    return __all_sync(0xFFFFFFFFu, wait(bar, parity, c, err, tag));
+    return __all_sync(0xFFFFFFFFu, wait<SLEEP>(bar, parity, c, err, tag));
 }
 __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity) {
     const uint64_t t0 = now_ns();

@@ -35,6 +35,7 @@ template <int D> constexpr int kStages = D == 128 ? 2 : 4;    // tiles of query 
 // Tiles of their log-sum-exps, which the sums read: rows are copied up to kStages tiles ahead of the products, and these are
 // up to kBuffers + 1 buffers, of a tile each at most, ahead of the sums.
 constexpr int kLse = 16;
+constexpr int kSeldomNs = 200;               // between looks of the warps that nothing waits for at once
 static_assert(kLse >= 4 + kBuffers + 2, "");
 
 // Positions that pass are in two of the tiles' places by turns; the other two hold their packed rows on their way, each of
@@ -53,11 +54,12 @@ struct Share {
 struct Ctl {
     uint64_t k_full[kTiles], k_empty[kTiles], q_full[4], q_empty[4];
     uint64_t d_full[kBuffers], d_empty[kBuffers], sum_full[kTiles], sum_empty[kTiles];
-    uint64_t seg_full[2], seg_empty[2], shares;
+    uint64_t seg_full[2], seg_empty[2];
     uint64_t done, stall;
     uint64_t wait_ns;
     uint32_t tmem;
     int abort;
+    int loaded;             // what the load warps' wait came to
 };
 // A segment of the run, and the tiles [q0, q1) of query rows that see something of it (n = 0: the run is over).
 struct Part {
@@ -110,6 +112,19 @@ __device__ __forceinline__ void copy16_or_0(uint32_t to, const void* from, bool 
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
 }
 
+// Shared memory by its own addresses.
+__device__ __forceinline__ float4 lds128(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float lds(uint32_t at) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts(uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
+
 // A thread's share of a tile's keys on their way: a quarter of each of two rows.
 template <int D>
 struct Codes {
@@ -150,7 +165,6 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
             mbar_init(&ctl->seg_full[i], 1);
             mbar_init(&ctl->seg_empty[i], kReaders);
         }
-        mbar_init(&ctl->shares, kLoadWarps);
         mbar_init(&ctl->done, 1);
         mbar_init(&ctl->stall, 1);
         ctl->wait_ns = b.wait_ns;
@@ -183,7 +197,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
         const int group = warp >> 2, mine = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + 32 * group;      // (lane 32 (warp % 4) << 16)
         const uint64_t cc = pack2(b.scale_log2e, b.scale_log2e);
-        float* sums = s_sum + group * kTile + mine;
+        const uint32_t sums = smem_u32(s_sum) + 4 * (group * kTile + mine), lses = smem_u32(s_lse) + 128 * group;
         uint32_t item = 0, n_q = 0, n_tile = 0;
         bool ok = true;
         while (ok && begin()) {
@@ -211,7 +225,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 return c0 >= c1 ? 0u : (0xFFFFFFFFu << c0) & (0xFFFFFFFFu >> (32 - c1));
             };
             // the sum of the thread's columns of one product; some: its group has any
-            auto gather = [&](int row0, int k, bool some, bool edge, const float* lse) {
+            auto gather = [&](int row0, int k, bool some, bool edge, uint32_t lse) {
                 const uint32_t d = item % kBuffers, phase = item / kBuffers & 1;
                 ++item;
                 if (!(ok = wait_warp(&ctl->d_full[d], phase, ctl, b.err, 10))) return 0.f;
@@ -236,7 +250,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 uint64_t l0 = 0, l1 = 0;
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
-                    const float4 nl = *reinterpret_cast<const float4*>(lse + e);
+                    const float4 nl = lds128(lse + 4 * e);
                     float y0, y1, y2, y3;
                     unpack2(ffma2(pack2(z[e], z[e + 1]), cc, pack2(nl.x, nl.y)), y0, y1);
                     unpack2(ffma2(pack2(z[e + 2], z[e + 3]), cc, pack2(nl.z, nl.w)), y2, y3);
@@ -247,7 +261,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 unpack2(fadd2(l0, l1), a0, a1);
                 return a0 + a1;
             };
-            auto place = [&](int k) { return sums + (n_tile + k) % kTiles * kGroups * kTile; };
+            auto place = [&](int k) { return sums + (n_tile + k) % kTiles * (kGroups * kTile * 4); };
             // a tile's place in shared memory, which the writer has left
             auto open = [&](int k) {
                 const uint32_t n = n_tile + k;
@@ -258,7 +272,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&ctl->sum_full[(n_tile + k) % kTiles]);
             };
-            auto lse_at = [&](int q) { return s_lse + (n_q + q - v.q0) % kLse * kTile + 32 * group; };
+            auto lse_at = [&](int q) { return lses + (n_q + q - v.q0) % kLse * (kTile * 4); };
             if (v.resident) {
                 for (int k = 0; k < v.tiles && open(k); ++k) {
                     float sum = 0.f;
@@ -267,17 +281,20 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                         const int row0 = q * kTile + 32 * group;
                         if (k >= s.first && k < s.last) sum += gather(row0, k, row0 < v.rows, k < s.low || k >= s.high, lse_at(q));
                     }
-                    *place(k) = sum;
+                    sts(place(k), sum);
                     close(k);
                 }
             } else {
-                for (int k = 0; k < v.tiles && open(k); ++k) *place(k) = 0.f;
+                for (int k = 0; k < v.tiles && open(k); ++k) sts(place(k), 0.f);
                 for (int q = v.q0; q < v.q1 && ok; ++q) {
                     const View::Span s = v.span_of(q);
                     const int row0 = q * kTile + 32 * group;
-                    const float* lse = lse_at(q);
+                    const uint32_t lse = lse_at(q);
 #pragma unroll 1
-                    for (int k = s.first; k < s.last && ok; ++k) *place(k) += gather(row0, k, row0 < v.rows, k < s.low || k >= s.high, lse);
+                    for (int k = s.first; k < s.last && ok; ++k) {
+                        const float sum = gather(row0, k, row0 < v.rows, k < s.low || k >= s.high, lse);
+                        sts(place(k), lds(place(k)) + sum);
+                    }
                 }
                 for (int k = 0; k < v.tiles; ++k) close(k);
             }
@@ -299,8 +316,20 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
         uint8_t* share = sk + 2 * kOp + lw * (Share<D>::kAhead * Share<D>::kBytes);
         const uint32_t share32 = smem_u32(share);
         uint32_t n_q = 0, k_parity = 0, k_used = 0, bad = 0;      // bits: uses of a tile's place, any use
+        // One warp waits for all eight, which meet at a barrier in hardware: eight warps that poll took the issue slots of
+        // the sums.  (They meet whatever it saw, and all go by it.)
+        auto together = [&](uint64_t* bar, uint32_t parity, int tag) {
+            if (lw == 0) {
+                const bool there = wait_warp(bar, parity, ctl, b.err, tag);
+                if (lane == 0) ctl->loaded = there;
+            }
+            asm volatile("bar.sync 2, %0;" ::"n"(kLoadThreads) : "memory");
+            const bool there = *reinterpret_cast<volatile int*>(&ctl->loaded);
+            asm volatile("bar.sync 2, %0;" ::"n"(kLoadThreads) : "memory");
+            return there;
+        };
         bool ok = true;
-        while (ok && begin()) {
+        while (ok && together(&ctl->seg_full[nth & 1], nth >> 1 & 1, 9) && parts[nth & 1].x.n > 0) {
             const Part& part = parts[nth & 1];
             const Segment& x = part.x;
             const View v(b, part, kStages<D>);
@@ -309,10 +338,8 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
             const float* lses = b.w[x.seq].lse + head;
             const uint16_t* q_from = s.q + (int64_t)head * s.s_head + u % P * 8;
             const int64_t tok_bytes = s.s_tok;
-            // (tiles that stay take the place of the shares: every warp has read what its last segment left there)
-            if (nth && !(ok = wait_warp(&ctl->shares, (nth - 1) & 1, ctl, b.err, 13))) break;
             auto vacant = [&](int slot) {
-                return !(k_used >> slot & 1) || wait_warp(&ctl->k_empty[slot], (k_parity >> slot & 1) ^ 1, ctl, b.err, 13);
+                return !(k_used >> slot & 1) || together(&ctl->k_empty[slot], (k_parity >> slot & 1) ^ 1, 13);
             };
             auto filled = [&](int slot) {
                 fence_async_smem();
@@ -330,7 +357,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
             };
             auto copy_rows = [&](int q, const float (&lse)[R]) {       // into a stage that the products have left
                 const uint32_t n = n_q + q - v.q0;
-                if (n >= (uint32_t)kStages<D> && !wait_warp(&ctl->q_empty[n % kStages<D>], (n / kStages<D> - 1) & 1, ctl, b.err, 12)) {
+                if (n >= (uint32_t)kStages<D> && !together(&ctl->q_empty[n % kStages<D>], (n / kStages<D> - 1) & 1, 12)) {
                     ok = false;
                     return;
                 }
@@ -341,7 +368,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
 #pragma unroll
                 for (int i = 0; i < R; ++i) {
                     const bool there = isfinite(lse[i]);
-                    copy16_or_0(to + i * N * 128, there ? from + i * step : s.q, there);
+                    copy16_or_0(to + i * N * 128, from + i * step, there);            // (reads nothing where it is not)
                     if (u % P == 0) l[i * N] = there ? lse[i] * -1.4426950408889634f : -INFINITY;
                 }
             };
@@ -472,8 +499,6 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 }
             }
             n_q += v.q1 - v.q0;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ctl->shares);
             finish();
         }
         copy_wait<0>();
@@ -563,7 +588,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 float before[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) before[i] = v.w.before(ws, g, k * kTile + 32 * i + lane);
-                if (!(ok = wait_warp(&ctl->sum_full[n_tile % kTiles], n_tile / kTiles & 1, ctl, b.err, 17))) break;
+                if (!(ok = wait_warp<kSeldomNs>(&ctl->sum_full[n_tile % kTiles], n_tile / kTiles & 1, ctl, b.err, 17))) break;
                 const float* sums = s_sum + n_tile % kTiles * kGroups * kTile + lane;
                 float sum[4];
 #pragma unroll
@@ -590,7 +615,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
             int unit = attend_run(runs, run);
             for (bool more = true; more; ++nth) {
                 Part& part = parts[nth & 1];
-                if (nth >= 2 && !wait(&ctl->seg_empty[nth & 1], (nth / 2 - 1) & 1, ctl, b.err, 18)) break;
+                if (nth >= 2 && !wait<kSeldomNs>(&ctl->seg_empty[nth & 1], (nth / 2 - 1) & 1, ctl, b.err, 18)) break;
                 more = unit < end;
                 part.x.n = 0;
                 if (more) {
