@@ -234,19 +234,30 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                     return 0.f;
                 }
                 tc_fence_after();
+                auto leave = [&]() {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ctl->d_empty[d]);
+                };
+                if (edge) {                                     // (apart: what is masked in place is moved about elsewhere too)
+                    const uint32_t bits = sees(row0, k);
+                    float sum = 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < 32; c += 8) {
+                        float z[8];
+                        tmem_ld8(from + d * 128 + c, z);
+                        tmem_wait_ld(z);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            sum += bits >> (c + e) & 1u ? ex2(fmaf(z[e], b.scale_log2e, lds(lse + 4 * (c + e)))) : 0.f;
+                    }
+                    leave();
+                    return sum;
+                }
                 float z[32];
                 tmem_ld32(from + d * 128, z);
-                uint32_t bits = 0xFFFFFFFFu;
-                if (edge) bits = sees(row0, k);
                 tmem_wait_ld(z);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&ctl->d_empty[d]);
-                if (edge) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (!(bits >> e & 1u)) z[e] = -INFINITY;
-                }
+                leave();
                 uint64_t l0 = 0, l1 = 0;
 #pragma unroll
                 for (int e = 0; e < 32; e += 4) {
