@@ -872,39 +872,72 @@ class CacheBack:
         _require(len(weights) == n and all(x is None or len(x) == n for x in (into, weights_into, idx, lengths)),
                  "one entry per cache in every list")
         _require(into is not None or weights_into is None, "weights move where the rows do")
+        like, targets = self._shape, caches if into is None else into
         keep = [int(k) for k in _each(keep, n, "keep")]
-        targets = caches if into is None else into
         if idx is None:
             import torch
             idx = [torch.empty(tuple(w.shape[:2]) + (k,), dtype=torch.int32, device=p.device) for w, k, p in zip(weights, keep, caches)]
-        layers = weights[0].shape[0] if n else 0
+        many = [hasattr(x, "data_ptr") for x in (weights, weights_into, idx)]      # one tensor each
+        most = max([p.T for p in caches], default=0)
+        if many[0]:
+            _require(weights.dim() == 4, "weights are fp32 [sequences][layers][Hkv][rows]")
+            layers, (w, w_step, ws) = weights.shape[1], self._weights(weights, weights.shape[1], most)
+        else:
+            layers = weights[0].shape[0] if n else 0
+        if many[1]:
+            out, out_step, ts = self._weights(weights_into, layers, min(max(keep, default=0), most))
+        if many[2]:
+            k = idx.shape[-1]
+            if not (_is_int32(idx) and tuple(idx.shape[1:3]) == (layers, like[1]) and all(x == k for x in keep) and
+                    (n == 0 or idx[0].is_contiguous())):
+                raise ValueError("idx is int32 [sequences][layers][Hkv][keep]")
+            at, at_step = idx.data_ptr(), 4 * idx.stride(0)
         fields, left = array("q"), []         # of the header's cb_eviction, eight bytes each
-        for i, (p, to, w, k) in enumerate(zip(caches, targets, weights, keep)):
-            self._fits(p)
-            self._fits(to)
-            out = w if to is p else None if weights_into is None else weights_into[i]
-            for x, rows in ((w, p.T),) if out is None or out is w else ((w, p.T), (out, min(k, p.T))):
-                if not (x.dim() == 3 and _is_f32(x) and x.shape[0] == layers and x.shape[1] == p.n_kv_heads and x.shape[2] >= rows and
-                        (x.stride(2) == 1 or x.shape[2] == 1)):
-                    raise ValueError("weights are fp32 [layers][Hkv][rows]")
-            at = idx[i]
-            if not (_is_int32(at) and at.is_contiguous() and tuple(at.shape) == (layers, p.n_kv_heads, k)):
-                raise ValueError("idx is int32 [layers][Hkv][keep]")
+        first, last = int(first), int(last)
+        for i in range(n):
+            p, to, k = caches[i], targets[i], keep[i]
+            if p._shape != like or to._shape != like:
+                self._fits(p)
+                self._fits(to)
+            if not many[0]:
+                w, w_step, ws = self._weights(weights[i], layers, p.T)
+            if to is p:
+                out, out_step, ts = w, w_step, ws
+            elif not many[1]:
+                x = None if weights_into is None else weights_into[i]
+                out, out_step, ts = (0, 0, (0, 0)) if x is None else self._weights(x, layers, min(k, p.T))
+            if not many[2]:
+                x = idx[i]
+                if not (_is_int32(x) and x.is_contiguous() and tuple(x.shape) == (layers, like[1], k)):
+                    raise ValueError("idx is int32 [layers][Hkv][keep]")
+                at, at_step = x.data_ptr(), 0
             own = to.length if lengths is None else lengths[i]
-            _require(own is None or (_is_int32(own) and own.numel() == 1), "a length is one int32")
-            _require(own is not None or p.length is None, "a length on the device needs one that receives the rows kept")
-            left.append(own)
-            ws, ts = w.stride(), (0, 0) if out is None else out.stride()
-            fields.extend((w.data_ptr(), _address(out), ws[0], ws[1], ts[0], ts[1], k, int(first), int(last), at.data_ptr(), _address(own)))
+            if own is None:
+                _require(p.length is None, "a length on the device needs one that receives the rows kept")
+                length = 0
+            else:
+                _require(own.numel() == 1 and _is_int32(own), "a length is one int32")
+                length = own.data_ptr()
+            left.append(length)
+            fields.extend((w + i * w_step, out + i * out_step, ws[0], ws[1], ts[0], ts[1], k, first, last, at + i * at_step, length))
         held = b"".join([p._state[1] or p._described() for p in caches])
         taken = None if into is None else b"".join([p._described() if p is q else p._described_room() for p, q in zip(into, caches)])
         self._check(self.lib.cb_evict(self.h, int(layer), int(layers), n, held, taken, fields.buffer_info()[0],
                                       _stream_on(stream, caches[0].k) if n else 0))
         if lengths is None:
             for p, to, k, own in zip(caches, targets, keep, left):
-                if own is None:
+                if not own:
                     to.T = min(p.T, k)
         return idx
+
+    def _weights(self, x, layers: int, rows: int):
+        """fp32 [layers][Hkv][rows or more], or one such a sequence in a tensor: its address, the bytes to the next sequence's, and
+        the strides of layers and heads."""
+        shape, st = x.shape, x.stride()
+        if not (_is_f32(x) and len(shape) in (3, 4) and tuple(shape[-3:-1]) == (layers, self._shape[1]) and shape[-1] >= rows and
+                (st[-1] == 1 or shape[-1] == 1)):
+            raise ValueError("weights are fp32 [layers][Hkv][rows]")
+        return x.data_ptr(), 4 * st[0] if len(shape) == 4 else 0, st[-3:-1]
 
     def keep(self, caches: Sequence, idx: Sequence, drafted, counts: Optional[Sequence] = None, weights: Optional[Sequence] = None,
              lengths: Optional[Sequence] = None, stream=None):
@@ -931,14 +964,10 @@ class CacheBack:
         elif counts is None:
             count = count_step = 0
         if many[2]:
-            ws = weights.stride()
-            most = max([p.T for p in caches], default=0)
-            _require(len(ws) == 4 and _is_f32(weights) and tuple(weights.shape[1:3]) == like[:2] and weights.shape[3] >= most and
-                     (ws[3] == 1 or weights.shape[3] == 1), "weights are fp32 [sequences][layers][Hkv][rows]")
-            w, w_step, ws = weights.data_ptr(), 4 * ws[0], ws[1:3]
+            _require(weights.dim() == 4, "weights are fp32 [sequences][layers][Hkv][rows]")
+            w, w_step, ws = self._weights(weights, like[0], max([p.T for p in caches], default=0))
         elif weights is None:
-            w = w_step = 0
-            ws = (0, 0)
+            w, w_step, ws = 0, 0, (0, 0)
         for i, p in enumerate(caches):
             if p._shape != like:
                 self._fits(p)
@@ -952,12 +981,7 @@ class CacheBack:
                 _require(x is None or (_is_int32(x) and x.numel() == 1), "a count is one int32")
                 count, count_step = _address(x), 0
             if not many[2] and weights is not None:
-                x = weights[i]
-                w, w_step, ws = _address(x), 0, (0, 0)
-                if x is not None:
-                    ws = x.stride()
-                    _require(len(ws) == 3 and _is_f32(x) and tuple(x.shape[:2]) == like[:2] and x.shape[2] >= p.T and
-                             (ws[2] == 1 or x.shape[2] == 1), "weights are fp32 [layers][Hkv][rows]")
+                w, w_step, ws = (0, 0, (0, 0)) if weights[i] is None else self._weights(weights[i], like[0], p.T)
             own = p.length if lengths is None else lengths[i]
             if own is None:
                 _require(not count and p.length is None, "lengths and counts on the device need a length that receives the rows left")

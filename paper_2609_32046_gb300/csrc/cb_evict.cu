@@ -1,4 +1,5 @@
 // Rows of 4-bit caches that stay (cb_evict, cb_keep): which (k_rank), and their moving together (k_move).
+#include <atomic>
 #include <cooperative_groups.h>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -17,7 +18,7 @@ __device__ __forceinline__ int64_t rows_of(int64_t T, const int32_t* length) {
 
 // ---- which rows stay ----------------------------------------------------------------------------
 
-constexpr int kRankThreads = 512;
+constexpr int kRankThreads = 1024, kRankWarps = kRankThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kRankPasses = 3;
 constexpr int kRankKeys = 24 * 1024;         // keys of a block's slice held in shared memory at most (96 KB)
@@ -41,34 +42,36 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t& before, uin
     }
     if (lane == 31) sh[warp] = x;
     __syncthreads();
-    uint32_t all = 0, mine = 0;
+    uint32_t w = sh[lane];                               // (as many warps as lanes)
+    const uint32_t own = w;
 #pragma unroll
-    for (int i = 0; i < kRankThreads / 32; ++i) {
-        if (i == warp) mine = all;
-        all += sh[i];
+    for (int k = 1; k < 32; k *= 2) {
+        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, w, k);
+        if (lane >= k) w += y;
     }
+    const uint32_t all = __shfl_sync(0xFFFFFFFFu, w, 31), mine = __shfl_sync(0xFFFFFFFFu, w - own, warp);
     __syncthreads();
     before = mine + x - v;
     return all;
 }
+static_assert(kRankWarps == 32 && kBins == 2 * kRankThreads, "");
 
 // A cluster of blocks ranks one list (cache, layer, KV head), a slice of its inner rows each: a radix select by 11, 11 and
 // 10 bits from the top finds the key where the budget runs out (histograms joined in the first block's shared
-// memory); rows above it stay, and of those at it the lowest.
-template <int C>
+// memory); rows above it stay, and of those at it the lowest.  HELD: no slice has more keys than shared memory holds.
+template <int C, bool HELD>
 __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ RankBatch b, uint32_t held) {
     extern __shared__ uint32_t keys[];                   // [held]
     __shared__ uint32_t own[kBins], all[C > 1 ? kRankPasses : 1][C > 1 ? kBins : 1];
-    __shared__ uint32_t scan[kRankThreads / 32];
+    __shared__ uint32_t scan[kRankWarps];
     __shared__ uint32_t found[3];                        // bin, keys above it, keys in it
     __shared__ uint32_t counts[2];                       // this block's keys above the last, and at it
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = C > 1 ? (int)cluster.block_rank() : 0;
-    const int list = blockIdx.x / C, lists = b.n_layers * b.n_kv_heads;
+    const int list = blockIdx.x / C, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const RankSeq& s = b.s[blockIdx.y];
     const int64_t L = rows_of(s.T, s.length);
     int32_t* idx = s.idx + list * s.keep;
-    if (list >= lists) return;
     if (L <= s.keep) {
         for (int64_t j = (int64_t)rank * kRankThreads + threadIdx.x; j < s.keep; j += C * kRankThreads)
             idx[j] = j < L ? (int32_t)j : -1;
@@ -84,53 +87,64 @@ __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ R
     const uint32_t per = ((n + C - 1) / C + 3) & ~3u;
     const uint32_t lo = min(n, rank * per), len = min(n, lo + per) - lo;
     w += lo;
-    auto key = [&](uint32_t i) { return i < held ? keys[i] : rank_key(__ldg(w + i)); };
+    auto key = [&](uint32_t i) { return HELD || i < held ? keys[i] : rank_key(__ldg(w + i)); };
 
-    if (C > 1)
-        for (int i = threadIdx.x; i < kRankPasses * kBins; i += kRankThreads) all[i / kBins][i % kBins] = 0;
-#pragma unroll 8
-    for (uint32_t i = threadIdx.x; i < min(len, held); i += kRankThreads) keys[i] = rank_key(__ldg(w + i));
+    for (int i = threadIdx.x; i < kBins; i += kRankThreads) {
+        own[i] = 0;
+        if (C > 1) all[0][i] = all[C > 1 ? 1 : 0][i] = all[C > 1 ? 2 : 0][i] = 0;
+    }
+    __syncthreads();
+    for (uint32_t i0 = threadIdx.x; i0 < len; i0 += 8 * kRankThreads) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = i0 + k * kRankThreads < len ? __ldg(w + i0 + k * kRankThreads) : 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t i = i0 + k * kRankThreads, y = rank_key(x[k]);
+            if (i >= len) break;
+            if (HELD || i < held) keys[i] = y;
+            atomicAdd(&own[y >> 21], 1u);                        // the first pass
+        }
+    }
     if (C > 1) cluster.sync();
+    else __syncthreads();
     uint32_t need = want, prefix = 0, above = 0, equal = 0;      // above, equal: this block's
     int shift = 32;
 #pragma unroll 1
     for (int pass = 0; pass < kRankPasses; ++pass) {
         const int bits = pass == 2 ? 10 : 11, up = shift;        // keys that match `prefix` in the bits from `up` on
         shift -= bits;
-        for (int i = threadIdx.x; i < kBins; i += kRankThreads) own[i] = 0;
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < len; i += kRankThreads) {
-            const uint32_t k = key(i);
-            if (pass == 0 || k >> up == prefix) atomicAdd(&own[(k >> shift) & ((1u << bits) - 1)], 1u);
+        if (pass) {
+            for (int i = threadIdx.x; i < kBins; i += kRankThreads) own[i] = 0;
+            __syncthreads();
+#pragma unroll 4
+            for (uint32_t i = threadIdx.x; i < len; i += kRankThreads) {
+                const uint32_t k = key(i);
+                if (k >> up == prefix) atomicAdd(&own[(k >> shift) & ((1u << bits) - 1)], 1u);
+            }
+            __syncthreads();
         }
-        __syncthreads();
         uint32_t* joined = C > 1 ? cluster.map_shared_rank(all[C > 1 ? pass : 0], 0) : own;
         if (C > 1) {
             for (int i = threadIdx.x; i < kBins; i += kRankThreads)
                 if (own[i]) atomicAdd(joined + i, own[i]);
             cluster.sync();
         }
-        // bins from the top: thread t has bins 4 (511 - t) .. + 3
-        const int bin0 = kBins - 4 - 4 * threadIdx.x;
-        uint32_t c[4], before;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) c[k] = joined[bin0 + 3 - k];
-        block_scan(c[0] + c[1] + c[2] + c[3], before, scan);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (before < need && need <= before + c[k]) {
-                found[0] = bin0 + 3 - k;
-                found[1] = before;
-                found[2] = c[k];
-            }
-            before += c[k];
+        // bins from the top: thread t has bins 2 (1023 - t) + 1 and 2 (1023 - t)
+        const int bin0 = kBins - 2 - 2 * threadIdx.x;
+        const uint32_t c0 = joined[bin0 + 1], c1 = joined[bin0];
+        uint32_t before;
+        block_scan(c0 + c1, before, scan);
+        if (before < need && need <= before + c0 + c1) {
+            const bool upper = need <= before + c0;
+            found[0] = bin0 + upper;
+            found[1] = upper ? before : before + c0;
+            found[2] = upper ? c0 : c1;
         }
         __syncthreads();
         const uint32_t bin = found[0];
-        uint32_t mine = 0, nothing;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) mine += (uint32_t)(bin0 + 3 - k) > bin ? own[bin0 + 3 - k] : 0;
-        above += block_scan(mine, nothing, scan);
+        uint32_t nothing;
+        above += block_scan(((uint32_t)bin0 + 1 > bin ? own[bin0 + 1] : 0) + ((uint32_t)bin0 > bin ? own[bin0] : 0), nothing, scan);
         equal = own[bin];
         need -= found[1];
         prefix = prefix << bits | bin;
@@ -153,27 +167,30 @@ __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ R
         }
         cluster.sync();                                          // (no block leaves while another reads its memory)
     }
-    for (uint32_t i0 = 0; i0 < len; i0 += 4 * kRankThreads) {
-        const uint32_t i = i0 + 4 * threadIdx.x;
-        uint32_t v = 0, stays[4];                                // above in the low half, at it in the high half
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t x = i + k < len ? key(i + k) >> shift : 0;
-            stays[k] = i + k >= len ? 0u : x > prefix ? 1u : x == prefix ? 0x10000u : 0u;
-            v += stays[k];
-        }
-        uint32_t before;
-        const uint32_t sum = block_scan(v, before, scan);
-        uint32_t a = above0 + (before & 0xFFFFu), e = equal0 + (before >> 16);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (stays[k] == 1u || (stays[k] && e < need))
-                idx[s.first + a + min(e, need)] = (int32_t)(s.first + lo + i + k);
-            a += stays[k] & 0xFFFFu;
-            e += stays[k] >> 16;
-        }
-        above0 += sum & 0xFFFFu;
-        equal0 += sum >> 16;
+    // every warp a run of the keys: counted, then written
+    const uint32_t run = ((len + kRankWarps - 1) / kRankWarps + 31) & ~31u, from = min(len, warp * run), to = min(len, from + run);
+    uint32_t n_above = 0, n_equal = 0;
+#pragma unroll 4
+    for (uint32_t i = from; i < to; i += 32) {
+        const uint32_t x = i + lane < to ? key(i + lane) >> shift : 0;
+        n_above += __popc(__ballot_sync(0xFFFFFFFFu, i + lane < to && x > prefix));
+        n_equal += __popc(__ballot_sync(0xFFFFFFFFu, i + lane < to && x == prefix));
+    }
+    uint32_t before;
+    block_scan(lane ? 0 : n_above, before, scan);
+    above0 += __shfl_sync(0xFFFFFFFFu, before, 0);
+    block_scan(lane ? 0 : n_equal, before, scan);
+    equal0 += __shfl_sync(0xFFFFFFFFu, before, 0);
+    const uint32_t below = (1u << lane) - 1;
+#pragma unroll 4
+    for (uint32_t i = from; i < to; i += 32) {
+        const uint32_t x = i + lane < to ? key(i + lane) >> shift : 0;
+        const bool over = i + lane < to && x > prefix, at = i + lane < to && x == prefix;
+        const uint32_t o = __ballot_sync(0xFFFFFFFFu, over), e = __ballot_sync(0xFFFFFFFFu, at);
+        const uint32_t mine = equal0 + __popc(e & below);
+        if (over || (at && mine < need)) idx[s.first + above0 + __popc(o & below) + min(mine, need)] = (int32_t)(s.first + lo + i + lane);
+        above0 += __popc(o);
+        equal0 += __popc(e);
     }
 }
 
@@ -183,17 +200,17 @@ constexpr uint32_t kNone = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint4 ld16(const void* p) {
     uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    asm volatile("ld.global.L1::no_allocate.L2::64B.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
 __device__ __forceinline__ uint2 ld8(const void* p) {
     uint2 v;
-    asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    asm volatile("ld.global.L2::64B.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
     return v;
 }
 __device__ __forceinline__ uint32_t ld4(const void* p) {
     uint32_t v;
-    asm volatile("ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    asm volatile("ld.global.L2::64B.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
     return v;
 }
 
@@ -205,12 +222,88 @@ struct Held {
     uint32_t weight;
 };
 
+// What a call makes of one cache: row base + j becomes row base + idx[j], j < count, idx[j] in j .. limit - 1.
+struct Moving {
+    int64_t base, count, limit;
+    bool lists_own;
+    // first: of the thread that says how many rows are left, and what was wrong.  (Of lists of their own, no other reads the
+    // length.)
+    __device__ __forceinline__ Moving(const MoveBatch& b, const MoveSeq& s, bool first) : lists_own(s.drafted < 0) {
+        const bool says = first && s.left && !s.left_later;
+        const int64_t L = !lists_own || says ? rows_of(s.T, s.length) : 0;
+        base = lists_own ? 0 : L - s.drafted;
+        limit = lists_own ? s.T : s.drafted;
+        count = s.count;
+        if (s.n_kept) count = max((int64_t)0, min((int64_t)__ldcg(s.n_kept), count));
+        if (base < 0) {                       // fewer rows than `drafted`
+            count = 0;
+            if (first) atomicOr(b.err, kErrPackRow);
+        } else if (says) {
+            *s.left = (int32_t)(lists_own ? min(L, count) : base + count);
+        }
+    }
+    // Entry j's row of `from` and of `to`; false where nothing is moved.
+    __device__ __forceinline__ bool rows(const MoveBatch& b, const MoveSeq& s, int64_t j, int64_t i, uint2& r) const {
+        if (lists_own && i == -1) return false;
+        if (i < j || i >= limit) {
+            atomicOr(b.err, kErrCompactIndex);
+            return false;
+        }
+        if (i == j && s.in_place) return false;
+        const int64_t x = packed_row(s.from, base + i), y = packed_row(s.to, base + j);
+        if (x < 0 || y < 0) {
+            atomicOr(b.err, kErrPageIndex);
+            return false;
+        }
+        r = make_uint2((uint32_t)x, (uint32_t)y);
+        return true;
+    }
+};
+
+// Up to 32 entries: a thread moves a row of K or of V of one list, the block 256 / C of them (C: the power of two that
+// has room for the entries).  All read before any writes.
+template <int D>
+__global__ void __launch_bounds__(256) k_move_few(const __grid_constant__ MoveBatch b, int C) {
+    const MoveSeq& s = b.s[blockIdx.z];
+    const int per = 256 / C, j = threadIdx.x % C, unit = blockIdx.x * per + threadIdx.x / C;
+    const Moving m(b, s, blockIdx.x == 0 && threadIdx.x == 0);
+    const int kv = unit & 1, list = unit >> 1, l = list / b.n_kv_heads, g = list % b.n_kv_heads;
+    uint2 r = make_uint2(0, 0);
+    uint4 code[D / 32];
+    uint2 scale;
+    uint32_t weight;
+    int64_t i = 0;
+    bool moves = list < b.n_layers * b.n_kv_heads && j < m.count;
+    if (moves) {
+        i = s.idx[list * s.idx_list + j];
+        moves = m.rows(b, s, j, i, r);
+    }
+    const bool weigh = kv == 0 && s.w;
+    if (moves) {
+        const uint64_t row = (uint64_t)(l * s.from.s_layer + g * s.from.s_head) + r.x;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) code[k] = ld16(s.from.code[kv] + row * (D / 2) + 16 * k);
+        if (D == 128) scale = ld8(s.from.scale[kv] + row * (D / 32));
+        else scale.x = ld4(s.from.scale[kv] + row * (D / 32));
+        if (weigh) weight = ld4(s.w + l * s.w_layer + g * s.w_head + m.base + i);
+    }
+    __syncthreads();
+    if (moves) {
+        const uint64_t row = (uint64_t)(l * s.to.s_layer + g * s.to.s_head) + r.y;
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) *reinterpret_cast<uint4*>(s.to.code[kv] + row * (D / 2) + 16 * k) = code[k];
+        if (D == 128) *reinterpret_cast<uint2*>(s.to.scale[kv] + row * (D / 32)) = scale;
+        else *reinterpret_cast<uint32_t*>(s.to.scale[kv] + row * (D / 32)) = scale.x;
+        if (weigh) reinterpret_cast<uint32_t*>(s.w_to)[l * s.t_layer + g * s.t_head + m.base + j] = weight;
+    }
+}
+
 // A group of threads moves the rows of K or of V of one list, a row a thread a step: GROUP = 32, a warp; else a block, or
 // the blocks of a cluster together.  In place a row's source is never before its place, so what a step writes is
 // read by no later one; within a step every group reads before any writes (a barrier), and the next step's rows are on
-// their way by then.
+// their way by then, as are the entries of the one after it.
 template <int D, int GROUP>
-__global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch b, int blocks, int clustered) {
+__global__ void __launch_bounds__(256, 3) k_move(const __grid_constant__ MoveBatch b, int blocks, int clustered) {
     constexpr int P = D / 32;                 // pieces of a row's codes
     constexpr int N = GROUP / P;              // rows that a piece a thread covers
     __shared__ uint2 where[2][256];           // rows of the cache: from, to
@@ -219,18 +312,9 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
     const int t = threadIdx.x % GROUP;
     const int group = GROUP == 32 ? blockIdx.x * (256 / 32) + threadIdx.x / 32 : blockIdx.x;
     const int unit = group / blocks, part = group % blocks;
-    // (of lists of their own, only the thread that writes the number of rows reads the length)
-    const bool lists_own = s.drafted < 0, says = group == 0 && t == 0 && s.left && !s.left_later;
-    const int64_t L = !lists_own || says ? rows_of(s.T, s.length) : 0;
-    const int64_t base = lists_own ? 0 : L - s.drafted, limit = lists_own ? s.T : s.drafted;
-    int64_t count = s.count;
-    if (s.n_kept) count = max((int64_t)0, min((int64_t)*s.n_kept, count));
-    if (base < 0) {
-        if (group == 0 && t == 0) atomicOr(b.err, kErrPackRow);
-        return;
-    }
-    if (says) *s.left = (int32_t)(lists_own ? min(L, count) : base + count);
+    const Moving m(b, s, group == 0 && t == 0);
     if (unit >= 2 * lists) return;            // (a whole group)
+    const int64_t base = m.base, count = m.count;
     const int kv = unit % 2, list = unit / 2, l = list / b.n_kv_heads, g = list % b.n_kv_heads;
     const int64_t from0 = l * s.from.s_layer + g * s.from.s_head, to0 = l * s.to.s_layer + g * s.to.s_head;
     const uint8_t* code = s.from.code[kv] + from0 * (D / 2) + t % P * 16;
@@ -243,32 +327,13 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
     const int32_t* idx = s.idx + list * s.idx_list;
     uint2* rows = where[0] + threadIdx.x / GROUP * GROUP;      // and 256 on
 
-    // the row of the thread at step j0, looked up: its entry (-1: none)
-    auto look_up = [&](int64_t j0, uint2* to) {
-        const int64_t j = j0 + t;
+    // the thread's entry of the step at j0 (-1: none), and its rows
+    auto entry = [&](int64_t j0) { return j0 + t < count ? (int64_t)idx[j0 + t] : -1; };
+    auto look_up = [&](int64_t j0, int64_t i, uint2* to) {
         uint2 r = make_uint2(kNone, kNone);
-        int64_t i = -1;
-        if (j < count) {
-            i = idx[j];
-            if (lists_own && i == -1) {
-            } else if (i < j || i >= limit) {
-                atomicOr(b.err, kErrCompactIndex);
-                i = -1;
-            }
-        }
-        if (i >= 0 && (i != j || !s.in_place)) {
-            const int64_t x = packed_row(s.from, base + i), y = packed_row(s.to, base + j);
-            if (x < 0 || y < 0) {
-                atomicOr(b.err, kErrPageIndex);
-                i = -1;
-            } else {
-                r = make_uint2((uint32_t)x, (uint32_t)y);
-            }
-        } else {
-            i = -1;
-        }
+        const bool moves = j0 + t < count && m.rows(b, s, j0 + t, i, r);
         to[t] = r;
-        return i;
+        return moves ? i : -1;
     };
     auto meet = [&] {
         if (GROUP == 32) __syncwarp();
@@ -290,14 +355,17 @@ __global__ void __launch_bounds__(256) k_move(const __grid_constant__ MoveBatch 
     const int64_t step = (int64_t)GROUP * blocks;
     int64_t j0 = (int64_t)part * GROUP;
     const int64_t steps = (count + step - 1) / step;      // (the same for all of a cluster)
-    int64_t i = look_up(j0, rows);
+    int64_t ahead = entry(j0);
+    int64_t i = look_up(j0, ahead, rows);
+    ahead = entry(j0 + step);
     meet();
     Held<D> h;
     load(rows, i, h);
     for (int64_t n = 0; n < steps; ++n, j0 += step) {
         uint2* here = rows + (n & 1) * 256;
         uint2* next = rows + (~n & 1) * 256;
-        const int64_t i1 = n + 1 < steps ? look_up(j0 + step, next) : -1;
+        const int64_t i1 = look_up(j0 + step, ahead, next);
+        ahead = entry(j0 + 2 * step);
         if (GROUP != 32 && clustered) cg::this_cluster().sync();
         else meet();
         Held<D> h1;
@@ -334,6 +402,12 @@ __global__ void k_left(const __grid_constant__ MoveBatch b) {
 template <int D>
 cudaError_t launch(const MoveBatch& b, int64_t most, bool in_place, int num_sms, cudaStream_t st) {
     const int units = 2 * b.n_layers * b.n_kv_heads;
+    if (most <= 32) {
+        int C = 1;
+        while (C < most) C *= 2;
+        k_move_few<D><<<dim3((units * C + 255) / 256, 1, b.n), 256, 0, st>>>(b, C);
+        return cudaGetLastError();
+    }
     if (!in_place || most <= 64) {
         // warps of a list: as many as fill the GPU, a step's rows each at least
         int64_t warps = 1;
@@ -365,24 +439,35 @@ cudaError_t launch(const MoveBatch& b, int64_t most, bool in_place, int num_sms,
     return cudaLaunchKernelEx(&config, k_move<D, 256>, b, blocks, 1);
 }
 
-template <int C>
-cudaError_t launch_rank_by(const RankBatch& b, int64_t most, cudaStream_t st) {
-    const cudaError_t e = cudaFuncSetAttribute(k_rank<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRankKeys * 4);
+template <int C, bool HELD>
+cudaError_t launch_rank_by(const RankBatch& b, int64_t slice, cudaStream_t st) {
+    static std::atomic<bool> set[64];     // (the attribute belongs to the device's function)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    const int64_t slice = (most + C - 1) / C + 4;
+    if (dev >= 64 || !set[dev]) {
+        e = cudaFuncSetAttribute(k_rank<C, HELD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRankKeys * 4);
+        if (e != cudaSuccess) return e;
+        if (dev < 64) set[dev] = true;
+    }
     const uint32_t held = (uint32_t)(slice < kRankKeys ? slice : kRankKeys);
+    const dim3 grid(b.n_layers * b.n_kv_heads * C, b.n);
+    if (C == 1) {
+        k_rank<C, HELD><<<grid, kRankThreads, held * 4, st>>>(b, held);
+        return cudaGetLastError();
+    }
     cudaLaunchAttribute cluster;
     cluster.id = cudaLaunchAttributeClusterDimension;
     cluster.val.clusterDim.x = C;
     cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
     cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(b.n_layers * b.n_kv_heads * C, b.n);
+    config.gridDim = grid;
     config.blockDim = dim3(kRankThreads);
     config.dynamicSmemBytes = held * 4;
     config.stream = st;
     config.attrs = &cluster;
     config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, k_rank<C>, b, held);
+    return cudaLaunchKernelEx(&config, k_rank<C, HELD>, b, held);
 }
 
 }  // namespace
@@ -394,8 +479,10 @@ cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms) {
     const int64_t lists = (int64_t)b.n * b.n_layers * b.n_kv_heads;
     int c = 1;
     while (c < kRankCluster && (most > (int64_t)c * kRankKeys || (2 * lists * c <= num_sms && most > 2048 * c))) c *= 2;
-    return c == 1 ? launch_rank_by<1>(b, most, st) : c == 2 ? launch_rank_by<2>(b, most, st)
-         : c == 4 ? launch_rank_by<4>(b, most, st) : launch_rank_by<8>(b, most, st);
+    const int64_t slice = (most + c - 1) / c + 4;
+    if (slice > kRankKeys) return launch_rank_by<kRankCluster, false>(b, slice, st);       // (c is that)
+    return c == 1 ? launch_rank_by<1, true>(b, slice, st) : c == 2 ? launch_rank_by<2, true>(b, slice, st)
+         : c == 4 ? launch_rank_by<4, true>(b, slice, st) : launch_rank_by<8, true>(b, slice, st);
 }
 
 cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int num_sms) {
