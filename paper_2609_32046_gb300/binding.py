@@ -482,6 +482,14 @@ def _each(x, n: int, what: str) -> list:
     return [x] * n
 
 
+def _as_many(n: int, *lists) -> bool:
+    """Every list that is given has n entries (a tensor's length is asked of its shape: it takes a quarter of the time)."""
+    for x in lists:
+        if x is not None and (x.shape[0] if hasattr(x, "shape") else len(x)) != n:
+            return False
+    return True
+
+
 def _address(x) -> int:
     return 0 if x is None else x.data_ptr()
 
@@ -726,7 +734,7 @@ class CacheBack:
         n = len(caches)
         if trees is not None:
             _require(causal and not window, "trees go with causal and no window")
-            _require(len(trees) == n, "one tree (or None) per cache")
+            _require(_as_many(n, trees), "one tree (or None) per cache")
         cfg, like = self.cfg, self._shape
         for p in caches:
             if p._shape != like:
@@ -798,11 +806,12 @@ class CacheBack:
         Returns outs."""
         n = len(caches)
         cfg, like = self.cfg, self._shape
-        _require(len(Qs) == len(lses) == n and (weights is None or len(weights) == n) and (outs is None or len(outs) == n) and
-                 (trees is None or len(trees) == n), "one entry per cache in every list")
-        _require(weights is not None or outs is not None, "weights or outs")
-        _require(not window or causal, "a window goes with causal")
-        _require(trees is None or (causal and not window), "trees go with causal and no window")
+        if not _as_many(n, Qs, lses, weights, outs, trees):
+            raise ValueError("one entry per cache in every list")
+        if weights is None and outs is None:
+            raise ValueError("weights or outs")
+        if (window and not causal) or (trees is not None and (window or not causal)):
+            raise ValueError("a window goes with causal, trees go with causal and no window")
         to = weights if outs is None else outs
         most = 0
         for p in caches:
@@ -869,9 +878,10 @@ class CacheBack:
         the receiving cache's own `length`, where it has one, and its T becomes min(T, keep) where it has none.
         Evict all layers in one call, or give lengths of their own to all calls but the last.  Returns idx."""
         n = len(caches)
-        _require(len(weights) == n and all(x is None or len(x) == n for x in (into, weights_into, idx, lengths)),
-                 "one entry per cache in every list")
-        _require(into is not None or weights_into is None, "weights move where the rows do")
+        if not _as_many(n, weights, into, weights_into, idx, lengths):
+            raise ValueError("one entry per cache in every list")
+        if into is None and weights_into is not None:
+            raise ValueError("weights move where the rows do")
         like, targets = self._shape, caches if into is None else into
         keep = [int(k) for k in _each(keep, n, "keep")]
         if idx is None:
@@ -887,11 +897,12 @@ class CacheBack:
         if many[1]:
             out, out_step, ts = self._weights(weights_into, layers, min(max(keep, default=0), most))
         if many[2]:
-            k = idx.shape[-1]
-            if not (_is_int32(idx) and tuple(idx.shape[1:3]) == (layers, like[1]) and all(x == k for x in keep) and
-                    (n == 0 or idx[0].is_contiguous())):
-                raise ValueError("idx is int32 [sequences][layers][Hkv][keep]")
-            at, at_step = idx.data_ptr(), 4 * idx.stride(0)
+            shape, st = idx.shape, idx.stride()
+            k = shape[-1]
+            if not (_is_int32(idx) and len(shape) == 4 and shape[1] == layers and shape[2] == like[1] and keep.count(k) == n and
+                    (k < 2 or st[3] == 1) and (shape[2] < 2 or st[2] == k) and (layers < 2 or st[1] == k * shape[2])):
+                raise ValueError("idx is int32 [sequences][layers][Hkv][keep], contiguous in each sequence")
+            at, at_step = idx.data_ptr(), 4 * st[0]
         fields, left = array("q"), []         # of the header's cb_eviction, eight bytes each
         first, last = int(first), int(last)
         for i in range(n):
@@ -916,7 +927,8 @@ class CacheBack:
                 _require(p.length is None, "a length on the device needs one that receives the rows kept")
                 length = 0
             else:
-                _require(own.numel() == 1 and _is_int32(own), "a length is one int32")
+                if own.numel() != 1 or not _is_int32(own):
+                    raise ValueError("a length is one int32")
                 length = own.data_ptr()
             left.append(length)
             fields.extend((w + i * w_step, out + i * out_step, ws[0], ws[1], ts[0], ts[1], k, first, last, at + i * at_step, length))
@@ -934,7 +946,7 @@ class CacheBack:
         """fp32 [layers][Hkv][rows or more], or one such a sequence in a tensor: its address, the bytes to the next sequence's, and
         the strides of layers and heads."""
         shape, st = x.shape, x.stride()
-        if not (_is_f32(x) and len(shape) in (3, 4) and tuple(shape[-3:-1]) == (layers, self._shape[1]) and shape[-1] >= rows and
+        if not (_is_f32(x) and 3 <= len(shape) <= 4 and shape[-3] == layers and shape[-2] == self._shape[1] and shape[-1] >= rows and
                 (st[-1] == 1 or shape[-1] == 1)):
             raise ValueError("weights are fp32 [layers][Hkv][rows]")
         return x.data_ptr(), 4 * st[0] if len(shape) == 4 else 0, st[-3:-1]
@@ -949,7 +961,8 @@ class CacheBack:
         it where it has none (counts then are None too).  idx, counts and weights may be tensors with the sequences in their first
         dimension."""
         n = len(caches)
-        _require(len(idx) == n and all(x is None or len(x) == n for x in (counts, weights, lengths)), "one entry per cache in every list")
+        if not _as_many(n, idx, counts, weights, lengths):
+            raise ValueError("one entry per cache in every list")
         drafted = _each(drafted, n, "drafted")
         like, left = self._shape, []
         many = hasattr(idx, "data_ptr"), hasattr(counts, "data_ptr"), hasattr(weights, "data_ptr")      # one tensor each
@@ -988,7 +1001,8 @@ class CacheBack:
                 left.append(rows)
                 to = 0
             else:
-                _require(own.numel() == 1 and _is_int32(own), "a length is one int32")
+                if own.numel() != 1 or not _is_int32(own):
+                    raise ValueError("a length is one int32")
                 left.append(None)
                 to = own.data_ptr()
             fields.extend((at + i * step, rows, count + i * count_step, drafted[i], w + i * w_step, ws[0], ws[1], to))
