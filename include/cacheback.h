@@ -293,7 +293,7 @@ cb_status cb_stage_times(cb_ctx *ctx, float *ms, int32_t *calls);
  *                     and hangs nothing.  The mma.sync passes have no waits and ignore it.
  *                     2: the same for the next cb_attend that runs the tcgen05 kernel (its block 0's
  *                     MMA issuer); calls on the kernel of few rows, which has no waits, leave it set
- *                     3: the same for the next cb_weigh that runs its tcgen05 kernel
+ *                     4: the same for the next cb_weigh that runs its tcgen05 kernel
  * Errors: CB_EINVAL (NULL ctx, values out of range).  Host-only; affects later calls.
  */
 cb_status cb_set_wait_limit(cb_ctx *ctx, int64_t limit_ns, int32_t stall_next);

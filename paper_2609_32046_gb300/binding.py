@@ -1037,7 +1037,7 @@ class CacheBack:
         wait run out (failure-detection test)."""
         stalls = (stall_next_score, stall_next_attend, stall_next_weigh)
         _require(sum(map(bool, stalls)) <= 1, "one stall at a time")
-        self._check(self.lib.cb_set_wait_limit(self.h, int(limit_ns), sum(i + 1 for i, x in enumerate(stalls) if x)))
+        self._check(self.lib.cb_set_wait_limit(self.h, int(limit_ns), sum(k for k, x in zip((1, 2, 4), stalls) if x)))
 
     def set_score_sms(self, n_sms: int = 0):
         """cb_set_score_sms: SMs the persistent score kernels occupy (0: all)."""

@@ -578,11 +578,11 @@ cb_status cb_set_wait_limit(cb_ctx* ctx, int64_t limit_ns, int32_t stall_next) {
     ctx->last_error.clear();
     if (limit_ns != 0 && (limit_ns < 1000 || limit_ns > 60000000000ll))
         return fail(ctx, CB_EINVAL, "limit_ns = %lld: 0 (the default, 1 s) or 1e3 .. 6e10", (long long)limit_ns);
-    if (stall_next < 0 || stall_next > 3) return fail(ctx, CB_EINVAL, "stall_next must be 0, 1, 2 or 3");
+    if (stall_next < 0 || stall_next > 4 || stall_next == 3) return fail(ctx, CB_EINVAL, "stall_next must be 0, 1, 2 or 4");
     ctx->wait_ns = limit_ns ? limit_ns : kDefaultWaitNs;
     ctx->stall_next = stall_next == 1;
     ctx->stall_attend = stall_next == 2;
-    ctx->stall_weigh = stall_next == 3;
+    ctx->stall_weigh = stall_next == 4;
     return CB_OK;
 }
 

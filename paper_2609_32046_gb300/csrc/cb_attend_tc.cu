@@ -5,7 +5,7 @@
 //   0..7    softmax, four a stream (TMEM lane quarter = warp % 4): a thread is a query row
 //   8..11   K: four-bit rows from global memory, as bf16 into shared memory (K-major, 128-byte swizzle)
 //   12..15  V: the same, transposed, as fp16
-//   16      issues tcgen05.mma; 17 finds the next segment, 18 what the join has to (19 fills the warp group)
+//   16      issues tcgen05.mma; 17 finds the segments, one ahead, 18 what the join has to (19 fills the warp group)
 // Two streams alternate on the tensor core, so that one's softmax runs beside the other's products: with
 // more than 128 rows a stream is a half of the rows and both take every tile; with fewer the streams take
 // alternate tiles of the same rows, each with its own maximum and sums, and join at the end.
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
     constexpr int kOp = kTile * D * 2;              // bytes of an operand tile
     constexpr bool kOver = D == 128;                // P in S's columns
     extern __shared__ uint8_t raw[];
-    __shared__ Segment seg;
+    __shared__ Segment segs[2];             // the segment, and the next
     Ctl* ctl = reinterpret_cast<Ctl*>(raw);
     int* pre = reinterpret_cast<int*>(raw + 1024);
     uint8_t* sq = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + kCtlBytes + 1023) & ~uintptr_t(1023));
@@ -291,18 +291,30 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
     // Every role walks the run's segments by itself, in a branch of its own, whose registers are its own; all of
     // the block meets at a segment's beginning (the segment, then Q, are in shared memory) and end.
     const int log2g = b.G >> 1;                     // (G is 1, 2 or 4)
+    int nth = -1;                                   // of the segment
     auto begin = [&]() {
         if (ctl->unit >= ctl->run1 || *reinterpret_cast<volatile int*>(&ctl->abort)) return false;
+        ++nth;
         __syncthreads();
+        const Segment& seg = segs[nth & 1];
         const AttendSeq& s = b.s[seg.seq];
-        // Q: row 128 h + r of the segment, zeros behind the last
-        for (int e = threadIdx.x; e < 2 * kTile * (D / 8); e += kThreadsAt) {
-            const int r = e / (D / 8), c = e % (D / 8), row = seg.row0 + r;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (r < seg.rows)
-                v = __ldg(reinterpret_cast<const uint4*>(s.q + (int64_t)(row >> log2g) * s.s_tok +
-                                                         (int64_t)((seg.g << log2g) + (row & (b.G - 1))) * s.s_head + c * 8));
-            *reinterpret_cast<uint4*>(sq + (r / kTile) * kOp + piece(c / 8, kTile, r % kTile, c % 8)) = v;
+        // Q: row 128 h + r of the segment, zeros behind the last, and no second stream's where it has the first one's rows.
+        // All of a thread's pieces are on their way before the first is written.
+        constexpr int kPieces = (2 * kTile * (D / 8) + kThreadsAt - 1) / kThreadsAt;
+        uint4 v[kPieces];
+        const int pieces = (seg.rows > kTile ? 2 : 1) * kTile * (D / 8);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int e = threadIdx.x + i * kThreadsAt, r = e / (D / 8), c = e % (D / 8), row = seg.row0 + r;
+            v[i] = make_uint4(0, 0, 0, 0);
+            if (e < pieces && r < seg.rows)
+                v[i] = __ldg(reinterpret_cast<const uint4*>(s.q + (int64_t)(row >> log2g) * s.s_tok +
+                                                            (int64_t)((seg.g << log2g) + (row & (b.G - 1))) * s.s_head + c * 8));
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int e = threadIdx.x + i * kThreadsAt, r = e / (D / 8), c = e % (D / 8);
+            if (e < pieces) *reinterpret_cast<uint4*>(sq + (r / kTile) * kOp + piece(c / 8, kTile, r % kTile, c % 8)) = v[i];
         }
         fence_async_smem();
         __syncthreads();
@@ -317,13 +329,14 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
             ctl->tiles += n_tiles;
             ctl->items[0] += (items + 1) / 2;
             ctl->items[1] += items / 2;
-            ctl->unit += seg.n;
+            ctl->unit += segs[nth & 1].n;
             ++ctl->segment;
         }
         __syncthreads();
     };
     // A stream is a half of the rows, not every other tile; tiles; items (item i: stream i % 2, tile i / 2 or i).
 #define SEGMENT()                                             \
+    const Segment& seg = segs[nth & 1];                       \
     const bool both = seg.rows > kTile;                       \
     const int n_tiles = (seg.len + kTile - 1) / kTile;        \
     const int items = both ? 2 * n_tiles : n_tiles
@@ -333,12 +346,19 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
         regs_down<kRegsIssue>();
         if (threadIdx.x == 18 * 32) b.cuts[blockIdx.x] = cut_of(b, pre, blockIdx.x, gridDim.x);
         __syncwarp();
-        while (true) {
-            if (threadIdx.x == 17 * 32 && ctl->unit < ctl->run1)
-                attend_segment(b, pre, b.n_kv_heads, 0, ctl->unit, ctl->run1, D, kRowTile, &seg);
+        // (the next segment while the first tiles of this one are on their way: one thread takes microseconds for it)
+        int found = 0;
+        auto find = [&](int unit) {
+            if (threadIdx.x == 17 * 32 && unit < ctl->run1)
+                attend_segment(b, pre, b.n_kv_heads, 0, unit, ctl->run1, D, kRowTile, &segs[found & 1]);
+            ++found;
             __syncwarp();
+        };
+        find(ctl->unit);
+        while (true) {
             if (!begin()) break;
             SEGMENT();
+            find(ctl->unit + seg.n);
             if (warp == 16 && elect_one()) {
                 const uint32_t hi = (uint32_t)(smem_desc_sw128(0) >> 32), lo = (uint32_t)smem_desc_sw128(0);
                 const uint32_t q0 = (smem_u32(sq) >> 4) + lo, k0 = (smem_u32(sk) >> 4) + lo, v0 = (smem_u32(sv) >> 4) + lo;
