@@ -31,28 +31,16 @@ __device__ __forceinline__ uint32_t rank_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Sum over the block of a value a thread, and (before) those of the threads before this one.
-__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t& before, uint32_t* sh) {
+// Sum over the warps before this one of a number each warp has, and over all.
+__device__ __forceinline__ uint32_t warps_before(uint32_t mine, uint32_t& all, uint32_t* sh) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t x = v;
-#pragma unroll
-    for (int k = 1; k < 32; k *= 2) {
-        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, k);
-        if (lane >= k) x += y;
-    }
-    if (lane == 31) sh[warp] = x;
+    if (lane == 0) sh[warp] = mine;
     __syncthreads();
-    uint32_t w = sh[lane];                               // (as many warps as lanes)
-    const uint32_t own = w;
-#pragma unroll
-    for (int k = 1; k < 32; k *= 2) {
-        const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, w, k);
-        if (lane >= k) w += y;
-    }
-    const uint32_t all = __shfl_sync(0xFFFFFFFFu, w, 31), mine = __shfl_sync(0xFFFFFFFFu, w - own, warp);
+    const uint32_t w = sh[lane];                         // (as many warps as lanes)
+    all = __reduce_add_sync(0xFFFFFFFFu, w);
+    const uint32_t before = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w : 0u);
     __syncthreads();
-    before = mine + x - v;
-    return all;
+    return before;
 }
 static_assert(kRankWarps == 32 && kBins == 2 * kRankThreads, "");
 
@@ -130,21 +118,34 @@ __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ R
                 if (own[i]) atomicAdd(joined + i, own[i]);
             cluster.sync();
         }
-        // bins from the top: thread t has bins 2 (1023 - t) + 1 and 2 (1023 - t)
+        // bins from the top: warp w has 64 of them, its lanes two each, bin0 + 1 and bin0
         const int bin0 = kBins - 2 - 2 * threadIdx.x;
         const uint32_t c0 = joined[bin0 + 1], c1 = joined[bin0];
-        uint32_t before;
-        block_scan(c0 + c1, before, scan);
-        if (before < need && need <= before + c0 + c1) {
-            const bool upper = need <= before + c0;
-            found[0] = bin0 + upper;
-            found[1] = upper ? before : before + c0;
-            found[2] = upper ? c0 : c1;
+        uint32_t total;
+        const uint32_t here = __reduce_add_sync(0xFFFFFFFFu, c0 + c1);
+        uint32_t before = warps_before(here, total, scan);
+        if (before < need && need <= before + here) {            // the warp where the budget runs out
+            uint32_t x = c0 + c1;
+#pragma unroll
+            for (int k = 1; k < 32; k *= 2) {
+                const uint32_t y = __shfl_up_sync(0xFFFFFFFFu, x, k);
+                if (lane >= k) x += y;
+            }
+            before += x - c0 - c1;
+            if (before < need && need <= before + c0 + c1) {
+                const bool upper = need <= before + c0;
+                found[0] = bin0 + upper;
+                found[1] = upper ? before : before + c0;
+                found[2] = upper ? c0 : c1;
+            }
         }
         __syncthreads();
         const uint32_t bin = found[0];
-        uint32_t nothing;
-        above += block_scan(((uint32_t)bin0 + 1 > bin ? own[bin0 + 1] : 0) + ((uint32_t)bin0 > bin ? own[bin0] : 0), nothing, scan);
+        if (C > 1) {
+            warps_before(__reduce_add_sync(0xFFFFFFFFu, ((uint32_t)bin0 + 1 > bin ? own[bin0 + 1] : 0) + ((uint32_t)bin0 > bin ? own[bin0] : 0)),
+                         total, scan);
+            above += total;
+        }
         equal = own[bin];
         need -= found[1];
         prefix = prefix << bits | bin;
@@ -169,18 +170,15 @@ __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ R
     }
     // every warp a run of the keys: counted, then written
     const uint32_t run = ((len + kRankWarps - 1) / kRankWarps + 31) & ~31u, from = min(len, warp * run), to = min(len, from + run);
-    uint32_t n_above = 0, n_equal = 0;
+    uint32_t n_above = 0, n_equal = 0, total;
 #pragma unroll 4
-    for (uint32_t i = from; i < to; i += 32) {
-        const uint32_t x = i + lane < to ? key(i + lane) >> shift : 0;
-        n_above += __popc(__ballot_sync(0xFFFFFFFFu, i + lane < to && x > prefix));
-        n_equal += __popc(__ballot_sync(0xFFFFFFFFu, i + lane < to && x == prefix));
+    for (uint32_t i = from + lane; i < to; i += 32) {
+        const uint32_t x = key(i) >> shift;
+        n_above += x > prefix;
+        n_equal += x == prefix;
     }
-    uint32_t before;
-    block_scan(lane ? 0 : n_above, before, scan);
-    above0 += __shfl_sync(0xFFFFFFFFu, before, 0);
-    block_scan(lane ? 0 : n_equal, before, scan);
-    equal0 += __shfl_sync(0xFFFFFFFFu, before, 0);
+    above0 += warps_before(__reduce_add_sync(0xFFFFFFFFu, n_above), total, scan);
+    equal0 += warps_before(__reduce_add_sync(0xFFFFFFFFu, n_equal), total, scan);
     const uint32_t below = (1u << lane) - 1;
 #pragma unroll 4
     for (uint32_t i = from; i < to; i += 32) {
@@ -298,6 +296,57 @@ __global__ void __launch_bounds__(256) k_move_few(const __grid_constant__ MoveBa
     }
 }
 
+// Rows into another cache: nothing that is read is written, so a warp takes 32 entries by itself, four (two) lanes a row.
+// (Blocks in the order of entries within a list: neighbours' places are neighbours.)
+template <int D>
+__global__ void __launch_bounds__(256) k_move_into(const __grid_constant__ MoveBatch b, int blocks) {
+    constexpr int P = D / 32;                 // pieces of a row's codes, and rows of a lane
+    const MoveSeq& s = b.s[blockIdx.z];
+    const int unit = blockIdx.x / blocks, kv = unit & 1, list = unit >> 1, l = list / b.n_kv_heads, g = list % b.n_kv_heads;
+    const int lane = threadIdx.x & 31, p = lane % P;
+    const int64_t j0 = (int64_t)(blockIdx.x % blocks) * 256 + (threadIdx.x & ~31);
+    const Moving m(b, s, blockIdx.x == 0 && threadIdx.x == 0);
+    if (j0 >= m.count) return;
+    const int32_t* idx = s.idx + list * s.idx_list;
+    // the lane's own entry looked up, then handed to those that move its row
+    const int64_t j = j0 + lane;
+    const int64_t i = j < m.count ? (int64_t)idx[j] : -1;
+    uint2 mine = make_uint2(0, 0);
+    const bool moves = j < m.count && m.rows(b, s, j, i, mine);
+    const int64_t from0 = l * s.from.s_layer + g * s.from.s_head, to0 = l * s.to.s_layer + g * s.to.s_head;
+    const uint8_t* code = s.from.code[kv] + from0 * (D / 2) + p * 16;
+    uint8_t* code_to = s.to.code[kv] + to0 * (D / 2) + p * 16;
+    const uint32_t all = __ballot_sync(0xFFFFFFFFu, moves);
+    uint4 x[P];
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        const int r = lane / P + k * (32 / P);
+        const uint32_t row = __shfl_sync(0xFFFFFFFFu, mine.x, r);
+        if (all >> r & 1u) x[k] = ld16(code + (uint64_t)row * (D / 2));
+    }
+    uint2 scale = make_uint2(0, 0);
+    uint32_t weight = 0;
+    const bool weigh = kv == 0 && s.w && moves;
+    if (moves) {
+        const uint8_t* from = reinterpret_cast<const uint8_t*>(s.from.scale[kv]) + (from0 + mine.x) * (D / 16);
+        if (D == 128) scale = ld8(from);
+        else scale.x = ld4(from);
+    }
+    if (weigh) weight = ld4(s.w + l * s.w_layer + g * s.w_head + m.base + i);
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        const int r = lane / P + k * (32 / P);
+        const uint32_t row = __shfl_sync(0xFFFFFFFFu, mine.y, r);
+        if (all >> r & 1u) *reinterpret_cast<uint4*>(code_to + (uint64_t)row * (D / 2)) = x[k];
+    }
+    if (moves) {
+        uint8_t* to = reinterpret_cast<uint8_t*>(s.to.scale[kv]) + (to0 + mine.y) * (D / 16);
+        if (D == 128) *reinterpret_cast<uint2*>(to) = scale;
+        else *reinterpret_cast<uint32_t*>(to) = scale.x;
+    }
+    if (weigh) reinterpret_cast<uint32_t*>(s.w_to)[l * s.t_layer + g * s.t_head + m.base + j] = weight;
+}
+
 // A group of threads moves the rows of K or of V of one list, a row a thread a step: GROUP = 32, a warp; else a block, or
 // the blocks of a cluster together.  In place a row's source is never before its place, so what a step writes is
 // read by no later one; within a step every group reads before any writes (a barrier), and the next step's rows are on
@@ -408,15 +457,13 @@ cudaError_t launch(const MoveBatch& b, int64_t most, bool in_place, int num_sms,
         k_move_few<D><<<dim3((units * C + 255) / 256, 1, b.n), 256, 0, st>>>(b, C);
         return cudaGetLastError();
     }
-    if (!in_place || most <= 64) {
-        // warps of a list: as many as fill the GPU, a step's rows each at least
-        int64_t warps = 1;
-        if (!in_place) {
-            warps = 48 * (int64_t)num_sms / ((int64_t)units * b.n);
-            if (warps > (most + 31) / 32) warps = (most + 31) / 32;
-            if (warps < 1) warps = 1;
-        }
-        k_move<D, 32><<<dim3((unsigned)((units * warps + 7) / 8), 1, b.n), 256, 0, st>>>(b, (int)warps, 0);
+    if (!in_place) {
+        const int blocks = (int)((most + 255) / 256);
+        k_move_into<D><<<dim3((unsigned)(units * blocks), 1, b.n), 256, 0, st>>>(b, blocks);
+        return cudaGetLastError();
+    }
+    if (most <= 64) {
+        k_move<D, 32><<<dim3((units + 7) / 8, 1, b.n), 256, 0, st>>>(b, 1, 0);
         return cudaGetLastError();
     }
     // blocks of a list: as many as fill the GPU, a step's rows each at least
