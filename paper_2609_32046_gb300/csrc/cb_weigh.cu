@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kStages = 2;
+constexpr int kBlocksPerSm = 5;          // (48 sequences' weights: 4 blocks 55 us, 5 53, 6 54.4, 7 64)
 
 // Copies 32 positions' keys; mine: the row of this lane's.  The codes of a position that has none are some row's: its
 // scales are zeros.
@@ -57,7 +58,7 @@ __device__ __forceinline__ bool look_over_keys(uint8_t* stage, uint32_t* err) {
 // copies.  S^T [16 positions][8 rows] = K Q^T (cb_few.cuh), the rows' weights are added up over a quad's lanes, and
 // every position's sum is written by one lane.
 template <int D, int NT>
-__global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_constant__ WeighBatch b) {
+__global__ void __launch_bounds__(kWarps * 32, kBlocksPerSm) k_weigh_few(const __grid_constant__ WeighBatch b) {
     using S = Stage<D, 1>;
     __shared__ __align__(128) uint8_t smem[kWarps * kStages * S::kBytes];
     __shared__ int pre[kMaxBatch + 1];
@@ -75,11 +76,19 @@ __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_const
         __syncthreads();
         const WeighSeq& w = b.w[x.seq];
         const WeighRows rows(b, x);
+        // positions before `low` no token sees; those before `all_to` and from `all_from` on not every one does
+        const bool windowed = rows.causal && rows.window && !rows.tree;
+        const int low = windowed ? max(0, rows.at - rows.window + 1) : 0, len = x.len;
+        const int all_to = windowed ? rows.at + rows.m - rows.window : 0;
+        const int all_from = rows.tree ? rows.at : rows.causal ? rows.at + 1 : len;
+        float* to_w = w.weights + (int64_t)g * w.w_head + x.begin;
+        const float* from_w = w.before + (int64_t)g * w.b_head + x.begin;
+        const int had = w.before ? min(len, rows.fresh) : 0;
         int t0 = warp * kStep, ahead = t0;
         uint32_t page = segment_page(x, ahead + lane);
 #pragma unroll
         for (int i = 0; i < kStages; ++i) {
-            if (ahead < x.len && !rows.blind(ahead, kStep)) copy_keys<D>(to + i * S::kBytes, x, segment_row(x, ahead + lane, page, b.err));
+            if (ahead < len && ahead + kStep > low) copy_keys<D>(to + i * S::kBytes, x, segment_row(x, ahead + lane, page, b.err));
             copy_commit();
             ahead += kWarps * kStep;
             page = segment_page(x, ahead + lane);
@@ -95,15 +104,15 @@ __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_const
                 const float lse = row < x.rows ? rows.lse(w, g, row) : INFINITY;
                 nl[nt][h] = isfinite(lse) ? lse * -1.4426950408889634f : -INFINITY;
             }
-        for (int turn = 0; t0 < x.len; t0 += kWarps * kStep) {
+        for (int turn = 0; t0 < len; t0 += kWarps * kStep) {
             uint8_t* st = stages + turn * S::kBytes;
             const int own = t0 + 8 * tig + place(gid);          // the position whose sum this lane writes
-            const float before = rows.before(w, g, own);
+            const float before = own < had ? from_w[own] : 0.f;
             copy_wait<kStages - 1>();
             __syncwarp();
             float s[4] = {};                                    // of positions t0 + 8 k + place(gid)
-            if (!rows.blind(t0, kStep)) {
-                const bool near = look_over_keys<D>(st, b.err), edge = rows.edge(t0, kStep);
+            if (t0 + kStep > low) {
+                const bool near = look_over_keys<D>(st, b.err), edge = t0 + kStep > min(len, all_from) || t0 < all_to;
                 float z[2][NT][4];
                 if (near) {
                     score_keys<D, NT, true, 1>(st, 0, q, z[0]);
@@ -136,9 +145,9 @@ __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_const
                 s[k] += __shfl_xor_sync(0xFFFFFFFFu, s[k], 2);
             }
             const float sum = tig == 0 ? s[0] : tig == 1 ? s[1] : tig == 2 ? s[2] : s[3];
-            if (own < x.len) w.weights[(int64_t)g * w.w_head + x.begin + own] = fmaf(b.decay, before, sum);
+            if (own < len) to_w[own] = fmaf(b.decay, before, sum);
             __syncwarp();
-            if (ahead < x.len && !rows.blind(ahead, kStep)) copy_keys<D>(to + turn * S::kBytes, x, segment_row(x, ahead + lane, page, b.err));
+            if (ahead < len && ahead + kStep > low) copy_keys<D>(to + turn * S::kBytes, x, segment_row(x, ahead + lane, page, b.err));
             copy_commit();
             ahead += kWarps * kStep;
             page = segment_page(x, ahead + lane);
@@ -152,7 +161,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) k_weigh_few(const __grid_const
 
 template <int D, int NT>
 cudaError_t launch_few(const WeighBatch& b, int64_t units, int num_sms, cudaStream_t st) {
-    const int64_t most = num_sms * 4 / b.n_kv_heads, all = units / b.n_kv_heads;
+    const int64_t most = num_sms * kBlocksPerSm / b.n_kv_heads, all = units / b.n_kv_heads;
     const int64_t runs = all < most ? all : most;
     k_weigh_few<D, NT><<<(int)(runs > 1 ? runs : 1) * b.n_kv_heads, kWarps * 32, 0, st>>>(b);
     return cudaGetLastError();

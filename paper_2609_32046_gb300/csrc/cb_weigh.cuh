@@ -28,16 +28,6 @@ struct WeighRows {
         fresh = (int)(x.at + m - b.w[x.seq].fresh);
     }
 
-    // No token sees any of the n positions from t0 on.  (Token 0's window begins first.)
-    __device__ __forceinline__ bool blind(int t0, int n) const {
-        return !tree && causal && window && t0 + n - 1 <= at - window;
-    }
-    // Some token does not see all of them.
-    __device__ __forceinline__ bool edge(int t0, int n) const {
-        if (t0 + n > len) return true;
-        if (tree) return t0 + n > at;
-        return causal && (t0 + n - 1 > at || (window && t0 <= at + m - 1 - window));
-    }
     // Of the 32 positions from t0 on, those that a token sees, as bits.  (Tokens behind the last: some.)
     __device__ __forceinline__ uint32_t seen(const WeighSeq& w, int token, int t0) const {
         int lo = t0, hi = len;                              // positions [lo, hi)
