@@ -578,7 +578,8 @@ typedef struct {
  * over the query heads h of KV head g (h / G = g) and the tokens r that see row t, which is as in cb_attend (causal, window) or, with
  * trees, as in cb_attend_tree.  A token's head whose lse is not finite adds nothing: what saw no row, and
  * what a caller leaves out by setting its lse to infinity (drafts that were not accepted).  Weights of rows
- * from L on are not written.  Sums are fp32, in a fixed order.
+ * from L on are not written.  Sums are fp32, in a fixed order.  No sequence's weights may be another's weights or
+ * before, or overlap anything else that the call reads.
  * m = 0 skips a sequence.
  *   trees   NULL, or one a sequence (then causal = 1 and window = 0)
  *   decay   within 0 .. 1
@@ -612,6 +613,7 @@ typedef struct {
  *   into   NULL: in the cache itself; or the cache that receives the rows, whose T is at least keep or
  *          caches[i].T.  into[i] that names caches[i]'s own codes of K is in place too and has to be its equal;
  *          another's memory may not touch that of any cache of the call
+ * Rows that are written may be no other sequence's (pages that two block tables share, say).
  * A block-table entry outside [0, n_pages) leaves its rows out and is reported by cb_sync_status as CB_EDEVICE.
  * Errors: CB_EINVAL (also a cache or a length that is written twice, a length that is written and another cache's), CB_ESHAPE
  * (layers, T, keep), CB_EBUDGET (first + last above keep, into too small).
@@ -639,7 +641,8 @@ typedef struct {
  * After cb_attend_tree: idx is the accepted path; with drafted = T: the rows that stay of a message.
  * idx[j] has to lie in j .. drafted - 1 (what an ascending list does): an entry that does not, and a
  * block-table entry outside [0, n_pages), skips its row and is reported by cb_sync_status as CB_EDEVICE, as is a
- * cache of fewer than `drafted` rows, of which nothing is moved or written.  The rest of the cache stays as it is.
+ * cache of fewer than `drafted` rows, of which nothing is moved or written.  The rest of the cache stays as it is.  Rows that
+ * are written may be no other sequence's.
  * Errors: CB_EINVAL (also a cache that is given twice, lengths as in cb_evict), CB_ESHAPE, CB_EBUDGET (count not within 0 .. drafted,
  * drafted above T).
  */

@@ -518,6 +518,14 @@ cb_status weigh_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* cac
     }
     if (some.empty()) return CB_OK;
     if (written_twice(written)) return fail(ctx, CB_EINVAL, "two sequences write the same weights");
+    // (sorted by now, or in order) what one sequence writes is not what another reads
+    for (const int32_t i : some) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(queries[i].before);
+        if (!at || queries[i].before == queries[i].weights) continue;
+        const auto x = std::lower_bound(written.begin(), written.end(), at, [](const Written& a, uintptr_t b) { return a.lo < b; });
+        if (x != written.end() && x->lo == at)
+            return fail(ctx, CB_EINVAL, "queries[%d].before is another sequence's weights", i);
+    }
     for (size_t b0 = 0; b0 < some.size(); b0 += kMaxBatch) {
         WeighBatch b;
         std::memset(&b, 0, sizeof b);
@@ -562,12 +570,15 @@ cb_status weigh_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* cac
 struct Places {
     std::vector<Written> codes;
     std::vector<std::pair<uintptr_t, uintptr_t>> paged;     // codes and table of every cache written
+    std::vector<std::pair<uintptr_t, uintptr_t>> read, written;   // the same of those read and of all written, entry by entry
     std::vector<Written> weights, idx;
-    std::vector<uintptr_t> lengths, left;                   // of the caches read, of those left
+    std::vector<uintptr_t> lengths, left;                   // numbers that are read, and lengths that are written
 
-    void add(const cb_packed& p, int d, const cb_config& c) {
-        if (p.T == 0) return;
+    // An entry's rows: from a cache, to a cache.
+    void add(const cb_packed& from, const cb_packed& p, int d, const cb_config& c) {
         const uintptr_t at = reinterpret_cast<uintptr_t>(p.k);
+        read.emplace_back(reinterpret_cast<uintptr_t>(from.k), reinterpret_cast<uintptr_t>(from.pages));
+        written.emplace_back(at, reinterpret_cast<uintptr_t>(p.pages));
         if (p.pages) {
             paged.emplace_back(at, reinterpret_cast<uintptr_t>(p.pages));
             return;
@@ -583,9 +594,17 @@ struct Places {
         std::sort(left.begin(), left.end());
         for (size_t i = 1; i < left.size(); ++i)
             if (left[i] == left[i - 1]) return true;
+        // what one entry writes is not what another reads
+        auto sorted = read;
+        std::sort(sorted.begin(), sorted.end());
+        for (size_t i = 0; i < written.size(); ++i) {
+            const auto all = std::equal_range(sorted.begin(), sorted.end(), written[i]);
+            if (all.second - all.first > (read[i] == written[i] ? 1 : 0)) return true;
+        }
         return written_twice(codes) || written_twice(weights) || written_twice(idx);
     }
-    // A length that is written is also another cache's, which reads it.  `own`: what each cache reads and what it writes.
+    // A length that is written is also another cache's, or a count, which is read.  `own`: the length that each cache has and
+    // the one it writes.
     bool lengths_clash(const std::vector<std::pair<uintptr_t, uintptr_t>>& own) {
         std::sort(lengths.begin(), lengths.end());
         for (const auto& x : own) {
@@ -662,7 +681,7 @@ cb_status evict_impl(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, co
             const uintptr_t w = reinterpret_cast<uintptr_t>(e.weights_to), x = reinterpret_cast<uintptr_t>(e.idx);
             if (w) places.weights.push_back(Written{w, w + 4 * (uintptr_t)span_to, span_to == lists * rows});
             places.idx.push_back(Written{x, x + 4 * (uintptr_t)(lists * e.keep), true});
-            places.add(to, d, c);
+            places.add(p, to, d, c);
         }
         places.lengths.push_back(reinterpret_cast<uintptr_t>(p.length));
         if (e.length) places.left.push_back(reinterpret_cast<uintptr_t>(e.length));
@@ -732,6 +751,7 @@ cb_status keep_impl(cb_ctx* ctx, int32_t n, const cb_packed* caches, const cb_ke
         if (e.length && (st = ptrs.check(e.length, "kept.length", i, 4))) return st;
         if (e.n_kept && (st = ptrs.check(e.n_kept, "kept.n_kept", i, 4))) return st;
         places.lengths.push_back(reinterpret_cast<uintptr_t>(p.length));
+        places.lengths.push_back(reinterpret_cast<uintptr_t>(e.n_kept));
         if (e.length) places.left.push_back(reinterpret_cast<uintptr_t>(e.length));
         lengths.emplace_back(reinterpret_cast<uintptr_t>(p.length), reinterpret_cast<uintptr_t>(e.length));
         MoveSeq m{};
@@ -751,7 +771,7 @@ cb_status keep_impl(cb_ctx* ctx, int32_t n, const cb_packed* caches, const cb_ke
                 const uintptr_t w = reinterpret_cast<uintptr_t>(e.weights);
                 places.weights.push_back(Written{w, w + 4 * (uintptr_t)span, span == (int64_t)c.n_layers * c.n_kv_heads * p.T});
             }
-            places.add(p, d, c);
+            places.add(p, p, d, c);
             m.count = e.count;
             m.from = m.to = packed_rows(p, d);
             m.w = e.weights;

@@ -35,6 +35,7 @@ template <int D> constexpr int kStages = D == 128 ? 2 : 4;    // tiles of query 
 // Tiles of their log-sum-exps, which the sums read: rows are copied up to kStages tiles ahead of the products, and these are
 // up to kBuffers + 1 buffers, of a tile each at most, ahead of the sums.
 constexpr int kLse = 16;
+constexpr int kMostTiles = 1024;              // of a segment (about a millisecond)
 constexpr int kSeldomNs = 200;               // between looks of the warps that nothing waits for at once
 static_assert(kLse >= 4 + kBuffers + 2, "");
 
@@ -633,9 +634,11 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                     attend_segment(b, pre, b.n_kv_heads, 0, unit, end, D, kWeighRows, &part.x);
                     part.q0 = 0;
                     part.q1 = part.x.len ? (part.x.rows + kTile - 1) / kTile : 0;
-                    if (part.q1 > kStages<D> && part.x.n > kTiles) {            // the positions stay: no more than fit
-                        part.x.n = kTiles;
-                        part.x.len = min(part.x.len, kTiles * kTile);
+                    // no more tiles than fit where they stay, nor than pass in a small part of a wait's limit
+                    const int most = part.q1 > kStages<D> ? kTiles : kMostTiles;
+                    if (part.x.n > most) {
+                        part.x.n = most;
+                        part.x.len = min(part.x.len, most * kTile);
                     }
                     const View v(b, part, kStages<D>);
                     auto idle = [&](int q) {

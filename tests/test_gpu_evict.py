@@ -272,7 +272,8 @@ def test_evict_refusals():
             call(**kw)
     i = torch.zeros(2, 2, 50, dtype=torch.int32, device="cuda")
     for kw in (dict(first=30, last=21), dict(first=-1), dict(last=-1), dict(keep=-1), dict(layer=1), dict(into=o.caches),
-               dict(caches=[c.caches[0]] * 2), dict(idx=[i, i]), dict(keep=20, into=[o.caches[0]] * 2),
+               dict(caches=[c.caches[0]] * 2), dict(idx=[i, i]), dict(keep=20, caches=[c.caches[0]] * 2, into=[c.caches[0], o.caches[0]]),
+               dict(keep=20, into=[o.caches[0], c.caches[0]]), dict(keep=20, into=[o.caches[0]] * 2),
                dict(keep=20, into=o.caches, weights_into=w), dict(weights=[w[0], w[0]]),
                dict(weights=[w[0].cpu(), w[1]]), dict(weights=[w[0].as_strided((2, 2, 100), (10, 100, 1)), w[1]])):
         if kw.get("keep") == -1:
@@ -353,7 +354,7 @@ def test_keep_refusals():
         with pytest.raises(ValueError):
             call(**kw)
     for kw in (dict(drafted=4), dict(drafted=101), dict(drafted=-1), dict(caches=[c.caches[0]] * 2), dict(idx=[i.cpu(), i]),
-               dict(lengths=[n, n]), dict(weights=[c.weights[0], c.weights[0]])):
+               dict(lengths=[n, n]), dict(weights=[c.weights[0], c.weights[0]]), dict(counts=[n, n], lengths=[n, n.clone()])):
         with pytest.raises(cb.CBError):
             call(**kw)
     c.rx.sync_status()

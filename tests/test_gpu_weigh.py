@@ -253,6 +253,7 @@ def test_many_query_rows(d, Hq, Hkv, m, T, see):
 
 @pytest.mark.parametrize("m", [150, 600, 1024])
 def test_many_drafts(m):
+    """Trees of more tokens than stay in shared memory."""
     bits = [bits_of("tree", m, 0), None, bits_of("any", m, 2)]
     c = Weighed(128, 4, 1, [m] * 3, [m, 900 + m, 2000], see=dict(trees=[None if x is None else cb.pack_words(x).cuda() for x in bits]))
     c.weigh()
@@ -266,6 +267,25 @@ def test_more_segments_than_blocks(d):
     c = Weighed(d, 16, 8, [9 + 53 * (i % 6) for i in range(n)], [300 + 97 * i for i in range(n)], page=32)
     c.weigh()
     c.check()
+
+
+def test_a_long_cache():
+    """More tiles a block than one segment may have: a row's sum does not depend on the call that it is in."""
+    T = 152 * 1024 * 128 + 5000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    codes = [torch.randint(0, 256, (1, 1, T, 32), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    scales = [torch.rand((1, 1, T, 2), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    q = torch.randn((5, 4, 64), generator=g, device="cuda").to(torch.bfloat16)
+    lse = torch.full((5, 4), 6.0, device="cuda")
+    rx = cb.Receiver(1, 4, 1, 64, 5, T, 2)
+    whole, halves = torch.zeros(1, T, device="cuda"), torch.zeros(1, T, device="cuda")
+    rx.weigh([cb.PackedKV(*codes, *scales)], [q], [lse], None, outs=[whole], causal=False)
+    cut = 7 * 128 * 1000 + 3
+    parts = [cb.PackedKV(*[x[:, :, i] for x in codes + scales]) for i in (slice(0, cut), slice(cut, T))]
+    for p, out in zip(parts, (halves[:, :cut], halves[:, cut:])):
+        rx.weigh([p], [q], [lse], None, outs=[out], causal=False)
+    rx.sync_status()
+    assert torch.equal(whole, halves) and bool((whole > 0).all())
 
 
 @pytest.mark.parametrize("d", [64, 128])
@@ -316,6 +336,9 @@ def test_refusals():
     both = torch.zeros(2, 250, device="cuda")
     with pytest.raises(cb.CBError):
         rx.weigh(c.caches, c.q, c.lse, [both[:, :200], w[1]], outs=[both[:, 20:220], None])        # overlaps `before`
+    spare = torch.zeros_like(w[0])
+    with pytest.raises(cb.CBError):
+        rx.weigh(c.caches, c.q, c.lse, w, outs=[spare, w[0]])                                      # the second writes what the first reads
     rx.sync_status()
     for a, b in zip(c.weights, c.before):
         assert torch.equal(a, b)
