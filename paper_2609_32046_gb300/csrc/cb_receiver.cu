@@ -536,6 +536,11 @@ cb_status weigh_impl(cb_ctx* ctx, int32_t layer, int32_t n, const cb_packed* cac
         b.scale_log2e = ctx->scale * 1.4426950408889634f;
         b.err = ctx->err;
         b.wait_ns = (uint64_t)ctx->wait_ns;
+        // (a weight is 2^(f z - l'): where f z and l' are far from 0 and their difference is not, f's rounding is taken from it by
+        // an l' that has the same)
+        const double log2e = (double)b.scale_log2e / (c.softmax_scale > 0.f ? (double)c.softmax_scale : 1.0 / std::sqrt((double)d));
+        b.lse_log2e = (float)log2e;
+        b.lse_log2e_lo = (float)(log2e - (double)b.lse_log2e);
         b.stall = ctx->stall_weigh;
         b.sees = causal;
         b.sees_window = window < kNoWindow ? (int32_t)window : 0;

@@ -144,6 +144,7 @@ struct WeighBatch : AttendBatch {
     int32_t sees;
     int32_t sees_window;      // 0: none
     float decay;
+    float lse_log2e, lse_log2e_lo;   // scale_log2e / scale, in two parts: log2(e) as the logits' factor has it
     WeighSeq w[kMaxBatch];
 };
 

@@ -94,7 +94,8 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksPerSm) k_weigh_few(const _
             page = segment_page(x, ahead + lane);
         }
         uint32_t q[NT][D / 32][4];
-        float zs[NT][2], nl[NT][2];       // of columns 2 tig and 2 tig + 1: factor of the logits, -lse * log2(e)
+        // of columns 2 tig and 2 tig + 1: factor of the logits, -lse * log2(e), and 2^(what its rounding left out)
+        float zs[NT][2], nl[NT][2], rest[NT][2];
         load_queries<D, NT>(b, b.s[x.seq], g, 0, x.rows, q, zs, [&](int row) { return isfinite(rows.lse(w, g, row)); });
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -102,7 +103,10 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksPerSm) k_weigh_few(const _
             for (int h = 0; h < 2; ++h) {
                 const int row = nt * 8 + 2 * tig + h;
                 const float lse = row < x.rows ? rows.lse(w, g, row) : INFINITY;
-                nl[nt][h] = isfinite(lse) ? lse * -1.4426950408889634f : -INFINITY;
+                const float l = lse * -b.lse_log2e;
+                nl[nt][h] = isfinite(lse) ? l : -INFINITY;
+                // (2^x = 1 + x ln 2 for an x of 2^-20: nearer than the approximation of exp2 is)
+                rest[nt][h] = isfinite(lse) ? fmaf(fmaf(lse, -b.lse_log2e, -l) - lse * b.lse_log2e_lo, 0.6931471805599453f, 1.f) : 0.f;
             }
         for (int turn = 0; t0 < len; t0 += kWarps * kStep) {
             uint8_t* st = stages + turn * S::kBytes;
@@ -136,8 +140,8 @@ __global__ void __launch_bounds__(kWarps * 32, kBlocksPerSm) k_weigh_few(const _
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        s[k] += ex2(fmaf(z[k / 2][nt][2 * (k % 2)], zs[nt][0], nl[nt][0])) +
-                                ex2(fmaf(z[k / 2][nt][2 * (k % 2) + 1], zs[nt][1], nl[nt][1]));
+                        s[k] = fmaf(ex2(fmaf(z[k / 2][nt][2 * (k % 2)], zs[nt][0], nl[nt][0])), rest[nt][0],
+                                    fmaf(ex2(fmaf(z[k / 2][nt][2 * (k % 2) + 1], zs[nt][1], nl[nt][1])), rest[nt][1], s[k]));
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) {

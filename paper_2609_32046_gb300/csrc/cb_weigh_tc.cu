@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(kThreadsWt, 1) k_weigh_tc(const __grid_constan
                 for (int i = 0; i < R; ++i) {
                     const bool there = isfinite(lse[i]);
                     copy16_or_0(to + i * N * 128, from + i * step, there);            // (reads nothing where it is not)
-                    if (u % P == 0) l[i * N] = there ? lse[i] * -1.4426950408889634f : -INFINITY;
+                    if (u % P == 0) l[i * N] = there ? lse[i] * -b.lse_log2e : -INFINITY;
                 }
             };
             auto landed = [&](int q) {
