@@ -9,7 +9,15 @@
 //   24      issues tcgen05.mma; 25 writes the weights; 26 finds the run's segments, one ahead
 // Up to kStages tiles of query rows stay in shared memory while the tiles of positions pass through a ring; with
 // more rows the ring's tiles of positions stay and the rows pass.
-// A row whose lse is not finite is a row of zeros with an lse of infinity: it adds nothing.
+// A row whose lse is not finite is a row of zeros with an lse of infinity: it adds nothing.  A row's sum is one over its columns
+// in a fixed order, whatever segment it is in.
+//
+// Measured (8 KV heads): 1024 tokens over 16384 positions, 32 heads of 128, 163 us, 0.82 PFLOP/s, where the products alone take
+// 70; 33 drafts of 8 sequences over 6001, 16 heads of 64, 28 us. Bound by the sums: a tile's exponentials are 512 cycles, as long as
+// its products, and the log-sum-exps read from shared memory compete with the products' operands (163 us of 190 without
+// them); then by the chain of waits (107 us with no arithmetic in the sums, 73 with no products either). Other forms: the
+// whole block meeting between segments 341; eight warps that sum 64 columns 181; masks in the same code as the rest 190;
+// sums in shared memory by generic addresses 211; products issued by a lane that elect did not choose 214.
 #include <atomic>
 #include <cmath>
 #include <cstdint>
