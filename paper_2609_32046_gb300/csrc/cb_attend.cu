@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(kWarps * 32, few_blocks<D, NT>()) k_attend_few
         if (!whole) {
             // n parts, from run b0 on, in groups of `size`, about the root of their number.  (Loads that the last
             // block waits for: 76 parts a head joined at once took 11 us of one token's 38 over 65536 positions, in
-            // two steps 6; 16 parts took 0.8 us longer in two.)
+            // two steps 6; 16 parts took 0.8 us longer in two.  Both before join_parts.)
             const int b0 = attend_block(runs, x.first), n = attend_block(runs, x.first + x.units - 1) - b0 + 1;
             int size = 16;
             while (size * size < n) size += 8;
@@ -469,13 +469,13 @@ static cudaError_t launch_by_rows(Batch& b, int head_dim, cudaStream_t st, int n
     rows *= b.G;
     if (rows == 0) return cudaSuccess;
     // Up to 16 rows a KV head (token, head of its group) their sums stay in a warp's registers, above that the tcgen05
-    // kernel takes over.  8 KV heads of 128, 2048 / 16384 positions: 8 rows 12.4 / 21.5 us here and 16.8 / 33.2 us
-    // there, 16 rows 18.2 / 29.2 and 17.1 / 33.6 us.
+    // kernel takes over.  8 KV heads of 128, 2048 / 16384 positions: 8 rows 11.2 / 19.5 us here and 17.8 / 35.0 us
+    // there, 16 rows 15.7 / 24.6 and 18.1 / 35.2 us.
     // The rule goes by the longest of the call's sequences.  What one of many rows costs the others, 47 decoding
     // sequences in pages (4 rows each, 8 KV heads of 128; 86 us by themselves) with one of m tokens, in one call / in
     // two: m = 2 88 / 106 us, 4 111 / 116, 16 240 / 111, 64 288 / 118, 1024 398 / 207.
     if (rows > 16) return launch_attend_tc(b, head_dim, st, num_sms);
-    // (8 rows in a tile of 16: 13.4 / 22.3 us; 4 rows 10.2 / 17.1 in one of 8, 10.8 / 18.4 in one of 16)
+    // (With the join as it was, 8 rows in a tile of 16: 13.4 / 22.3 us; 4 rows 10.2 / 17.1 in one of 8, 10.8 / 18.4 in one of 16.)
     const int tile_rows = rows <= 8 ? 8 : 16;
     const int64_t units = attend_pairs(b, tile_rows);
     if (head_dim == 128)

@@ -18,7 +18,7 @@
 // after the first tiles; until then weights are up to 2^15, in fp16's range.
 //
 // Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 266 us, 1001 TFLOP/s, 253 of it before
-// the join; 64 tokens over 12352 positions 41 us, 34 before it. Bound by the chain of waits of a stream (weights, their
+// the join; 64 tokens over 12352 positions 39 us, 32 before it. Bound by the chain of waits of a stream (weights, their
 // product, the next scores, its maximum), by fetching the roles' code and by the shared memory that the products read.
 // 256 rows a block, because each unpacking of a tile serves all of them.  Other forms, when this one (with a slower
 // join) took 286 to 292 us: 128 rows 367; two warps that issue 335; 16 softmax warps of 72 registers 408; registers not
