@@ -156,12 +156,26 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
             }
         }
     };
+    // (64 at a time where none is looked at: half of the waits. 1024 tokens over 16384 positions 266 -> 257 us; masked tiles in the
+    // same way cost a tree's kernel registers.)
+    if constexpr (EDGE) {
 #pragma unroll 1
-    for (int c = 0; c < kTile; c += 32) {
-        tmem_ld32(ts + c, z);
-        tmem_wait_ld(z);
-        seen(z, c);
-        high = fmaxf(high, max_tree1(z));
+        for (int c = 0; c < kTile; c += 32) {
+            tmem_ld32(ts + c, z);
+            tmem_wait_ld(z);
+            seen(z, c);
+            high = fmaxf(high, max_tree1(z));
+        }
+    } else {
+        float z1[32];
+#pragma unroll 1
+        for (int c = 0; c < kTile; c += 64) {
+            tmem_ld32(ts + c, z);
+            tmem_ld32(ts + c + 32, z1);
+            tmem_wait_ld(z);
+            tmem_wait_ld(z1);
+            high = fmaxf(high, fmaxf(max_tree1(z), max_tree1(z1)));
+        }
     }
     const float top = high * scale;
     const bool grow = top > M + kGrow || (M == -INFINITY && top > -INFINITY);
@@ -199,12 +213,25 @@ __device__ __forceinline__ void softmax_tile(uint32_t ts, uint32_t tp, uint32_t 
         }
         tmem_st16(tp + first / 2, p);
     };
+    if constexpr (EDGE) {
 #pragma unroll 1
-    for (int c = 0; c < kTile; c += 32) {
-        tmem_ld32(ts + c, z);
-        tmem_wait_ld(z);
-        seen(z, c);
-        weigh(z, c);
+        for (int c = 0; c < kTile; c += 32) {
+            tmem_ld32(ts + c, z);
+            tmem_wait_ld(z);
+            seen(z, c);
+            weigh(z, c);
+        }
+    } else {
+        float z1[32];
+#pragma unroll 1
+        for (int c = 0; c < kTile; c += 64) {
+            tmem_ld32(ts + c, z);
+            tmem_ld32(ts + c + 32, z1);
+            tmem_wait_ld(z);
+            tmem_wait_ld(z1);
+            weigh(z, c);
+            weigh(z1, c + 32);
+        }
     }
     float a, e;
     unpack2(fadd2(l0, l1), a, e);
