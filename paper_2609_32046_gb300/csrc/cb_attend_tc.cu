@@ -17,11 +17,12 @@
 // O is scaled in place when a row's maximum has grown by more than 8 (log2 domain) since M was set: seldom
 // after the first tiles; until then weights are up to 2^15, in fp16's range.
 //
-// Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 266 us, 1001 TFLOP/s, 253 of it before
+// Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 254 us, 1048 TFLOP/s, 241 of it before
 // the join; 64 tokens over 12352 positions 39 us, 32 before it. Bound by the chain of waits of a stream (weights, their
 // product, the next scores, its maximum), by fetching the roles' code and by the shared memory that the products read.
-// 256 rows a block, because each unpacking of a tile serves all of them.  Other forms, when this one (with a slower
-// join) took 286 to 292 us: 128 rows 367; two warps that issue 335; 16 softmax warps of 72 registers 408; registers not
+// 256 rows a block, because each unpacking of a tile serves all of them.  Few rows (64 drafts' of 16 tokens): bound by the
+// unpacking warps, 1.5 to 1.9 us a tile, and about 9 us a segment; rows asked for ahead in L2 206 us for 194 (more for those warps to do).
+// Other forms, when this one (with a slower join) took 286 to 292 us: 128 rows 367; two warps that issue 335; 16 softmax warps of 72 registers 408; registers not
 // moved between the roles and 8 + 8 + 1 warps 317; scores in two halves of 64 positions 293 to 299; the products alone,
 // without softmax and unpacking, 249.
 #include <atomic>
@@ -553,7 +554,7 @@ __global__ void __launch_bounds__(kThreadsAt, 1) k_attend_tc(const __grid_consta
                 page = segment_page(seg, t);
                 if (j >= kStages && !wait_warp(&ctl->k_empty[j % kStages], (j / kStages - 1) & 1, ctl, b.err, 5)) break;
                 uint8_t* to = sk + (j % kStages) * kOp + at;
-#pragma unroll 1
+#pragma unroll 2
                 for (int y = 0; y < 4; ++y, to += 8 * 128) {
                     const uint32_t s2 = checked_scale(sc[0], bad) * 0x10001u;
 #pragma unroll
