@@ -20,7 +20,7 @@
 // Measured (32 query heads, 8 KV heads of 128): 1024 tokens over 16384 positions 254 us, 1048 TFLOP/s, 241 of it before
 // the join; 64 tokens over 12352 positions 39 us, 32 before it. Bound by the chain of waits of a stream (weights, their
 // product, the next scores, its maximum), by fetching the roles' code and by the shared memory that the products read.
-// 256 rows a block, because each unpacking of a tile serves all of them.  Few rows (64 drafts' of 16 tokens): bound by the
+// 256 rows a block, because each unpacking of a tile serves all of them.  Few rows (16 drafts of 4 heads): bound by the
 // unpacking warps, 1.5 to 1.9 us a tile, and about 9 us a segment; rows asked for ahead in L2 206 us for 194 (more for those warps to do).
 // Other forms, when this one (with a slower join) took 286 to 292 us: 128 rows 367; two warps that issue 335; 16 softmax warps of 72 registers 408; registers not
 // moved between the roles and 8 + 8 + 1 warps 317; scores in two halves of 64 positions 293 to 299; the products alone,
