@@ -165,6 +165,44 @@ def test_weights_of_all_kinds(kind, T, keep):
         assert torch.equal(check[0][l, 0, :keep], check[1][l, 0, torch.tensor(at[l][0], device="cuda")])
 
 
+def test_many_lists_of_many_caches():
+    """More caches than a launch of either kernel takes, more lists than SMs, in place and not."""
+    n = 70
+    Ts = [1 + 7 * i for i in range(n)]
+    for into in (False, True):
+        c = Caches(64, 3, Ts, layers=2)
+        o = Caches(64, 3, [100] * n, layers=2, seed=1) if into else None
+        idx = c.rx.evict(c.caches, c.weights, 100, 2, 5, into=o.caches if into else None)
+        c.rx.sync_status()
+        for i in (0, 13, 14, 31, 32, 63, 64, 69):
+            at = want(c, i, 100, 2, 5)
+            check_idx(idx[i], at, 100)
+            check_moved(c, i, at, 0, c.rows((o if into else c).caches[i]), None if into else c.weights[i], was=o.was[i] if into else None)
+    c = Caches(64, 3, [300] * n, layers=2)
+    path = torch.arange(1, 40, 3, dtype=torch.int32, device="cuda")
+    c.rx.keep(c.caches, [path] * n, 40, weights=c.weights)
+    c.rx.sync_status()
+    for i in (0, 31, 32, 69):
+        check_moved(c, i, [[[260 + x for x in path.tolist()]] * 3] * 2, 260, c.rows(c.caches[i]), c.weights[i])
+
+
+def test_on_another_stream():
+    """Work queued behind other work of the stream that is given, not of the current one."""
+    c = Caches(128, 2, [3000])
+    stream = torch.cuda.Stream()
+    w = c.weights[0]
+    late = w.flip(-1).contiguous()
+    c.had = [late.clone()]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)
+        w.copy_(late)
+    c.rx.evict(c.caches, c.weights, 500, 1, 9, stream=stream)
+    stream.synchronize()
+    c.rx.sync_status(stream)
+    check_moved(c, 0, want(c, 0, 500, 1, 9), 0, c.rows(c.caches[0]), c.weights[0])
+
+
 def test_a_long_list():
     """More keys than the blocks of a cluster hold in shared memory, few and many rows kept."""
     T = 8 * 24 * 1024 + 5000

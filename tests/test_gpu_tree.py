@@ -143,6 +143,15 @@ def test_one_tensor_for_all_and_repeated_runs(m):
     assert torch.equal(again, out)
 
 
+@pytest.mark.parametrize("m", [2, 30])
+def test_more_sequences_than_a_launch_takes(m):
+    n = 70
+    c = Case(64, 4, 2, [m] * n, [m + 5 * i for i in range(n)])
+    bits = [None if i % 7 == 3 else bits_of("tree", m, i) for i in range(n)]
+    c.run(trees=[None if x is None else cb.pack_words(x).cuda() for x in bits])
+    check(c, bits)
+
+
 def test_refusals():
     c = Case(128, 8, 2, [8], [100])
     w = cb.pack_words(bits_of("tree", 8, 0)).cuda()

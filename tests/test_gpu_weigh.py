@@ -304,6 +304,13 @@ def test_a_wait_that_gives_up(d, m):
     c.check()
 
 
+@pytest.mark.parametrize("m", [1, 9, 40])
+def test_more_heads_than_blocks(m):
+    c = Weighed(64, 900, 900, [m, 1], [70, 200])
+    c.weigh()
+    c.check()
+
+
 def test_weights_of_a_softmax_sum_to_one():
     c = Weighed(128, 32, 8, [70], [3000])
     w = torch.zeros(8, 3000, device="cuda")
