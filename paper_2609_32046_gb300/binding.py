@@ -470,6 +470,28 @@ def pack_words(seen):
     return torch.where(w >= 1 << 31, w - (1 << 32), w).to(torch.int32)
 
 
+_int32s = set()
+
+
+def _one_int32(x) -> int:
+    """The address of a tensor of one int32."""
+    t = x.dtype
+    if t not in _int32s:                      # (types that were one before are known)
+        _require(_is_int32(x), "a length or count is one int32")
+        _int32s.add(t)
+    if x.numel() != 1:
+        raise ValueError("a length or count is one int32")
+    return x.data_ptr()
+
+
+def _spread(fields, places, n: int):
+    """fields[at], fields[at + width] ... of n records as first, first + step ...: (at, first, step) each, `width` numbers a record."""
+    width = len(fields) // n
+    for at, first, step in places:
+        if step:
+            fields[at::width] = array("q", range(first, first + n * step, step))
+
+
 def _is_f32(x) -> bool:
     return x.element_size() == 4 and x.dtype.is_floating_point
 
@@ -895,7 +917,7 @@ class CacheBack:
         else:
             layers = weights[0].shape[0] if n else 0
         if many[1]:
-            out, out_step, ts = self._weights(weights_into, layers, min(max(keep, default=0), most))
+            theirs = self._weights(weights_into, layers, min(max(keep, default=0), most))
         if many[2]:
             shape, st = idx.shape, idx.stride()
             k = shape[-1]
@@ -905,6 +927,9 @@ class CacheBack:
             at, at_step = idx.data_ptr(), 4 * st[0]
         fields, left = array("q"), []         # of the header's cb_eviction, eight bytes each
         first, last = int(first), int(last)
+        # one tensor each, and all in place or none: the sequences' addresses by arithmetic
+        alike = n > 1 and many[0] and many[2] and (into is None or ((many[1] or weights_into is None) and
+                                                                    not any(p is q for p, q in zip(caches, into))))
         for i in range(n):
             p, to, k = caches[i], targets[i], keep[i]
             if p._shape != like or to._shape != like:
@@ -914,7 +939,9 @@ class CacheBack:
                 w, w_step, ws = self._weights(weights[i], layers, p.T)
             if to is p:
                 out, out_step, ts = w, w_step, ws
-            elif not many[1]:
+            elif many[1]:
+                out, out_step, ts = theirs
+            else:
                 x = None if weights_into is None else weights_into[i]
                 out, out_step, ts = (0, 0, (0, 0)) if x is None else self._weights(x, layers, min(k, p.T))
             if not many[2]:
@@ -927,11 +954,14 @@ class CacheBack:
                 _require(p.length is None, "a length on the device needs one that receives the rows kept")
                 length = 0
             else:
-                if own.numel() != 1 or not _is_int32(own):
-                    raise ValueError("a length is one int32")
-                length = own.data_ptr()
+                length = _one_int32(own)
             left.append(length)
-            fields.extend((w + i * w_step, out + i * out_step, ws[0], ws[1], ts[0], ts[1], k, first, last, at + i * at_step, length))
+            if not alike:
+                fields.extend((w + i * w_step, out + i * out_step, ws[0], ws[1], ts[0], ts[1], k, first, last, at + i * at_step, length))
+        if alike:
+            fields = array("q", (w, out, ws[0], ws[1], ts[0], ts[1], 0, first, last, at, 0)) * n
+            _spread(fields, ((0, w, w_step), (1, out, out_step), (9, at, at_step)), n)
+            fields[6::11], fields[10::11] = array("q", keep), array("q", left)
         held = b"".join([p._state[1] or p._described() for p in caches])
         taken = None if into is None else b"".join([p._described() if p is q else p._described_room() for p, q in zip(into, caches)])
         self._check(self.lib.cb_evict(self.h, int(layer), int(layers), n, held, taken, fields.buffer_info()[0],
@@ -964,7 +994,7 @@ class CacheBack:
         if not _as_many(n, idx, counts, weights, lengths):
             raise ValueError("one entry per cache in every list")
         drafted = _each(drafted, n, "drafted")
-        like, left = self._shape, []
+        like, left, kept = self._shape, [], []
         many = hasattr(idx, "data_ptr"), hasattr(counts, "data_ptr"), hasattr(weights, "data_ptr")      # one tensor each
         fields = array("q")                   # of the header's cb_kept, eight bytes each
         if many[0]:
@@ -981,6 +1011,7 @@ class CacheBack:
             w, w_step, ws = self._weights(weights, like[0], max([p.T for p in caches], default=0))
         elif weights is None:
             w, w_step, ws = 0, 0, (0, 0)
+        alike = n > 1 and many[0] and (many[1] or counts is None) and (many[2] or weights is None)
         for i, p in enumerate(caches):
             if p._shape != like:
                 self._fits(p)
@@ -990,27 +1021,29 @@ class CacheBack:
                     raise ValueError("idx holds an int32 a row")
                 at, step, rows = x.data_ptr(), 0, x.numel()
             if not many[1] and counts is not None:
-                x = counts[i]
-                _require(x is None or (_is_int32(x) and x.numel() == 1), "a count is one int32")
-                count, count_step = _address(x), 0
+                count, count_step = 0 if counts[i] is None else _one_int32(counts[i]), 0
             if not many[2] and weights is not None:
                 w, w_step, ws = (0, 0, (0, 0)) if weights[i] is None else self._weights(weights[i], like[0], p.T)
             own = p.length if lengths is None else lengths[i]
             if own is None:
                 _require(not count and p.length is None, "lengths and counts on the device need a length that receives the rows left")
-                left.append(rows)
                 to = 0
             else:
-                if own.numel() != 1 or not _is_int32(own):
-                    raise ValueError("a length is one int32")
-                left.append(None)
-                to = own.data_ptr()
-            fields.extend((at + i * step, rows, count + i * count_step, drafted[i], w + i * w_step, ws[0], ws[1], to))
+                to = _one_int32(own)
+            left.append(to)
+            if not alike:
+                kept.append(rows)
+                fields.extend((at + i * step, rows, count + i * count_step, drafted[i], w + i * w_step, ws[0], ws[1], to))
+        if alike:
+            kept = [rows] * n
+            fields = array("q", (at, rows, count, 0, w, ws[0], ws[1], 0)) * n
+            _spread(fields, ((0, at, step), (2, count, count_step), (4, w, w_step)), n)
+            fields[3::8], fields[7::8] = array("q", drafted), array("q", left)
         held = b"".join([p._state[1] or p._described() for p in caches])
         self._check(self.lib.cb_keep(self.h, n, held, fields.buffer_info()[0], _stream_on(stream, caches[0].k) if n else 0))
         if lengths is None:
-            for p, rows, m in zip(caches, left, drafted):
-                if rows is not None:
+            for p, to, rows, m in zip(caches, left, kept, drafted):
+                if not to:
                     p.T = p.T - m + rows
     def _queries(self, Q, out, lse):
         """One sequence's fields of a cb_attend_query, looked over."""

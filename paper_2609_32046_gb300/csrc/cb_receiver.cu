@@ -622,7 +622,9 @@ struct Places {
 };
 
 cb_status move_all(cb_ctx* ctx, std::vector<MoveSeq>& seqs, int32_t n_layers, cudaStream_t strm) {
-    for (int pass = 0; pass < 2; ++pass)                    // rows, then lengths
+    bool later = false;
+    for (const MoveSeq& m : seqs) later |= m.left_later != 0;
+    for (int pass = 0; pass < (later ? 2 : 1); ++pass)      // rows, then lengths
         for (size_t b0 = 0; b0 < seqs.size(); b0 += kMaxPackBatch) {
             MoveBatch b;
             std::memset(&b, 0, sizeof b);

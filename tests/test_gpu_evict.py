@@ -186,6 +186,25 @@ def test_many_lists_of_many_caches():
         check_moved(c, i, [[[260 + x for x in path.tolist()]] * 3] * 2, 260, c.rows(c.caches[i]), c.weights[i])
 
 
+def test_in_place_and_into_others_in_one_call():
+    """One tensor of weights to move into, of which a cache that is held in place takes none."""
+    c, o = Caches(128, 2, [200, 300, 250]), Caches(128, 2, [90, 90, 90], seed=4)
+    weights = torch.zeros(3, 2, 2, 300, device="cuda")
+    for i, w in enumerate(c.weights):
+        weights[i, :, :, :w.shape[2]] = w
+    had = weights.clone()
+    to, into = torch.full((3, 2, 2, 90), -1.0, device="cuda"), [o.caches[0], c.caches[1], o.caches[2]]
+    idx = torch.zeros(3, 2, 2, 90, dtype=torch.int32, device="cuda")
+    c.rx.evict(c.caches, weights, 90, 1, 9, into=into, weights_into=to, idx=idx)
+    c.rx.sync_status()
+    for i in range(3):
+        at = want(c, i, 90, 1, 9)
+        check_idx(idx[i], at, 90)
+        check_moved(c, i, at, 0, c.rows(into[i]), weights[i] if i == 1 else to[i], was=None if i == 1 else o.was[i])
+    assert (to[1] == -1).all() and torch.equal(weights[::2], had[::2])
+    assert [p.T for p in c.caches] == [200, 90, 250]
+
+
 def test_on_another_stream():
     """Work queued behind other work of the stream that is given, not of the current one."""
     c = Caches(128, 2, [3000])
