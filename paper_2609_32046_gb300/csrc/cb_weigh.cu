@@ -59,7 +59,7 @@ __device__ __forceinline__ bool look_over_keys(uint8_t* stage, uint32_t* err) {
 // lanes, and every position's sum is written by one lane: nothing to join.
 //
 // Bound by instructions, as k_attend_few's half of the keys is (some 570 a warp for 32 positions, 64 of them conversions and
-// 140 masks and shifts of codes): 48 sequences in pages, 8 KV heads of 128, 4 rows: 53 us, 2.8 TB/s of 22 that the bytes take;
+// 140 masks and shifts of codes): 48 sequences in pages, 8 KV heads of 128, 4 rows: 53 us, 2.8 TB/s, where the bytes take 22;
 // one token over 2048 positions 5.3 us.
 template <int D, int NT>
 __global__ void __launch_bounds__(kWarps * 32, kBlocksPerSm) k_weigh_few(const __grid_constant__ WeighBatch b) {
