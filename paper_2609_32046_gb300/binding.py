@@ -6,6 +6,7 @@ the import of `CacheBack` fails loudly: there is no CPU fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -224,6 +225,18 @@ def _stream_on(stream, tensor) -> int:
         import torch
         _raw_stream = torch._C._cuda_getCurrentRawStream
     return _raw_stream(tensor.device.index)
+
+
+def _memory_for(stream, tensor):
+    """A context in which memory for a call on `stream` is allocated: the stream's own, so that who gets the memory next
+    comes behind the call, whatever the current stream is."""
+    if stream is None or not tensor.is_cuda or _stream_on(stream, tensor) == _stream_on(None, tensor):
+        return contextlib.nullcontext()
+    import torch
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream_on(stream, tensor)            # (0 and 1 name the default stream)
+        stream = torch.cuda.ExternalStream(handle, device=tensor.device) if handle > 1 else torch.cuda.default_stream(tensor.device)
+    return torch.cuda.stream(stream)
 
 
 class PagedKV:
@@ -898,7 +911,8 @@ class CacheBack:
         [layers][Hkv][keep or more]; None: weights do not move).  idx[i] (int32 [layers][Hkv][keep], contiguous) receives the
         rows that stayed, -1 behind them.  lengths[i] (int32, one element) receives their number; lengths None:
         the receiving cache's own `length`, where it has one, and its T becomes min(T, keep) where it has none.
-        Evict all layers in one call, or give lengths of their own to all calls but the last.  Returns idx."""
+        Evict all layers in one call, or give lengths of their own to all calls but the last.  Returns idx, by default new tensors:
+        memory of the call's stream, as that of other tensors made there is."""
         n = len(caches)
         if not _as_many(n, weights, into, weights_into, idx, lengths):
             raise ValueError("one entry per cache in every list")
@@ -908,7 +922,8 @@ class CacheBack:
         keep = [int(k) for k in _each(keep, n, "keep")]
         if idx is None:
             import torch
-            idx = [torch.empty(tuple(w.shape[:2]) + (k,), dtype=torch.int32, device=p.device) for w, k, p in zip(weights, keep, caches)]
+            with _memory_for(stream, caches[0].k) if n else contextlib.nullcontext():
+                idx = [torch.empty(tuple(w.shape[:2]) + (k,), dtype=torch.int32, device=p.device) for w, k, p in zip(weights, keep, caches)]
         many = [hasattr(x, "data_ptr") for x in (weights, weights_into, idx)]      # one tensor each
         most = max([p.T for p in caches], default=0)
         if many[0]:
