@@ -685,9 +685,8 @@ cb_status evict_impl(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, co
                               (c.n_kv_heads == 1 || e.w_head == e.t_head);
             if (e.weights_to && (other ? touch(e.weights, 4 * span, e.weights_to, 4 * span_to) : !same))
                 return fail(ctx, CB_EINVAL, "evictions[%d]: weights move as the rows do, in place or to memory of their own", i);
-            const uintptr_t w = reinterpret_cast<uintptr_t>(e.weights_to), x = reinterpret_cast<uintptr_t>(e.idx);
+            const uintptr_t w = reinterpret_cast<uintptr_t>(e.weights_to);
             if (w) places.weights.push_back(Written{w, w + 4 * (uintptr_t)span_to, span_to == lists * rows});
-            places.idx.push_back(Written{x, x + 4 * (uintptr_t)(lists * e.keep), true});
             places.add(p, to, d, c);
         }
         places.lengths.push_back(reinterpret_cast<uintptr_t>(p.length));
@@ -699,7 +698,10 @@ cb_status evict_impl(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, co
         m.length = p.length;
         m.left = e.length;
         m.drafted = -1;
-        if (p.T > 0 && e.keep > 0) {
+        if (e.keep > 0 && e.idx) {                     // (of an empty cache -1 everywhere: its weights are not read)
+            if (p.T == 0 && (st = ptrs.check(e.idx, "evictions.idx", i, 4))) return st;
+            const uintptr_t x = reinterpret_cast<uintptr_t>(e.idx);
+            places.idx.push_back(Written{x, x + 4 * (uintptr_t)(lists * e.keep), true});
             RankSeq r{};
             r.weights = e.weights;
             r.w_layer = e.w_layer; r.w_head = e.w_head;
@@ -708,6 +710,8 @@ cb_status evict_impl(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, co
             r.keep = e.keep; r.first = e.first; r.last = e.last;
             r.idx = e.idx;
             ranks.push_back(r);
+        }
+        if (p.T > 0 && e.keep > 0) {
             m.from = packed_layer(p, d, layer);
             m.to = packed_layer(to, d, layer);
             m.w = e.weights_to ? e.weights : nullptr;
