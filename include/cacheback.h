@@ -613,9 +613,11 @@ typedef struct {
  *   into   NULL: in the cache itself; or the cache that receives the rows, whose T is at least keep or
  *          caches[i].T.  into[i] that names caches[i]'s own codes of K is in place too and has to be its equal;
  *          another's memory may not touch that of any cache of the call
- * Rows that are written may be no other sequence's (pages that two block tables share, say).
+ * Rows that are written may be no other sequence's (pages that two block tables share, say), nor may weights_to be weights of
+ * another sequence that move.
  * A block-table entry outside [0, n_pages) leaves its rows out and is reported by cb_sync_status as CB_EDEVICE.
- * Errors: CB_EINVAL (also a cache or a length that is written twice, a length that is written and another cache's), CB_ESHAPE
+ * Errors: CB_EINVAL (also a cache or a length that is written twice, a length that is written and another cache's, weights
+ * that one entry writes and another moves), CB_ESHAPE
  * (layers, T, keep), CB_EBUDGET (first + last above keep, into too small).
  */
 cb_status cb_evict(cb_ctx *ctx, int32_t layer, int32_t n_layers, int32_t n, const cb_packed *caches, const cb_packed *into,

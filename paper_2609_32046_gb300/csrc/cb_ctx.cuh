@@ -124,6 +124,31 @@ inline bool written_twice(std::vector<Written>& w) {
     return false;
 }
 
+// A part reads what another part writes: they begin there both, or both are dense and overlap.  `reads` and `writes` name their
+// parts by `of`; no two writes clash (written_twice).
+struct PartOf {
+    Written at;
+    int32_t of;
+};
+inline bool read_and_written(const std::vector<PartOf>& reads, std::vector<PartOf> writes) {
+    if (writes.empty()) return false;
+    auto by_lo = [](const PartOf& a, const PartOf& b) { return a.at.lo < b.at.lo; };
+    if (!std::is_sorted(writes.begin(), writes.end(), by_lo)) std::sort(writes.begin(), writes.end(), by_lo);
+    for (const PartOf& r : reads) {
+        const auto same = std::lower_bound(writes.begin(), writes.end(), r, by_lo);
+        if (same != writes.end() && same->at.lo == r.at.lo && same->of != r.of) return true;
+    }
+    writes.erase(std::remove_if(writes.begin(), writes.end(), [](const PartOf& w) { return !w.at.dense; }), writes.end());
+    for (const PartOf& r : reads) {
+        if (!r.at.dense) continue;
+        // (dense writes lie apart, in order: those that overlap are the last ones that begin before the end)
+        auto w = std::lower_bound(writes.begin(), writes.end(), r.at.hi, [](const PartOf& a, uintptr_t hi) { return a.at.lo < hi; });
+        while (w != writes.begin() && (--w)->at.hi > r.at.lo)
+            if (w->of != r.of) return true;
+    }
+    return false;
+}
+
 inline bool stride_ok(int64_t s) { return s > 0 && (s % 8) == 0; }
 
 // An NVTX range over one call of the C-ABI (header-only NVTX: free unless a profiler listens).

@@ -577,6 +577,7 @@ struct Places {
     std::vector<std::pair<uintptr_t, uintptr_t>> paged;     // codes and table of every cache written
     std::vector<std::pair<uintptr_t, uintptr_t>> read, written;   // the same of those read and of all written, entry by entry
     std::vector<Written> weights, idx;
+    std::vector<PartOf> weights_from, weights_to;             // weights that move: where they are read, and `weights` again
     std::vector<uintptr_t> lengths, left;                   // numbers that are read, and lengths that are written
 
     // An entry's rows: from a cache, to a cache.
@@ -606,7 +607,7 @@ struct Places {
             const auto all = std::equal_range(sorted.begin(), sorted.end(), written[i]);
             if (all.second - all.first > (read[i] == written[i] ? 1 : 0)) return true;
         }
-        return written_twice(codes) || written_twice(weights) || written_twice(idx);
+        return written_twice(codes) || written_twice(weights) || written_twice(idx) || read_and_written(weights_from, weights_to);
     }
     // A length that is written is also another cache's, or a count, which is read.  `own`: the length that each cache has and
     // the one it writes.
@@ -686,7 +687,12 @@ cb_status evict_impl(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, co
             if (e.weights_to && (other ? touch(e.weights, 4 * span, e.weights_to, 4 * span_to) : !same))
                 return fail(ctx, CB_EINVAL, "evictions[%d]: weights move as the rows do, in place or to memory of their own", i);
             const uintptr_t w = reinterpret_cast<uintptr_t>(e.weights_to);
-            if (w) places.weights.push_back(Written{w, w + 4 * (uintptr_t)span_to, span_to == lists * rows});
+            if (w) {
+                const uintptr_t from = reinterpret_cast<uintptr_t>(e.weights);
+                places.weights.push_back(Written{w, w + 4 * (uintptr_t)span_to, span_to == lists * rows});
+                places.weights_to.push_back(PartOf{places.weights.back(), i});
+                places.weights_from.push_back(PartOf{{from, from + 4 * (uintptr_t)span, span == lists * p.T}, i});
+            }
             places.add(p, to, d, c);
         }
         places.lengths.push_back(reinterpret_cast<uintptr_t>(p.length));

@@ -5,6 +5,7 @@ from types import SimpleNamespace
 import pytest
 import torch
 
+import host_program
 from paper_2609_32046_gb300 import binding
 from test_budget_host import Spy, cache, receiver
 
@@ -53,3 +54,50 @@ def test_evict_allocates_there(monkeypatch, stream):
     assert [tuple(x.shape) for x in idx] == [(3, 2, 9)] * 2 and made == [[stream]] * 2
     rx.evict(caches, w, 9, idx=idx, stream=stream)
     assert len(made) == 2
+
+
+def test_what_one_part_reads_and_another_writes(tmp_path):
+    """Parts (from, to, dense, of whom): found where both begin at one place, or both are dense and overlap, in any order."""
+    cases = [([], [], 0), ([(0, 8, 1, 0)], [], 0), ([(0, 8, 1, 0), (8, 16, 1, 1)], [(0, 8, 1, 0), (8, 16, 1, 1)], 0),         # in place
+             ([(0, 8, 1, 0), (8, 16, 1, 1)], [(8, 16, 1, 0), (0, 8, 1, 1)], 1),                                               # exchanged
+             ([(0, 8, 1, 0), (8, 16, 1, 1)], [(40, 48, 1, 0), (20, 28, 1, 1)], 0),
+             ([(0, 8, 1, 0), (8, 16, 1, 1)], [(20, 28, 1, 0), (0, 8, 0, 1)], 1),                                              # begins there
+             ([(0, 8, 1, 0), (8, 16, 1, 1)], [(20, 28, 1, 0), (7, 9, 1, 1)], 1),
+             ([(0, 8, 1, 0), (8, 16, 1, 1)], [(20, 28, 1, 0), (7, 9, 0, 1)], 0),                                              # between rows
+             ([(0, 100, 0, 0), (10, 110, 0, 1)], [(20, 120, 0, 0), (30, 130, 0, 1)], 0),
+             ([(0, 100, 1, 0)], [(0, 10, 1, 0), (10, 20, 1, 0), (50, 60, 1, 1), (200, 300, 1, 2)], 1),
+             ([(0, 100, 1, 0)], [(90, 110, 1, 0), (100, 102, 0, 1), (110, 120, 1, 2)], 0),
+             ([(100, 110, 1, 5)], [(0, 101, 1, 4)], 1), ([(100, 110, 1, 5)], [(0, 100, 1, 4), (110, 111, 1, 3)], 0)]
+    part = lambda p: "cbk::PartOf{{%du, %du, %s}, %d}" % (p[0], p[1], "true" if p[2] else "false", p[3])       # noqa: E731
+    body = "".join("std::printf(\"%%d\\n\", (int)cbk::read_and_written({%s}, {%s}));\n" % tuple(", ".join(map(part, x)) for x in (r, w))
+                   for r, w, _ in cases)
+    lines = host_program.run(tmp_path, "#include <cstdio>\n#include \"cb_ctx.cuh\"\nint main() {\n%sreturn 0; }\n" % body)
+    assert [int(x) for x in lines] == [want for _, _, want in cases]
+
+
+def test_weights_that_two_entries_share(tmp_path):
+    """cb_evict's look over a call's entries: weights that one writes and another moves."""
+    program = r"""
+#include <cstdio>
+#include "cb_receiver.cu"
+int main() {
+    // two entries: where the weights of each are read (-1: they do not move) and written, 100 bytes each
+    const long long calls[][4] = {{0, 500, 100, 600}, {0, 0, 100, 100}, {0, 100, 100, 0}, {0, 500, 100, 0}, {0, 500, 100, 50}, {0, 500, -1, -1}};
+    for (auto& c : calls) {
+        Places p;
+        for (int i = 0; i < 2; ++i) {
+            if (c[2 * i] < 0) continue;
+            const uintptr_t from = 1000 + c[2 * i], to = 1000 + c[2 * i + 1];
+            p.weights.push_back(Written{to, to + 100, true});
+            p.weights_to.push_back(PartOf{p.weights.back(), i});
+            p.weights_from.push_back(PartOf{{from, from + 100, true}, i});
+        }
+        std::printf("%d\n", (int)p.clash());
+    }
+    return 0;
+}
+"""
+    objects = ["cb_api", "cb_rotary", "cb_pack", "cb_attend", "cb_attend_tc", "cb_weigh", "cb_weigh_tc", "cb_evict", "cb_score", "cb_score_tc_0",
+               "cb_score_tc_64", "cb_score_tc_128", "cb_select", "cb_compact", "cb_gather", "cb_rope", "cb_depage"]
+    lines = host_program.run(tmp_path, program, objects)
+    assert [int(x) for x in lines] == [0, 0, 1, 1, 1, 0]

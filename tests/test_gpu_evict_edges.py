@@ -59,3 +59,37 @@ def test_empty_caches(Ts, into):
         assert torch.equal(c.rx.evict(c.caches[:1], c.weights[:1], keep)[0], torch.full((2, 2, keep), -1, dtype=torch.int32, device="cuda"))
         with pytest.raises(cb.CBError):
             c.rx.evict(c.caches[:1], c.weights[:1], keep, idx=[idx[0].cpu()])
+
+
+def test_weights_that_two_entries_share():
+    """Entries whose weights move to where another's are taken from are refused, in place and into other caches; weights that
+    two only read are not."""
+    c, o = Caches(128, 2, [100, 100, 100]), Caches(128, 2, [20, 20, 20], seed=2)
+    w = c.weights
+    spare = [torch.zeros(2, 2, 20, device="cuda") for _ in w]
+    wide = torch.zeros(2, 2, 100, device="cuda")
+    both = torch.rand(500, device="cuda")
+    for weights, to, into in (([w[0], w[1]], [w[1], w[0]], None), ([w[0], w[1]], [wide, w[0]], None), ([w[0], w[0]], [w[0], spare[0]], True),
+                              ([both[:400].view(2, 2, 100), w[1]], [spare[0], both[390:470].view(2, 2, 20)], None)):
+        caches = o.caches[:2] if into is None else [c.caches[0], o.caches[1]]
+        with pytest.raises(cb.CBError):
+            c.rx.evict(c.caches[:2], weights, 20, into=caches, weights_into=to)
+    c.rx.sync_status()
+    assert all(torch.equal(a, b) for p, x in zip(c.caches, c.was) for a, b in zip(c.rows(p), x)) and [p.T for p in c.caches] == [100] * 3
+    c.had = [w[0].clone() for _ in w]
+    idx = c.rx.evict(c.caches, [w[0]] * 3, 20, 1, 2, into=o.caches, weights_into=spare)
+    c.rx.sync_status()
+    for i in range(3):
+        at = want(c, i, 20, 1, 2)
+        check_idx(idx[i], at, 20)
+        check_moved(c, i, at, 0, c.rows(o.caches[i]), spare[i], was=o.was[i])
+    # weights that are ranked by and stay where they are may be what another entry writes: all are ranked first
+    c, o = Caches(128, 2, [100, 100], seed=5), Caches(128, 2, [20, 20], seed=2)
+    c.had[1] = c.had[0]
+    into = [c.caches[0], o.caches[1]]
+    idx = c.rx.evict(c.caches, [c.weights[0]] * 2, 20, 1, 2, into=into)
+    c.rx.sync_status()
+    for i in range(2):
+        at = want(c, i, 20, 1, 2)
+        check_idx(idx[i], at, 20)
+        check_moved(c, i, at, 0, c.rows(into[i]), c.weights[0] if i == 0 else None, was=None if i == 0 else o.was[1])
