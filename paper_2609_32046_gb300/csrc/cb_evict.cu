@@ -21,8 +21,6 @@ __device__ __forceinline__ int64_t rows_of(int64_t T, const int32_t* length) {
 constexpr int kRankThreads = 1024, kRankWarps = kRankThreads / 32;
 constexpr int kBins = 2048;
 constexpr int kRankPasses = 3;
-constexpr int kRankKeys = 24 * 1024;         // keys of a block's slice held in shared memory at most (96 KB)
-constexpr int kRankCluster = 8;
 
 // Larger weights have larger keys; -0 is 0, NaN below all.
 __device__ __forceinline__ uint32_t rank_key(float w) {
@@ -525,17 +523,25 @@ cudaError_t launch_rank_by(const RankBatch& b, int64_t slice, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms) {
+RankPlan rank_plan(const RankBatch& b, int num_sms) {
     int64_t most = 0;
     for (int i = 0; i < b.n; ++i) most = b.s[i].T > most ? b.s[i].T : most;
     // blocks of a list: as many as hold it, and while the lists leave SMs idle
     const int64_t lists = (int64_t)b.n * b.n_layers * b.n_kv_heads;
-    int c = 1;
-    while (c < kRankCluster && (most > (int64_t)c * kRankKeys || (2 * lists * c <= num_sms && most > 2048 * c))) c *= 2;
-    const int64_t slice = (most + c - 1) / c + 4;
-    if (slice > kRankKeys) return launch_rank_by<kRankCluster, false>(b, slice, st);       // (c is that)
-    return c == 1 ? launch_rank_by<1, true>(b, slice, st) : c == 2 ? launch_rank_by<2, true>(b, slice, st)
-         : c == 4 ? launch_rank_by<4, true>(b, slice, st) : launch_rank_by<8, true>(b, slice, st);
+    RankPlan p{1, (most + 3) & ~(int64_t)3};
+    while (p.blocks < kRankCluster && (p.slice > kRankKeys || (2 * lists * p.blocks <= num_sms && most > 2048 * p.blocks))) {
+        p.blocks *= 2;
+        p.slice = ((most + p.blocks - 1) / p.blocks + 3) & ~(int64_t)3;
+    }
+    p.held = p.slice <= kRankKeys;
+    return p;
+}
+
+cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms) {
+    const RankPlan p = rank_plan(b, num_sms);
+    if (!p.held) return launch_rank_by<kRankCluster, false>(b, p.slice, st);
+    return p.blocks == 1 ? launch_rank_by<1, true>(b, p.slice, st) : p.blocks == 2 ? launch_rank_by<2, true>(b, p.slice, st)
+         : p.blocks == 4 ? launch_rank_by<4, true>(b, p.slice, st) : launch_rank_by<8, true>(b, p.slice, st);
 }
 
 cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int num_sms) {

@@ -196,6 +196,16 @@ cudaError_t launch_attend(AttendBatch& b, int head_dim, cudaStream_t st, int num
 cudaError_t launch_attend(AttendTreeBatch& b, int head_dim, cudaStream_t st, int num_sms);
 // Fills in pair0 and pairs, and launches.
 cudaError_t launch_weigh(WeighBatch& b, int head_dim, cudaStream_t st, int num_sms);
+// How k_rank takes a batch: blocks of a list, keys of a block at most, and whether its shared memory holds them all (where it
+// does not, there are kRankCluster).
+constexpr int kRankKeys = 24 * 1024;         // keys of a block's slice held in shared memory at most (96 KB)
+constexpr int kRankCluster = 8;
+struct RankPlan {
+    int blocks;
+    int64_t slice;
+    bool held;
+};
+RankPlan rank_plan(const RankBatch& b, int num_sms);
 cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms);
 cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int num_sms);
 cudaError_t launch_left(const MoveBatch& b, cudaStream_t st);     // those that are left_later, behind every launch_move of a call

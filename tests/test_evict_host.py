@@ -101,3 +101,41 @@ int main() {
                "cb_score_tc_64", "cb_score_tc_128", "cb_select", "cb_compact", "cb_gather", "cb_rope", "cb_depage"]
     lines = host_program.run(tmp_path, program, objects)
     assert [int(x) for x in lines] == [0, 0, 1, 1, 1, 0]
+
+
+def test_blocks_of_a_list(tmp_path):
+    """k_rank's plan: as few blocks a list as hold its keys where lists fill the GPU, most blocks alone where eight do not."""
+    keys = 24 * 1024
+    rows = sorted({0, 1, 2, 100, 16384, 200000, 8 * keys + 40} |
+                  {c * keys + x for c in (1, 2, 4, 8) for x in (-5, -4, -3, -1, 0, 1, 2, 7)})
+    program = r"""
+#include <cstdio>
+#include <cstring>
+#include "cb_receiver.cuh"
+int main() {
+    static cbk::RankBatch b;
+    for (int lists : {288, 76, 1})
+        for (long long T : {%s}) {
+            std::memset(&b, 0, sizeof b);
+            b.n = 2;
+            b.n_layers = 1;
+            b.n_kv_heads = lists;
+            b.s[1].T = T;
+            const cbk::RankPlan p = cbk::rank_plan(b, 152);
+            std::printf("%%d %%lld %%d\n", p.blocks, (long long)p.slice, (int)p.held);
+        }
+    return 0;
+}
+""" % ", ".join("%dll" % T for T in rows)
+    lines = iter(host_program.run(tmp_path, program, ["cb_evict"]))
+    for lists in (288, 76, 1):
+        for T in rows:
+            blocks, part, held = map(int, next(lines).split())
+            for n in {T, max(0, T - 1), max(0, T - 65)}:                    # inner rows: the kernel's slices hold them all
+                assert (-(-n // blocks) + 3) // 4 * 4 <= part
+            assert held == (part <= keys) and (held or blocks == 8)
+            assert held == (T <= 8 * keys)
+            if lists > 1:
+                assert blocks == next((c for c in (1, 2, 4) if T <= c * keys), 8)
+            elif T >= 16384:
+                assert blocks == 8

@@ -93,3 +93,26 @@ def test_weights_that_two_entries_share():
         at = want(c, i, 20, 1, 2)
         check_idx(idx[i], at, 20)
         check_moved(c, i, at, 0, c.rows(into[i]), c.weights[0] if i == 0 else None, was=None if i == 0 else o.was[1])
+
+
+@pytest.mark.parametrize("T", [24572, 24573, 24576, 24577, 49145, 49152, 49153, 98304])
+@pytest.mark.parametrize("lists", [1, 160])
+def test_lists_that_just_fit(T, lists):
+    """Keys up to the last one that a block's, or a cluster's, shared memory holds, and one more."""
+    layers, keep, first, last = (1, 700, 0, 0) if lists == 1 else (20, 90, 3, 10)
+    Hkv = lists // layers
+    g = torch.Generator(device="cuda").manual_seed(T)
+    codes = [torch.randint(0, 256, (layers, Hkv, T, 32), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    scales = [torch.rand((layers, Hkv, T, 2), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    into = [torch.zeros(layers, Hkv, keep, x.shape[-1], dtype=x.dtype, device="cuda") for x in codes + scales]
+    w = torch.randn((layers, Hkv, T), generator=g, device="cuda").exp_()
+    w[..., 100::3] = 1.0                                                    # many ties, past the last rows too
+    rx = cb.Receiver(layers, Hkv, Hkv, 64, 8, 64, 1)
+    idx = rx.evict([cb.PackedKV(*codes, *scales)], [w], keep, first, last, into=[cb.PackedKV(*into)])
+    rx.sync_status()
+    inner = torch.sort(w[..., first:T - last], dim=-1, descending=True, stable=True).indices[..., :keep - first - last] + first
+    ends = [torch.arange(a, b, device="cuda").expand(layers, Hkv, -1) for a, b in ((0, first), (T - last, T))]
+    at = torch.cat([ends[0], inner.sort(-1).values, ends[1]], -1)
+    assert torch.equal(idx[0].long(), at)
+    for a, b in zip(into, codes + scales):
+        assert torch.equal(a.view(torch.uint8), b.gather(2, at[..., None].expand(-1, -1, -1, b.shape[-1])).view(torch.uint8))
