@@ -551,9 +551,10 @@ cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int n
         most = b.s[i].count > most ? b.s[i].count : most;
         in_place |= b.s[i].in_place != 0;
     }
-    bool left = false;
-    for (int i = 0; i < b.n; ++i) left |= b.s[i].left && !b.s[i].left_later;
-    if (most == 0 && !left) return cudaSuccess;
+    // (no rows: lengths to write, and caches that may have fewer rows than `drafted`)
+    bool says = false;
+    for (int i = 0; i < b.n; ++i) says |= (b.s[i].left && !b.s[i].left_later) || (b.s[i].drafted > 0 && b.s[i].length);
+    if (most == 0 && !says) return cudaSuccess;
     return head_dim == 128 ? launch<128>(b, most, in_place, num_sms, st) : launch<64>(b, most, in_place, num_sms, st);
 }
 

@@ -116,3 +116,35 @@ def test_lists_that_just_fit(T, lists):
     assert torch.equal(idx[0].long(), at)
     for a, b in zip(into, codes + scales):
         assert torch.equal(a.view(torch.uint8), b.gather(2, at[..., None].expand(-1, -1, -1, b.shape[-1])).view(torch.uint8))
+
+
+@pytest.mark.parametrize("count", [0, 1])
+@pytest.mark.parametrize("own", [False, True])
+@pytest.mark.parametrize("others", [0, 40])
+def test_fewer_rows_than_drafts(count, own, others):
+    """A cache of fewer rows than were drafted is reported whether any of them are kept or none, and stays as it is, with its length."""
+    n = 1 + others
+    c = Caches(64, 2, [60] * n, lengths=[3] + [50] * others, layers=1)
+    path = torch.arange(1, 1 + count, dtype=torch.int32, device="cuda")
+    left = None if own else [torch.full((1,), 99, dtype=torch.int32, device="cuda") for _ in range(n)]
+    c.rx.keep(c.caches, [path] * n, 5, weights=c.weights, lengths=left)
+    with pytest.raises(cb.CBError) as e:
+        c.rx.sync_status()
+    assert e.value.status == cb.CB_EDEVICE
+    now = [int(p.length) if own else int(x) for p, x in zip(c.caches, left or c.caches)]
+    assert now == [3 if own else 99] + [45 + count] * others
+    for i in range(n):
+        check_moved(c, i, [[[46] * count if i else []] * 2], 45, c.rows(c.caches[i]), c.weights[i])
+
+
+def test_all_drafts_of_enough_rows_left_out():
+    """No error, and lengths without the drafts: host's, own and others'."""
+    c = Caches(64, 2, [60, 60], lengths=[5, 60], layers=1)
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    c.rx.keep(c.caches, [none, none], 5)
+    c.rx.sync_status()
+    assert [int(p.length) for p in c.caches] == [0, 55]
+    c = Caches(64, 2, [60, 60], layers=1)
+    c.rx.keep(c.caches, [none, none], [5, 60])
+    c.rx.sync_status()
+    assert [p.T for p in c.caches] == [55, 0]
