@@ -465,7 +465,7 @@ def tree_words(parents, device=None):
     p = torch.as_tensor(parents, dtype=torch.int64, device="cpu")
     _require(p.dim() >= 1 and bool(((p >= -1) & (p < torch.arange(p.shape[-1]))).all()), "a token follows an earlier one, or -1")
     m = p.shape[-1]
-    flat = p.reshape(-1, m)
+    flat = p.reshape(math.prod(p.shape[:-1]), m)
     seen = torch.zeros((flat.shape[0], m, m), dtype=torch.bool)
     at = torch.arange(flat.shape[0])
     for r in range(m):
