@@ -46,7 +46,7 @@ static_assert(kRankWarps == 32 && kBins == 2 * kRankThreads, "");
 // 10 bits from the top finds the key where the budget runs out (histograms joined in the first block's shared
 // memory); rows above it stay, and of those at it the lowest.  288 lists of 16384 rows, a block each, 20 us: loads (4), counting in
 // shared memory, whose adds to a few bins of like exponents queue, and barriers of 1024 threads; with every warp scanning every
-// count 25, with 512 threads and a scan for each 2048 keys 31, clusters of 8 for these lists 386.  HELD: no slice has more keys than shared memory holds.
+// count 25, with 512 threads and a scan for each 2048 keys 31.  HELD: no slice has more keys than shared memory holds.
 template <int C, bool HELD>
 __global__ void __launch_bounds__(kRankThreads) k_rank(const __grid_constant__ RankBatch b, uint32_t held) {
     extern __shared__ uint32_t keys[];                   // [held]
@@ -466,13 +466,18 @@ cudaError_t launch(const MoveBatch& b, int64_t most, bool in_place, int num_sms,
         k_move_into<D><<<dim3((unsigned)(units * blocks), 1, b.n), 256, 0, st>>>(b, blocks);
         return cudaGetLastError();
     }
-    if (most <= 64) {
+    // A warp a list, for up to 64 rows, and up to 128 where lists are many: 65 rows of 32 x 288 lists 48 us and with a block a list 108,
+    // 128 rows 69 and 115; 128 rows of 288 lists 13 and 13, of 80 lists 13 and 9; 200 rows of 288 lists 18 and 13.  (Graphs, of
+    // which 7 us are not the kernel's.)
+    if (most <= 64 || (most <= 128 && (int64_t)units * b.n >= 3 * num_sms)) {
         k_move<D, 32><<<dim3((units + 7) / 8, 1, b.n), 256, 0, st>>>(b, 1, 0);
         return cudaGetLastError();
     }
-    // blocks of a list: as many as fill the GPU, a step's rows each at least
+    // A block a list, or more while there are fewer than SMs, a step's rows each at least: 1024 rows of 4 lists 13 us with one block a
+    // list of K or V, 9 with four; of 64 lists 15.5 and 13.4 with two; of 152 lists 17.5 and 19.6 with two; 2048 rows of 288 lists
+    // 44 with one or two, 56 with eight.
     int blocks = 1;
-    while (blocks < 8 && (int64_t)units * b.n * blocks < 4 * num_sms && most > 256 * blocks) blocks *= 2;
+    while (blocks < 8 && (int64_t)units * b.n * blocks < num_sms && most > 256 * blocks) blocks *= 2;
     if (blocks == 1) {
         k_move<D, 256><<<dim3(units, 1, b.n), 256, 0, st>>>(b, 1, 0);
         return cudaGetLastError();
@@ -523,13 +528,14 @@ cudaError_t launch_rank_by(const RankBatch& b, int64_t slice, cudaStream_t st) {
 
 }  // namespace
 
-RankPlan rank_plan(const RankBatch& b, int num_sms) {
+RankPlan rank_plan(const RankBatch& b) {
     int64_t most = 0;
     for (int i = 0; i < b.n; ++i) most = b.s[i].T > most ? b.s[i].T : most;
-    // blocks of a list: as many as hold it, and while the lists leave SMs idle
-    const int64_t lists = (int64_t)b.n * b.n_layers * b.n_kv_heads;
+    // As few blocks of a list as hold it, however few lists there are: 2 lists of 16384 rows 16 us with one block each, 18 with
+    // four, 20 with eight; 288 lists 21, 60 and 169 (the cluster's barriers and histograms that are joined in one block's memory);
+    // 288 lists of 65536 rows 85 with four, 187 with eight.  (Calls that keep 32 rows, about 7 us of them not the ranking's.)
     RankPlan p{1, (most + 3) & ~(int64_t)3};
-    while (p.blocks < kRankCluster && (p.slice > kRankKeys || (2 * lists * p.blocks <= num_sms && most > 2048 * p.blocks))) {
+    while (p.blocks < kRankCluster && p.slice > kRankKeys) {
         p.blocks *= 2;
         p.slice = ((most + p.blocks - 1) / p.blocks + 3) & ~(int64_t)3;
     }
@@ -537,8 +543,8 @@ RankPlan rank_plan(const RankBatch& b, int num_sms) {
     return p;
 }
 
-cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms) {
-    const RankPlan p = rank_plan(b, num_sms);
+cudaError_t launch_rank(const RankBatch& b, cudaStream_t st) {
+    const RankPlan p = rank_plan(b);
     if (!p.held) return launch_rank_by<kRankCluster, false>(b, p.slice, st);
     return p.blocks == 1 ? launch_rank_by<1, true>(b, p.slice, st) : p.blocks == 2 ? launch_rank_by<2, true>(b, p.slice, st)
          : p.blocks == 4 ? launch_rank_by<4, true>(b, p.slice, st) : launch_rank_by<8, true>(b, p.slice, st);

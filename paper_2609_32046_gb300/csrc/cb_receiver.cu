@@ -740,7 +740,7 @@ cb_status evict_impl(cb_ctx* ctx, int32_t layer, int32_t n_layers, int32_t n, co
         b.n_layers = n_layers;
         b.n_kv_heads = c.n_kv_heads;
         for (int k = 0; k < b.n; ++k) b.s[k] = ranks[b0 + k];
-        const cudaError_t e = launch_rank(b, strm, ctx->num_sms);
+        const cudaError_t e = launch_rank(b, strm);
         if (e != cudaSuccess) return fail(ctx, CB_ECUDA, "rank launch failed: %s", cudaGetErrorString(e));
     }
     return move_all(ctx, moves, n_layers, strm);

@@ -205,8 +205,8 @@ struct RankPlan {
     int64_t slice;
     bool held;
 };
-RankPlan rank_plan(const RankBatch& b, int num_sms);
-cudaError_t launch_rank(const RankBatch& b, cudaStream_t st, int num_sms);
+RankPlan rank_plan(const RankBatch& b);
+cudaError_t launch_rank(const RankBatch& b, cudaStream_t st);
 cudaError_t launch_move(const MoveBatch& b, int head_dim, cudaStream_t st, int num_sms);
 cudaError_t launch_left(const MoveBatch& b, cudaStream_t st);     // those that are left_later, behind every launch_move of a call
 // Query rows of partial results that launch_attend may use on num_sms SMs.

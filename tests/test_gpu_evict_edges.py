@@ -148,3 +148,55 @@ def test_all_drafts_of_enough_rows_left_out():
     c.rx.keep(c.caches, [none, none], [5, 60])
     c.rx.sync_status()
     assert [p.T for p in c.caches] == [55, 0]
+
+
+@pytest.mark.parametrize("kind", ["equal", "few values", "nan", "late", "first", "close"])
+@pytest.mark.parametrize("T,keep", [(30000, 3001), (50000, 45000), (120000, 700)])
+def test_long_lists_of_all_kinds(kind, T, keep):
+    """Clusters of two, four and eight blocks: ties across the blocks' slices, all that stays in one of them."""
+    layers, first, last = 2, 3, 20
+    g = torch.Generator(device="cuda").manual_seed(T)
+    w = torch.rand((layers, 1, T), generator=g, device="cuda")
+    if kind == "equal":
+        w.fill_(0.25)
+    elif kind == "few values":
+        w.mul_(4).floor_()
+    elif kind == "nan":
+        w[w < 0.95] = float("nan")
+    elif kind == "late":
+        w.copy_(torch.arange(T, device="cuda").float())
+    elif kind == "first":
+        w.copy_(-torch.arange(T, device="cuda").float())
+    else:
+        w.copy_((torch.full_like(w, 1.0).view(torch.int32) + (w * 100).int()).view(torch.float32))
+    codes = [torch.randint(0, 256, (layers, 1, T, 32), generator=g, device="cuda", dtype=torch.uint8) for _ in range(2)]
+    scales = [torch.rand((layers, 1, T, 2), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    had, was = w.clone(), [x.clone() for x in codes + scales]
+    rx = cb.Receiver(layers, 1, 1, 64, 8, 64, 1)
+    idx = rx.evict([cb.PackedKV(*codes, *scales)], [w], keep, first, last)
+    rx.sync_status()
+    key = torch.nan_to_num(had[..., first:T - last].double(), nan=-1e300)
+    inner = torch.sort(key, dim=-1, descending=True, stable=True).indices[..., :keep - first - last] + first
+    ends = [torch.arange(a, b, device="cuda").expand(layers, 1, -1) for a, b in ((0, first), (T - last, T))]
+    at = torch.cat([ends[0], inner.sort(-1).values, ends[1]], -1)
+    assert torch.equal(idx[0].long(), at)
+    assert torch.equal(w[..., :keep].view(torch.int32), had.gather(-1, at).view(torch.int32)) and \
+        torch.equal(w[..., keep:].view(torch.int32), had[..., keep:].view(torch.int32))
+    for a, b in zip(codes + scales, was):
+        assert torch.equal(a[:, :, :keep].view(torch.uint8), b.gather(2, at[..., None].expand(-1, -1, -1, b.shape[-1])).view(torch.uint8))
+
+
+@pytest.mark.parametrize("layers,n", [(2, 1), (20, 12), (36, 2)])
+@pytest.mark.parametrize("m", [64, 65, 128, 129, 400])
+def test_kept_rows_of_few_and_many_lists(layers, n, m):
+    """Rows moved by a warp, a block and the blocks of a cluster, by the number of lists and of rows."""
+    c = Caches(64, 8, [m + 20] * n, layers=layers)
+    path = torch.arange(m // 7, m, dtype=torch.int32, device="cuda")
+    c.rx.keep(c.caches, [path] * n, m, weights=c.weights)
+    c.rx.sync_status()
+    x = torch.arange(20 + m // 7, 20 + m, device="cuda")
+    for i in range(n):
+        for a, b in zip(c.rows(c.caches[i]), c.was[i]):
+            assert torch.equal(a[:, :, 20:20 + len(x)], b[:, :, x]) and torch.equal(a[:, :, 20 + len(x):], b[:, :, 20 + len(x):])
+            assert torch.equal(a[:, :, :20], b[:, :, :20])
+        assert torch.equal(c.weights[i][:, :, 20:20 + len(x)], c.had[i][:, :, x])
