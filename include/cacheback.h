@@ -578,8 +578,9 @@ typedef struct {
  * over the query heads h of KV head g (h / G = g) and the tokens r that see row t, which is as in cb_attend (causal, window) or, with
  * trees, as in cb_attend_tree.  A token's head whose lse is not finite adds nothing: what saw no row, and
  * what a caller leaves out by setting its lse to infinity (drafts that were not accepted).  Weights of rows
- * from L on are not written.  Sums are fp32, in a fixed order.  No sequence's weights may be another's weights or
- * before, or overlap anything else that the call reads.
+ * from L on are not written.  Sums are fp32, in a fixed order.  What the rounding of lse * log2(e) leaves out is made good where
+ * the call's longest sequence has up to 16 query rows a KV head (m * G); with more a weight carries it, up to 2^-23 |lse| of itself.
+ * No sequence's weights may be another's weights or before, or overlap anything else that the call reads.
  * m = 0 skips a sequence.
  *   trees   NULL, or one a sequence (then causal = 1 and window = 0)
  *   decay   within 0 .. 1

@@ -836,8 +836,9 @@ class CacheBack:
         over the tokens of Qs[i] (bf16 [m][Hq][d]) that see it and the heads of its group, with lses[i] (fp32 [m][Hq],
         contiguous) as attend wrote them; a head whose lse is not finite adds nothing.  weights[i], outs[i]: fp32
         [Hkv][rows], in place where outs or outs[i] is None; weights None: nothing gathered yet (then outs are given).
-        causal, window and trees as in attend.  fresh (a number, or one per cache; None: m): rows at the cache's end
-        that have gathered nothing yet.  All of them may be tensors with the sequences in their first dimension.
+        causal, window and trees as in attend.  fresh (a number, or one per cache; None: m, the tokens' own rows): rows at the
+        cache's end that have gathered nothing yet and whose weights[i] are not read; 0 for tokens that have no rows of their
+        own in the cache, as most calls with causal=False.  All of them may be tensors with the sequences in their first dimension.
         Returns outs."""
         n = len(caches)
         cfg, like = self.cfg, self._shape
@@ -908,7 +909,7 @@ class CacheBack:
         of each layer and KV head the first `first` rows, the last `last` and the heaviest of the others
         stay, by weights[i] (fp32 [layers][Hkv][rows]), ties to the lowest, in their order.  They become the
         first rows of the cache itself, weights with them, or of into[i] (another PackedKV) and weights_into[i] (fp32
-        [layers][Hkv][keep or more]; None: weights do not move).  idx[i] (int32 [layers][Hkv][keep], contiguous) receives the
+        [layers][Hkv][keep or more], no other entry's weights; None: weights do not move).  idx[i] (int32 [layers][Hkv][keep], contiguous) receives the
         rows that stayed, -1 behind them.  lengths[i] (int32, one element) receives their number; lengths None:
         the receiving cache's own `length`, where it has one, and its T becomes min(T, keep) where it has none.
         Evict all layers in one call, or give lengths of their own to all calls but the last.  Returns idx, by default new tensors:
@@ -1060,6 +1061,7 @@ class CacheBack:
             for p, to, rows, m in zip(caches, left, kept, drafted):
                 if not to:
                     p.T = p.T - m + rows
+
     def _queries(self, Q, out, lse):
         """One sequence's fields of a cb_attend_query, looked over."""
         qt, ot = Q.stride(), out.stride()

@@ -58,9 +58,10 @@ __device__ __forceinline__ bool look_over_keys(uint8_t* stage, uint32_t* err) {
 // each with its own copies.  S^T [16 positions][8 rows] = K Q^T (cb_few.cuh), the rows' weights are added up over a quad's
 // lanes, and every position's sum is written by one lane: nothing to join.
 //
-// Bound by instructions, as k_attend_few's half of the keys is (some 570 a warp for 32 positions, 64 of them conversions and
-// 140 masks and shifts of codes): 48 sequences in pages, 8 KV heads of 128, 4 rows: 53 us, 2.8 TB/s, where the bytes take 22;
-// one token over 2048 positions 5.3 us.
+// Bound, as k_attend_few's half of the keys is, by some 570 instructions a warp for 32 positions (64 of them conversions and 140
+// masks and shifts of codes) and by what they wait for one another, with 20 warps an SM: issue slots 59%, logic pipe 48%, none
+// is full. 48 sequences in pages, 8 KV heads of 128, 4 rows: 53 us, 2.8 TB/s, where the bytes take 22; one token over 2048
+// positions 5.3 us.
 template <int D, int NT>
 __global__ void __launch_bounds__(kWarps * 32, kBlocksPerSm) k_weigh_few(const __grid_constant__ WeighBatch b) {
     using S = Stage<D, 1>;
@@ -183,7 +184,10 @@ cudaError_t launch_weigh(WeighBatch& b, int head_dim, cudaStream_t st, int num_s
     rows *= b.G;
     if (rows == 0) return cudaSuccess;
     // 8 KV heads of 128, 2048 / 16384 positions: 8 rows 5.7 / 8.4 us here and 8.4 / 16.0 us on tcgen05, 16 rows 7.3 / 10.2 and
-    // 8.4 / 15.9 us; 20 rows, a third tile of them here, 8.6 / 15.9 us there.
+    // 8.4 / 15.9 us; 20 rows, a third tile of them here, 8.6 / 15.9 us there.  48 sequences of 2048 / 6000 positions (graphs, 7 us
+    // of them not the kernel's): 4 rows 32 / 67 us here and 65 / 147 there, 16 rows 38 / 81 and 67 / 149.
+    // The rule goes by the longest of the call's sequences: 47 tokens and one sequence of 5 take 65 / 149 us in one call, 44 / 81 in
+    // two, so a server calls for them apart.
     if (rows > 16) return launch_weigh_tc(b, head_dim, st, num_sms);
     const int64_t units = attend_pairs(b, kWeighRows);
     if (head_dim == 128)

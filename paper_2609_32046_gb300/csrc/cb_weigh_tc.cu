@@ -9,6 +9,8 @@
 //   24      issues tcgen05.mma; 25 writes the weights; 26 finds the run's segments, one ahead
 // Up to kStages tiles of query rows stay in shared memory while the tiles of positions pass through a ring; with
 // more rows the ring's tiles of positions stay and the rows pass.
+// lse * log2(e) is rounded once, and unlike in k_weigh_few what that leaves out is not multiplied into the weight, which would
+// take a second read of shared memory for every product: weights are off by up to 2^-23 |lse| of themselves.
 // A row whose lse is not finite is a row of zeros with an lse of infinity: it adds nothing.  A row's sum is one over its columns
 // in a fixed order, whatever segment it is in.
 //
